@@ -410,6 +410,133 @@ mt_status mt_profile_query(mt_model *model, int kernel, double *total_ms, int64_
  * becomes +-inf.  HOST pointers; needs no device; n = 0 or a NULL pointer does nothing. */
 void mt_round_bf16(const float *src, uint16_t *dst, size_t n);
 
+/* ---- A recurrent layer for serving: products in 8 bits, causal convolution, selective scan ----
+ *
+ * The operators of a layer of the state space kind, in the two forms of the recurrent cells
+ * above: over whole prompts (a padded, ragged batch, as mt_encode) and for single tokens of
+ * hypotheses whose states are gathered along the beam (as mt_decoder_step; src_row is the
+ * row_out of mt_beam_topk).  In the order of their use:
+ *   [x' | z] = u Win            mt_i8_product       x  = conv(x')    mt_ssm_conv, mt_ssm_conv_step
+ *   [r | B | C] = x Wx, dt = r Wdt  mt_i8_product   y  = scan(...)   mt_ssm_scan, mt_ssm_step
+ *   out = y Wout                mt_i8_product       (and the output layer, for mt_beam_topk)
+ * They take these conventions in place of those above:
+ *   - Row matrices (x, y, dt, ...) have a row stride in elements (ld.. >= the row's width), so that
+ *     a column range of a wider matrix can be passed; their pointers need only the alignment
+ *     of their element type (16-byte aligned pointers and strides take wider accesses).  The
+ *     positions of a padded batch are rows b*S + i.
+ *   - A call reads its handle and does not change it: one handle serves several streams and
+ *     threads at once, each call with its own outputs and workspace.  The current device must
+ *     be the one the handle was loaded on (MT_ERR_STATE otherwise).  Calls may be captured into
+ *     a graph; they allocate nothing and record kernels only.
+ *   - An output that overlaps an input, the workspace or another output is refused (MT_ERR_ARG),
+ *     except where a call says otherwise; columns of one wider matrix (the same stride) do not
+ *     overlap.
+ *   - Results do not depend on how a call is split over the chip's units, and are the same in
+ *     every run, except that the length of a prompt batch (S) and its number of sentences choose
+ *     where a long scan is cut, which moves its results by roundings. */
+
+/* An [K, N] matrix in 8 bits with a scale per column:
+ *   q[k, n] = rint(W[k, n] * (127 / a_n)), s_n = a_n / 127, a_n = max_k |W[k, n]|,
+ * every operation in fp32, ties to even; a column with a_n < 2^-100 is all zeros (s_n = 0). */
+typedef struct mt_i8_matrix mt_i8_matrix; /* opaque, library-owned */
+
+/* Quantise W [K, N] fp32 row-major ([in x out], as the matrices of mt_weights) and copy it and
+ * bias [N] fp32 (or NULL) into library-owned memory of the current device.  Both pointers may
+ * be host or device memory.  1 <= K <= 65536, 1 <= N <= 2^24; a NaN or an infinity in W is
+ * MT_ERR_ARG.  Synchronises the device before (so W may come from any stream) and after. */
+mt_status mt_i8_load(int K, int N, const float *W, const float *bias, mt_i8_matrix **out);
+
+/* Release a matrix and its device memory (synchronises the device). */
+mt_status mt_i8_free(mt_i8_matrix *w);
+
+/* Workspace bytes of mt_i8_product for M rows (0 on bad input): the rows in 8 bits and their
+ * scales.  A workspace for more rows serves fewer. */
+size_t mt_i8_workspace_bytes(const mt_i8_matrix *w, int M);
+
+/* y[m, n] = (sum_k qx[m, k] q[k, n]) s_n s_m + bias_n for M rows x [M, K], each quantised within
+ * the call as the columns of W are (qx = rint(x * (127 / a_m)), s_m = a_m / 127): the sums are
+ * exact, and the two scales and the bias are applied in fp32 in this order.  A row that holds a
+ * NaN or an infinity gives NaN throughout.  x_dtype and y_dtype: MT_F32 or MT_BF16, each.
+ * 1 <= M <= 2^24. */
+mt_status mt_i8_product(mt_i8_matrix *w, int M, const void *x, int x_dtype, int64_t ldx, void *y, int y_dtype,
+                        int64_t ldy, void *ws, size_t ws_bytes, void *stream);
+
+/* A cell of the layer: D channels, each with a short causal convolution of width W and N states.
+ *   D: 1..65536.  N: 1..256.  G: 1..D, a divisor of D: groups of D/G channels that share their
+ *   B and C (channel d belongs to group d / (D/G)).  W: 0..8; 0: no convolution.
+ *   dtype: MT_F32 or MT_BF16, the type of x, dt, B, C, z, y and of the convolution's state.
+ *     Parameters, arithmetic and the scan's states are fp32.
+ *   conv_silu: 0/1 — v * sigmoid(v) after the convolution. */
+typedef struct {
+  int32_t D, N, G, W;
+  int32_t dtype;
+  int32_t conv_silu;
+} mt_ssm_config;
+
+/* Parameters: HOST pointers to fp32, only read during mt_ssm_load.
+ *   A[D,N]: finite, <= 0; dt_bias[D] or NULL (zero); skip[D] or NULL (none);
+ *   conv_w[D,W] (oldest position first) and conv_b[D] or NULL (zero), read only if W > 0. */
+typedef struct {
+  const float *A, *dt_bias, *skip;
+  const float *conv_w, *conv_b;
+} mt_ssm_weights;
+
+typedef struct mt_ssm mt_ssm; /* opaque, library-owned */
+
+/* Copy the parameters into library-owned memory of the current device.  Synchronous. */
+mt_status mt_ssm_load(const mt_ssm_config *cfg, const mt_ssm_weights *w, mt_ssm **out);
+
+/* Release a cell and its device memory (synchronises the device). */
+mt_status mt_ssm_free(mt_ssm *cell);
+
+/* Workspace bytes of mt_ssm_scan for B prompts of padded length S (0 on bad input).  Always
+ * positive otherwise; a workspace for one (B, S) need not serve another. */
+size_t mt_ssm_workspace_bytes(const mt_ssm *cell, int B, int S);
+
+/* The convolution over B prompts of padded length S:
+ *   y[b,t,d] = act(conv_b[d] + sum_{j<W} conv_w[d,j] x[b, t-W+1+j, d]),   t < len[b],
+ *   positions before the first taken from state_in[b] (its last W-1 inputs; NULL: zeros).
+ *   len [B] int32 (NULL: all S): valid positions of each prompt, 0..S (clamped, reported by
+ *     mt_ssm_device_errors).  Positions behind them are neither read nor written.
+ *   x, y [B*S, D]; state_in, state_out [B, W-1, D] (16-byte aligned; state_out or both NULL): the
+ *     last W-1 inputs after the prompt, oldest first, for the next piece of it or mt_ssm_conv_step.
+ * MT_ERR_STATE for a cell without a convolution.  B, S >= 1, B*S <= 2^24. */
+mt_status mt_ssm_conv(mt_ssm *cell, int B, int S, const int32_t *len, const void *x, int64_t ldx,
+                      const void *state_in, void *y, int64_t ldy, void *state_out, void *stream);
+
+/* The convolution for one token of each of M hypotheses: row m continues state_in[src_row[m]]
+ * (NULL: its own row m), x, y [M, D], state_in [n_state_rows, W-1, D], state_out [M, W-1, D] (both
+ * ignored for W = 1).  src_row out of range is clamped and reported by mt_ssm_device_errors.
+ * Without src_row state_out may be state_in.  1 <= M, n_state_rows <= 2^24 (n_state_rows >= M
+ * without src_row). */
+mt_status mt_ssm_conv_step(mt_ssm *cell, int M, const int32_t *src_row, int n_state_rows, const void *x, int64_t ldx,
+                           const void *state_in, void *y, int64_t ldy, void *state_out, void *stream);
+
+/* The selective scan over B prompts of padded length S: with D_t = softplus(dt[b,t,d] + dt_bias[d]),
+ *   h_t[n] = exp(D_t A[d,n]) h_{t-1}[n] + D_t x[b,t,d] B[b,t,g,n],  g = d / (D/G),
+ *   y[b,t,d] = (sum_n C[b,t,g,n] h_t[n] + skip[d] x[b,t,d]) * z sigmoid(z),  z = z[b,t,d]
+ * for t < len[b] (as in mt_ssm_conv); z NULL: no gate.
+ *   x, dt, z, y [B*S, D]; bmat, cmat [B*S, G*N], both with row stride ldbc;
+ *   state_in [B, D, N] fp32 (NULL: zeros): the state before the first position;
+ *   state_out [B, D, N] fp32 or NULL: the state after the last valid one (a prompt of length 0
+ *     copies its state_in).  Both 16-byte aligned.
+ * B, S >= 1, B*S <= 2^24. */
+mt_status mt_ssm_scan(mt_ssm *cell, int B, int S, const int32_t *len, const void *x, int64_t ldx, const void *dt,
+                      int64_t lddt, const void *bmat, const void *cmat, int64_t ldbc, const void *z, int64_t ldz,
+                      const float *state_in, void *y, int64_t ldy, float *state_out, void *ws, size_t ws_bytes,
+                      void *stream);
+
+/* One token of each of M hypotheses: the same with state row src_row[m] of state_in
+ * [n_state_rows, D, N] (NULL: row m) before and row m of state_out [M, D, N] after it; x, dt, z, y
+ * [M, D], bmat, cmat [M, G*N].  src_row, aliasing and sizes as mt_ssm_conv_step. */
+mt_status mt_ssm_step(mt_ssm *cell, int M, const int32_t *src_row, int n_state_rows, const void *x, int64_t ldx,
+                      const void *dt, int64_t lddt, const void *bmat, const void *cmat, int64_t ldbc, const void *z,
+                      int64_t ldz, const float *state_in, void *y, int64_t ldy, float *state_out, void *stream);
+
+/* Reads and clears the cell's device-side error bits (synchronises the device): bit 1 = a src_row
+ * out of range, bit 2 = a len out of range. */
+mt_status mt_ssm_device_errors(mt_ssm *cell, int32_t *flags);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char *mt_last_error(void);
 

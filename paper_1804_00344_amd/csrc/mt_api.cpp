@@ -11,11 +11,11 @@
 #include <new>
 #include <vector>
 
-#include "mt_internal.h"
+#include "mt_host.h"
 
 using namespace mt;
 
-namespace {
+namespace mt {
 
 thread_local char g_err[512] = "";
 
@@ -27,11 +27,9 @@ mt_status fail(mt_status s, const char *fmt, ...) {
   return s;
 }
 
-#define HIP_TRY(expr)                                                                      \
-  do {                                                                                     \
-    hipError_t e_ = (expr);                                                                \
-    if (e_ != hipSuccess) return fail(MT_ERR_HIP, "%s: %s", #expr, hipGetErrorString(e_)); \
-  } while (0)
+}  // namespace mt
+
+namespace {
 
 constexpr uint32_t kMagic = 0x4d545350u;  // "MTSP"
 constexpr int kNPad = 256;                // N padding of packed weights (>= any tile BN)
@@ -42,8 +40,6 @@ constexpr int kKPadFrag = 128;            // K padding of bf16 weights (one LDS 
 // any batch, only the speed of other row counts may differ.
 constexpr long kRefRows = 768, kRefCtxRows = 4096, kRefSentences = 64;
 constexpr int kMaxTransitions = 16;  // recurrent-only GRU blocks after GRU 2
-
-size_t rup(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 struct Packed {
   void *p = nullptr;
@@ -118,8 +114,6 @@ struct mt_model {
 namespace {
 
 bool valid_model(const mt_model *m) { return m && m->magic == kMagic; }
-
-bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
 mt_status check_cfg(const mt_config *c) {
   if (!c) return fail(MT_ERR_ARG, "config is NULL");
@@ -388,18 +382,6 @@ struct Timed {  // records events around one launch when profiling is on
     if (e_ != hipSuccess) return fail(MT_ERR_HIP, "%s: %s", #expr, hipGetErrorString(e_)); \
   } while (0)
 #define LAUNCH(kid, expr) LAUNCH_IF(kid, true, expr)
-
-mt_status check_dev_ptr(const void *p, const char *name, size_t align = 16) {
-  if (!p) return fail(MT_ERR_ARG, "%s is NULL", name);
-  if (!aligned(p, align)) return fail(MT_ERR_ARG, "%s is not %zu-byte aligned", name, align);
-  return MT_OK;
-}
-
-#define CHECK(expr)                 \
-  do {                              \
-    mt_status s_ = (expr);          \
-    if (s_ != MT_OK) return s_;     \
-  } while (0)
 
 }  // namespace
 

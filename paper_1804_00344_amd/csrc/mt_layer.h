@@ -1,0 +1,77 @@
+// Internal declarations of the recurrent layer's operators (mt_i8.hip, mt_conv.hip, mt_scan.hip).
+#pragma once
+
+#include "mt_internal.h"
+
+namespace mt {
+
+constexpr int kI8Block = 32;   // rows of a fragment block: 32 rows x 32 k in 1 KiB (see mt_i8.hip)
+constexpr int kI8KPad = 128;   // k padding of both operands
+constexpr int kI8Pad = 256;    // row and column padding of both operands
+constexpr int kI8MaxK = 65536; // 127 * 127 * 65536 < 2^31
+
+// ---- products in 8 bits (mt_i8.hip) ----
+struct I8Problem {
+  const void *x;        // [M][ldx] fp32 or bf16
+  long long ldx;
+  int x_bf16;
+  const int8_t *wq;     // packed columns in fragment order
+  const float *ws;      // [Np] column scales, zero padded
+  const float *bias;    // [N] or NULL
+  void *y;              // [M][ldy]
+  long long ldy;
+  int y_bf16;
+  int M, N, K, Kp;
+  int8_t *xq;           // workspace: rows in fragment order
+  float *xs;            // and their scales
+  int num_cu;
+};
+hipError_t launch_i8_product(const I8Problem &p, hipStream_t st);
+// quantises W [K][N] (device memory) into wq [Np/32][Kp/32][1024] and s [Np]; *bad is set to 1 where
+// W holds a NaN or an infinity
+hipError_t launch_i8_pack(const float *W, int K, int N, int Kp, int Np, int8_t *wq, float *s, int *bad, hipStream_t st);
+
+// ---- causal convolution (mt_conv.hip) ----
+struct ConvArgs {
+  const float *w;       // [W][D]
+  const float *b;       // [D]
+  int D, W, silu, bf16_io;
+  int B, S;             // prompts; a step: rows M and S = 1
+  const int32_t *len;   // [B] or NULL
+  const int32_t *row;   // step: state rows or NULL
+  int n_rows;
+  const void *x;
+  long long ldx;
+  void *y;
+  long long ldy;
+  const void *state_in; // [rows][W-1][D] or NULL
+  void *state_out;
+  int32_t *err;
+};
+hipError_t launch_conv(const ConvArgs &a, hipStream_t st);
+hipError_t launch_conv_step(const ConvArgs &a, hipStream_t st);
+
+// ---- selective scan (mt_scan.hip) ----
+struct ScanArgs {
+  const float *A2;      // [D][Np] A * log2(e), zero padded to Np = scan_padded_states(N)
+  const float *dt_bias, *skip;  // [D] each (skip: zeros if there is none)
+  int D, N, Np, G, bf16_io;
+  int B, S;             // prompts; a step: rows M and S = 1
+  const int32_t *len;
+  const int32_t *row;
+  int n_rows;
+  const void *x, *dt, *bm, *cm, *z;
+  long long ldx, lddt, ldbc, ldz, ldy;
+  void *y;
+  const float *state_in;
+  float *state_out;
+  void *ws;
+  int32_t *err;
+  int num_cu;
+};
+int scan_padded_states(int N);
+size_t scan_workspace_bytes(int B, int S, int D, int N, int num_cu);
+hipError_t launch_scan(const ScanArgs &a, hipStream_t st);
+hipError_t launch_scan_step(const ScanArgs &a, hipStream_t st);
+
+}  // namespace mt

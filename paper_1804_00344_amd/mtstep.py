@@ -56,6 +56,18 @@ class mt_taps(C.Structure):
     _fields_ = [("s1", C.c_void_p), ("c", C.c_void_p), ("t", C.c_void_p)]
 
 
+class mt_ssm_config(C.Structure):
+    _fields_ = [("D", C.c_int32), ("N", C.c_int32), ("G", C.c_int32), ("W", C.c_int32), ("dtype", C.c_int32),
+                ("conv_silu", C.c_int32)]
+
+
+SSM_WEIGHT_FIELDS = ["A", "dt_bias", "skip", "conv_w", "conv_b"]
+
+
+class mt_ssm_weights(C.Structure):
+    _fields_ = [(n, _fp) for n in SSM_WEIGHT_FIELDS]
+
+
 _lib = None
 _vp = C.c_void_p
 
@@ -114,6 +126,26 @@ def lib() -> C.CDLL:
         L.mt_ensemble_joint_ok.restype = C.c_int
         L.mt_recomputed_rows.argtypes = [_vp, C.POINTER(C.c_int64)]
         L.mt_recomputed_rows.restype = C.c_int
+        i64, sz = C.c_int64, C.c_size_t
+        L.mt_i8_load.argtypes = [C.c_int, C.c_int, _vp, _vp, C.POINTER(_vp)]
+        L.mt_i8_free.argtypes = [_vp]
+        L.mt_i8_workspace_bytes.argtypes = [_vp, C.c_int]
+        L.mt_i8_workspace_bytes.restype = sz
+        L.mt_i8_product.argtypes = [_vp, C.c_int, _vp, C.c_int, i64, _vp, C.c_int, i64, _vp, sz, _vp]
+        L.mt_ssm_load.argtypes = [C.POINTER(mt_ssm_config), C.POINTER(mt_ssm_weights), C.POINTER(_vp)]
+        L.mt_ssm_free.argtypes = [_vp]
+        L.mt_ssm_workspace_bytes.argtypes = [_vp, C.c_int, C.c_int]
+        L.mt_ssm_workspace_bytes.restype = sz
+        L.mt_ssm_conv.argtypes = [_vp, C.c_int, C.c_int, _vp, _vp, i64, _vp, _vp, i64, _vp, _vp]
+        L.mt_ssm_conv_step.argtypes = [_vp, C.c_int, _vp, C.c_int, _vp, i64, _vp, _vp, i64, _vp, _vp]
+        L.mt_ssm_scan.argtypes = [_vp, C.c_int, C.c_int, _vp, _vp, i64, _vp, i64, _vp, _vp, i64, _vp, i64, _vp, _vp,
+                                  i64, _vp, _vp, sz, _vp]
+        L.mt_ssm_step.argtypes = [_vp, C.c_int, _vp, C.c_int, _vp, i64, _vp, i64, _vp, _vp, i64, _vp, i64, _vp, _vp,
+                                  i64, _vp, _vp]
+        L.mt_ssm_device_errors.argtypes = [_vp, C.POINTER(C.c_int32)]
+        for f in ("mt_i8_load", "mt_i8_free", "mt_i8_product", "mt_ssm_load", "mt_ssm_free", "mt_ssm_conv",
+                  "mt_ssm_conv_step", "mt_ssm_scan", "mt_ssm_step", "mt_ssm_device_errors"):
+            getattr(L, f).restype = C.c_int
         L.mt_round_bf16.argtypes = [_vp, _vp, C.c_size_t]
         L.mt_round_bf16.restype = None
         for f in ("mt_load_weights", "mt_free", "mt_precompute_ctx", "mt_decoder_step", "mt_beam_topk",
@@ -353,3 +385,239 @@ def mt_profile_query(model: Model, kernel) -> tuple:
     ms, n = C.c_double(0), C.c_int64(0)
     _check(lib().mt_profile_query(model.handle, k, C.byref(ms), C.byref(n)))
     return float(ms.value), int(n.value)
+
+
+# ---- recurrent layer: products in 8 bits, causal convolution, selective scan ----------------------
+#
+# Row matrices are torch tensors [..., width] whose last dimension is contiguous and whose rows are
+# equally spaced (a column range of a wider matrix is fine); sizes come from their shapes.
+
+class I8Matrix:
+    """Owns an mt_i8_matrix handle (freed with mt_i8_free)."""
+
+    def __init__(self, handle: int, K: int, N: int, device):
+        self.handle, self.K, self.N, self.device = handle, K, N, device
+
+    def __del__(self):
+        if getattr(self, "handle", None):
+            try:
+                lib().mt_i8_free(self.handle)
+            except Exception:
+                pass
+            self.handle = None
+
+
+class Ssm:
+    """Owns an mt_ssm handle (freed with mt_ssm_free)."""
+
+    def __init__(self, handle: int, cfg: mt_ssm_config, device):
+        import torch
+        self.handle, self.cfg, self.device = handle, cfg, device
+        self.D, self.W = cfg.D, cfg.W
+        self.GN, self.state_shape = cfg.G * cfg.N, (cfg.D, cfg.N)
+        self.dtype = torch.bfloat16 if cfg.dtype == MT_BF16 else torch.float32
+
+    def __del__(self):
+        if getattr(self, "handle", None):
+            try:
+                lib().mt_ssm_free(self.handle)
+            except Exception:
+                pass
+            self.handle = None
+
+
+def _current_device():
+    import torch
+    return torch.device("cuda", torch.cuda.current_device()) if torch.cuda.is_available() else None
+
+
+def _rows(t, name, lead, width, dtype, device):
+    """(address, row stride) of a row matrix of shape lead + (width,)."""
+    if tuple(t.shape) != lead + (width,):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}: need {lead + (width,)}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} is {t.dtype}: need {dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}: need {device}")
+    st = t.stride()
+    if width > 1 and st[-1] != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    if len(lead) == 1:
+        return t.data_ptr(), st[0] if lead[0] > 1 else width
+    B, S = lead
+    ld = st[1] if S > 1 else (st[0] if B > 1 else width)
+    if B > 1 and st[0] != S * ld:
+        raise ValueError(f"the rows of {name} must be equally spaced")
+    return t.data_ptr(), ld
+
+
+def _packed(t, name, shape, dtype, device):
+    """Address of a contiguous tensor of a given shape, or None."""
+    if t is None:
+        return None
+    if tuple(t.shape) != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: need a contiguous {dtype} tensor of shape {shape} on {device}")
+    return t.data_ptr()
+
+
+def _index(t, name, n, device):
+    import torch
+    return _packed(t, name, (n,), torch.int32, device)
+
+
+def _host_or_device(a):
+    """An fp32 array and its address: a device tensor stays where it is."""
+    import torch
+    if isinstance(a, torch.Tensor):
+        a = a.detach().to(torch.float32).contiguous()
+        return a, a.data_ptr()
+    a = np.ascontiguousarray(a, np.float32)
+    return a, a.ctypes.data
+
+
+def mt_i8_load(W, bias=None) -> I8Matrix:
+    """W [K, N], bias [N] (or None): fp32, numpy arrays or torch tensors on any device."""
+    if len(W.shape) != 2 or (bias is not None and tuple(bias.shape) != (W.shape[1],)):
+        raise ValueError("need W [K, N] and bias [N]")
+    K, N = (int(n) for n in W.shape)
+    w, wp = _host_or_device(W)
+    b, bp = _host_or_device(bias) if bias is not None else (None, None)
+    h = _vp()
+    _check(lib().mt_i8_load(K, N, wp, bp, C.byref(h)))
+    return I8Matrix(h.value, K, N, _current_device())
+
+
+def mt_i8_free(mat: I8Matrix):
+    if mat.handle:
+        _check(lib().mt_i8_free(mat.handle))
+        mat.handle = None
+
+
+def mt_i8_workspace_bytes(mat: I8Matrix, M: int) -> int:
+    return int(lib().mt_i8_workspace_bytes(mat.handle, M))
+
+
+def _io(t, name):
+    import torch
+    if t.dtype == torch.float32:
+        return MT_F32
+    if t.dtype == torch.bfloat16:
+        return MT_BF16
+    raise ValueError(f"{name} is {t.dtype}: need float32 or bfloat16")
+
+
+def mt_i8_product(mat: I8Matrix, x, y, ws, stream=None):
+    """y = x W + bias with both operands in 8 bits; x [..., K], y [..., N] of the same leading shape."""
+    lead = tuple(x.shape[:-1])
+    if len(lead) not in (1, 2):
+        raise ValueError("x must have two or three dimensions")
+    xt, yt = _io(x, "x"), _io(y, "y")
+    xp, ldx = _rows(x, "x", lead, mat.K, x.dtype, mat.device)
+    yp, ldy = _rows(y, "y", lead, mat.N, y.dtype, mat.device)
+    M = lead[0] if len(lead) == 1 else lead[0] * lead[1]
+    _check(lib().mt_i8_product(mat.handle, M, xp, xt, ldx, yp, yt, ldy, _ptr(ws), ws.numel() * ws.element_size(),
+                               _stream(stream)))
+
+
+def make_ssm_config(D, N, *, groups=1, conv=0, conv_silu=True, dtype="f32"):
+    return mt_ssm_config(D, N, groups, conv, MT_BF16 if dtype == "bf16" else MT_F32, int(conv_silu))
+
+
+def mt_ssm_load(cfg: mt_ssm_config, weights) -> Ssm:
+    """weights: fp32 numpy arrays or torch tensors by field name (see mt_ssm_weights)."""
+    shapes = dict(A=(cfg.D, cfg.N), dt_bias=(cfg.D,), skip=(cfg.D,), conv_w=(cfg.D, cfg.W), conv_b=(cfg.D,))
+    w, keep = mt_ssm_weights(), []
+    for n in SSM_WEIGHT_FIELDS:
+        a = weights.get(n)
+        if a is None:
+            continue
+        if hasattr(a, "detach"):
+            a = a.detach().float().cpu().numpy()
+        a = np.ascontiguousarray(a, np.float32)
+        if a.shape != shapes[n]:
+            raise ValueError(f"{n} has shape {a.shape}: need {shapes[n]}")
+        keep.append(a)
+        setattr(w, n, a.ctypes.data_as(_fp))
+    h = _vp()
+    _check(lib().mt_ssm_load(C.byref(cfg), C.byref(w), C.byref(h)))
+    return Ssm(h.value, mt_ssm_config.from_buffer_copy(cfg), _current_device())
+
+
+def mt_ssm_free(cell: Ssm):
+    if cell.handle:
+        _check(lib().mt_ssm_free(cell.handle))
+        cell.handle = None
+
+
+def mt_ssm_workspace_bytes(cell: Ssm, B: int, S: int) -> int:
+    return int(lib().mt_ssm_workspace_bytes(cell.handle, B, S))
+
+
+def mt_ssm_device_errors(cell: Ssm) -> int:
+    f = C.c_int32(0)
+    _check(lib().mt_ssm_device_errors(cell.handle, C.byref(f)))
+    return int(f.value)
+
+
+def mt_ssm_conv(cell: Ssm, x, y, *, lens=None, state_in=None, state_out=None, stream=None):
+    """x, y [B, S, D]; lens [B] int32; state_in, state_out [B, W-1, D]."""
+    dt, dev = cell.dtype, cell.device
+    B, S = lead = tuple(x.shape[:-1])
+    st = (B, max(cell.W - 1, 0), cell.D)
+    xp, ldx = _rows(x, "x", lead, cell.D, dt, dev)
+    yp, ldy = _rows(y, "y", lead, cell.D, dt, dev)
+    _check(lib().mt_ssm_conv(cell.handle, B, S, _index(lens, "lens", B, dev), xp, ldx,
+                             _packed(state_in, "state_in", st, dt, dev), yp, ldy,
+                             _packed(state_out, "state_out", st, dt, dev), _stream(stream)))
+
+
+def mt_ssm_conv_step(cell: Ssm, x, y, state_in, state_out, *, src_row=None, stream=None):
+    """x, y [M, D]; state_in [rows, W-1, D], state_out [M, W-1, D]; src_row [M] int32."""
+    dt, dev, W1 = cell.dtype, cell.device, max(cell.W - 1, 0)
+    M, = lead = tuple(x.shape[:-1])
+    rows = state_in.shape[0] if state_in is not None else M
+    xp, ldx = _rows(x, "x", lead, cell.D, dt, dev)
+    yp, ldy = _rows(y, "y", lead, cell.D, dt, dev)
+    _check(lib().mt_ssm_conv_step(cell.handle, M, _index(src_row, "src_row", M, dev), rows, xp, ldx,
+                                  _packed(state_in, "state_in", (rows, W1, cell.D), dt, dev), yp, ldy,
+                                  _packed(state_out, "state_out", (M, W1, cell.D), dt, dev), _stream(stream)))
+
+
+def _scan_rows(cell, lead, x, dt, bmat, cmat, y, z):
+    """The row-matrix arguments of the scan in the order of the C calls, without the states."""
+    t, dev, D = cell.dtype, cell.device, cell.D
+    xp, ldx = _rows(x, "x", lead, D, t, dev)
+    dp, ldd = _rows(dt, "dt", lead, D, t, dev)
+    bp, ldb = _rows(bmat, "bmat", lead, cell.GN, t, dev)
+    cp, ldc = _rows(cmat, "cmat", lead, cell.GN, t, dev)
+    if ldb != ldc:
+        raise ValueError("bmat and cmat must have the same row stride")
+    zp, ldz = _rows(z, "z", lead, D, t, dev) if z is not None else (None, 0)
+    yp, ldy = _rows(y, "y", lead, D, t, dev)
+    return (xp, ldx, dp, ldd, bp, cp, ldb, zp, ldz), (yp, ldy)
+
+
+def mt_ssm_scan(cell: Ssm, x, dt, bmat, cmat, y, *, z=None, lens=None, state_in=None, state_out=None, ws, stream=None):
+    """x, dt, z, y [B, S, D]; bmat, cmat [B, S, G*N]; lens [B] int32; state_in, state_out [B, D, N] fp32."""
+    import torch
+    dev = cell.device
+    B, S = lead = tuple(x.shape[:-1])
+    ins, out = _scan_rows(cell, lead, x, dt, bmat, cmat, y, z)
+    st = (B,) + cell.state_shape
+    _check(lib().mt_ssm_scan(cell.handle, B, S, _index(lens, "lens", B, dev), *ins,
+                             _packed(state_in, "state_in", st, torch.float32, dev), *out,
+                             _packed(state_out, "state_out", st, torch.float32, dev), _ptr(ws),
+                             ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def mt_ssm_step(cell: Ssm, x, dt, bmat, cmat, y, state_in, state_out, *, z=None, src_row=None, stream=None):
+    """x, dt, z, y [M, D]; bmat, cmat [M, G*N]; state_in [rows, D, N], state_out [M, D, N] fp32; src_row [M] int32."""
+    import torch
+    dev = cell.device
+    M, = lead = tuple(x.shape[:-1])
+    rows = state_in.shape[0]
+    ins, out = _scan_rows(cell, lead, x, dt, bmat, cmat, y, z)
+    _check(lib().mt_ssm_step(cell.handle, M, _index(src_row, "src_row", M, dev), rows, *ins,
+                             _packed(state_in, "state_in", (rows,) + cell.state_shape, torch.float32, dev), *out,
+                             _packed(state_out, "state_out", (M,) + cell.state_shape, torch.float32, dev),
+                             _stream(stream)))

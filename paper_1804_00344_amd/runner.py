@@ -327,3 +327,85 @@ class Ensemble:
                 d.cur = 1 - d.cur
             d.first = False
         return [d.state[d.cur] for d in self.members]
+
+
+class SsmLayer:
+    """A recurrent layer of the state space kind for serving: over a padded batch of prompts, then
+    token by token for hypotheses whose states are gathered along the beam, as the Decoder's are.
+
+        [x' | z] = u Win,  x = conv(x'),  [r | B | C] = x Wx,  dt = r Wdt,  y = scan(x, dt, B, C; z),  out = y Wout
+
+    weights: Win [E, 2D], Wx [D, R + 2GN], Wdt [R, D], Wout [D, E], optional biases bin [2D], bout [E]
+    (products in 8 bits), and the cell's A, dt_bias, skip, conv_w, conv_b (see mt_ssm_weights)."""
+
+    def __init__(self, weights, *, groups: int = 1, conv_silu: bool = True, dtype: str = "bf16", device: str = "cuda:0"):
+        w = weights
+        self.E, self.D, self.R = w["Win"].shape[0], w["Wout"].shape[0], w["Wdt"].shape[0]
+        self.N, self.GN, self.W = w["A"].shape[1], groups * w["A"].shape[1], w["conv_w"].shape[1]
+        self.device = torch.device(device)
+        self.io_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        cfg = mt.make_ssm_config(self.D, self.N, groups=groups, conv=self.W, conv_silu=conv_silu, dtype=dtype)
+        with torch.cuda.device(self.device):
+            self.cell = mt.mt_ssm_load(cfg, {k: w.get(k) for k in mt.SSM_WEIGHT_FIELDS})
+            self.win = mt.mt_i8_load(w["Win"], w.get("bin"))
+            self.wx, self.wdt = mt.mt_i8_load(w["Wx"]), mt.mt_i8_load(w["Wdt"])
+            self.wout = mt.mt_i8_load(w["Wout"], w.get("bout"))
+
+    def _buffers(self, lead):
+        """Activations and workspace of a call over rows of shape lead."""
+        io = dict(dtype=self.io_dtype, device=self.device)
+        M = int(np.prod(lead))
+        # one product at a time uses the workspace, the scan after them
+        n = max([mt.mt_i8_workspace_bytes(w, M) for w in (self.win, self.wx, self.wdt, self.wout)] +
+                ([mt.mt_ssm_workspace_bytes(self.cell, *lead)] if len(lead) == 2 else []))
+        return dict(xz=torch.zeros(*lead, 2 * self.D, **io), x=torch.zeros(*lead, self.D, **io),
+                    rbc=torch.zeros(*lead, self.R + 2 * self.GN, **io), dt=torch.zeros(*lead, self.D, **io),
+                    y=torch.zeros(*lead, self.D, **io), out=torch.zeros(*lead, self.E, **io),
+                    ws=torch.empty(n, dtype=torch.uint8, device=self.device))
+
+    def _states(self, rows):
+        return (torch.zeros(rows, self.W - 1, self.D, dtype=self.io_dtype, device=self.device),
+                torch.zeros(rows, self.D, self.N, dtype=torch.float32, device=self.device))
+
+    def set_batch(self, B: int, S: int, K: int):
+        """Buffers for B prompts of padded length S and K hypotheses of each."""
+        self.B, self.S, self.K, self.M = B, S, K, B * K
+        self.pb, self.sb = self._buffers((B, S)), self._buffers((B * K,))
+        self.prompt_state = self._states(B)
+        self.beam_state = [self._states(B * K) for _ in range(2)]
+        self.cur = -1  # the states a step reads: the prompts' (-1), or those of the last step
+
+    def _project(self, u, f, stream):
+        mt.mt_i8_product(self.win, u, f["xz"], f["ws"], stream=stream)
+        return f["xz"][..., :self.D], f["xz"][..., self.D:]
+
+    def _inputs(self, f, stream):
+        mt.mt_i8_product(self.wx, f["x"], f["rbc"], f["ws"], stream=stream)
+        mt.mt_i8_product(self.wdt, f["rbc"][..., :self.R], f["dt"], f["ws"], stream=stream)
+        return f["x"], f["dt"], f["rbc"][..., self.R:self.R + self.GN], f["rbc"][..., self.R + self.GN:]
+
+    def prompt(self, u, lens=None, stream=None):
+        """u [B, S, E] in the io type, lens [B] int32: out [B, S, E] (valid positions); keeps the states."""
+        f, (cs, hs) = self.pb, self.prompt_state
+        xp, z = self._project(u, f, stream)
+        mt.mt_ssm_conv(self.cell, xp, f["x"], lens=lens, state_out=cs, stream=stream)
+        x, dt, bm, cm = self._inputs(f, stream)
+        mt.mt_ssm_scan(self.cell, x, dt, bm, cm, f["y"], z=z, lens=lens, state_out=hs, ws=f["ws"], stream=stream)
+        mt.mt_i8_product(self.wout, f["y"], f["out"], f["ws"], stream=stream)
+        self.cur = -1
+        return f["out"]
+
+    def step(self, u, src_row, stream=None):
+        """u [M, E]: out [M, E].  src_row [M] int32: the state row each hypothesis continues, of the prompts
+        (m // K) in the first step and of the previous step afterwards (row_out of mt_beam_topk)."""
+        f = self.sb
+        ci, hi = self.prompt_state if self.cur < 0 else self.beam_state[self.cur]
+        nxt = 0 if self.cur != 0 else 1
+        co, ho = self.beam_state[nxt]
+        xp, z = self._project(u, f, stream)
+        mt.mt_ssm_conv_step(self.cell, xp, f["x"], ci, co, src_row=src_row, stream=stream)
+        x, dt, bm, cm = self._inputs(f, stream)
+        mt.mt_ssm_step(self.cell, x, dt, bm, cm, f["y"], hi, ho, z=z, src_row=src_row, stream=stream)
+        mt.mt_i8_product(self.wout, f["y"], f["out"], f["ws"], stream=stream)
+        self.cur = nxt
+        return f["out"]

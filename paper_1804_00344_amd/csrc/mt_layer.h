@@ -70,7 +70,7 @@ struct ScanArgs {
   int num_cu;
 };
 int scan_padded_states(int N);
-size_t scan_workspace_bytes(int B, int S, int D, int N, int num_cu);
+size_t scan_workspace_bytes(int B, int S, int D, int N, int G, int num_cu);
 hipError_t launch_scan(const ScanArgs &a, hipStream_t st);
 hipError_t launch_scan_step(const ScanArgs &a, hipStream_t st);
 

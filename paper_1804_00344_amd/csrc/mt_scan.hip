@@ -2,6 +2,7 @@
 //   D_t = softplus(dt_t + dt_bias[d]),  h_t[n] = exp(D_t A[d,n]) h_{t-1}[n] + D_t x_t B_t[n],
 //   y_t = (sum_n C_t[n] h_t[n] + skip[d] x_t) * silu(z_t).
 #include <algorithm>
+#include <cmath>
 
 #include "mt_layer_dev.h"
 
@@ -11,22 +12,18 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// log(1 + e^v) = max(v, 0) + log1p(e^-|v|), log1p(e) = 2 atanh(s), s = e / (2 + e) <= 1/3, by the
-// atanh series to s^17 (its remainder is below 2^-27 of the sum): accurate for small e too, where
-// 1 + e would round e away.
+// log(1 + e^v) = max(v, 0) + log1p(e^-|v|), log1p(e) = 2 atanh(s), s = e / (2 + e) <= 1/3: accurate for
+// small e too, where 1 + e would round e away.  atanh(s) / s is a polynomial of degree 4 in s^2, fitted
+// at Chebyshev nodes of [0, 1/9]: within 2^-26.9.
 __device__ __forceinline__ float softplus(float v) {
   const float e = exp_acc(-fabsf(v));
   const float s = e * rcp_fast(2.0f + e), q = s * s;
-  float p = 1.0f / 17.0f;
-  p = fmaf(p, q, 1.0f / 15.0f);
-  p = fmaf(p, q, 1.0f / 13.0f);
-  p = fmaf(p, q, 1.0f / 11.0f);
-  p = fmaf(p, q, 1.0f / 9.0f);
-  p = fmaf(p, q, 1.0f / 7.0f);
-  p = fmaf(p, q, 1.0f / 5.0f);
-  p = fmaf(p, q, 1.0f / 3.0f);
+  float p = 0.14087328f;
+  p = fmaf(p, q, 0.13980709f);
+  p = fmaf(p, q, 0.20012426f);
+  p = fmaf(p, q, 0.33333158f);
   p = fmaf(p, q, 1.0f);
-  return fmaxf(v, 0.0f) + 2.0f * s * p;
+  return fmaf(s + s, p, fmaxf(v, 0.0f));
 }
 
 // Sum over the L neighbouring lanes of a channel (a power of two), the result in each
@@ -70,31 +67,90 @@ __device__ __forceinline__ void store_states(float *p, int n, bool wide, const f
 }
 
 struct ScanPlan {
+  int lanes;              // lanes per channel
   int chunks, chunk_len;  // pieces of the axis
-  int tile, ngr;          // positions of B and C staged together, groups of a workgroup's channels
+  int threads, ngr;       // of a workgroup; groups of its channels
   float *part;            // [B][chunks - 1][D][Np] state of each piece started from zero
   float *dsum;            // [B][chunks - 1][D] sum of D_t over it
 };
 
+// the value of lane j of each group of J lanes
+template <int J>
+__device__ __forceinline__ float bcast(float v, int j) {
+  if constexpr (J == 1) return v;
+  if constexpr (J == 2) return j == 0 ? dpp_mov<0xA0>(v) : dpp_mov<0xF5>(v);
+  switch (j) {
+    case 0: return dpp_mov<0x00>(v);
+    case 1: return dpp_mov<0x55>(v);
+    case 2: return dpp_mov<0xAA>(v);
+    default: return dpp_mov<0xFF>(v);
+  }
+}
+// lane j of each group of J receives the sum over its channel's L lanes of y[j]
+template <int L, int J>
+__device__ __forceinline__ float transpose_sum(float (&y)[J], int sub) {
+  if constexpr (L >= 16)
+#pragma unroll
+    for (int j = 0; j < J; ++j) y[j] += dpp_mov<0x140>(y[j]);  // row_mirror: lane 15 - l
+  if constexpr (L >= 8)
+#pragma unroll
+    for (int j = 0; j < J; ++j) y[j] += dpp_mov<0x141>(y[j]);  // row_half_mirror: lane 7 - l
+  if constexpr (J == 1) {
+    return y[0];
+  } else {
+    const bool o1 = sub & 1, o2 = sub & 2;
+    const float a = (o1 ? y[1] : y[0]) + dpp_mov<kDppQuadSwap1>(o1 ? y[0] : y[1]);
+    if constexpr (J == 2) {
+      return a;
+    } else {
+      const float b = (o1 ? y[3] : y[2]) + dpp_mov<kDppQuadSwap1>(o1 ? y[2] : y[3]);
+      return (o2 ? b : a) + dpp_mov<kDppQuadSwap2>(o2 ? a : b);
+    }
+  }
+}
+
+constexpr int kTile = 8;  // positions of B and C staged together
+
+// A workgroup takes the channels of its threads / LPC in one piece of a prompt; LPC lanes share a channel,
+// NS states each.  The work per position and channel (softplus, gate, skip) is spread over the lanes:
+// lane j of each J = min(LPC, 4) does it for the j-th of J positions.  B and C of the next tile and x,
+// dt and z of its positions are on their way while a tile is computed.  A tile is always computed whole:
+// behind the end the steps D_t are zero, which keeps the state as it is.
 template <typename T, int NS, int LPC, bool FINAL>
-__global__ void __launch_bounds__(kThreads) scan_kernel(ScanArgs a, ScanPlan pl) {
-  constexpr int CPB = kThreads / LPC;
+__global__ void __launch_bounds__(256, NS == 16 ? 2 : 4) scan_kernel(ScanArgs a, ScanPlan pl) {
+  constexpr int J = LPC < 4 ? LPC : 4, Np = NS * LPC, SLOTS = kTile / J;
+  constexpr int STAGE = Np / 16 > 4 ? Np / 16 : 4;  // elements of B and C that a thread holds for the next tile
   extern __shared__ __attribute__((aligned(16))) float lds[];
-  const int tid = threadIdx.x, sub = tid % LPC, n0 = sub * NS;
-  const int c0 = blockIdx.x * CPB;
+  const int tid = threadIdx.x, nthr = blockDim.x, cpb = nthr / LPC, sub = tid % LPC, n0 = sub * NS, tj = sub % J;
+  const int c0 = blockIdx.x * cpb;
   const int d = min(c0 + tid / LPC, a.D - 1);
   const bool owner = c0 + tid / LPC < a.D;
-  const int per = a.D / a.G;
-  const int g0 = c0 / per, ngr = min((c0 + CPB - 1) / per, a.G - 1) - g0 + 1, gi = d / per - g0;
-  const int tile = pl.tile, chunk = blockIdx.y;
-  const int tfl = pl.ngr * a.Np;  // floats of B (and of C) per position
-  const bool wide = a.N % 4 == 0;
-  const int nn = min(NS, a.N - n0);  // states of this lane that exist
+  const int per = a.D / a.G, g0 = c0 / per, gi = d / per - g0;
+  const int chunk = blockIdx.y;
+  constexpr int nw = FINAL ? 2 : 1;        // the first pass reads B only
+  constexpr int grpl = kTile * nw * Np;    // floats of a group's tile
+  const int bufl = pl.ngr * grpl;          // and of all groups'
+  const bool wide = a.N % 4 == 0, gated = a.z != nullptr;
+  const long long ldz = gated ? a.ldz : a.ldx;
+  const int nn = min(NS, a.N - n0);        // states of this lane that exist
   float A2[NS];
 #pragma unroll
-  for (int i = 0; i < NS; ++i) A2[i] = a.A2[(size_t)d * a.Np + n0 + i];
+  for (int i = 0; i < NS; ++i) A2[i] = a.A2[(size_t)d * Np + n0 + i];
   const float dtb = a.dt_bias[d], skip = a.skip[d];
-  for (int i = tid; i < tile * tfl * 2; i += kThreads) lds[i] = 0.f;
+
+  // A tile in LDS: [group][position][B, C][Np], states that do not exist zero.  Element e of it: its
+  // position (none if there is no such element) and its source.
+  auto element = [&](int e, int &t, const T *&src) {
+    const int n = e % Np, w = e / Np % nw, g = g0 + e / grpl;
+    t = e / (Np * nw) % kTile;
+    src = (const T *)(w ? a.cm : a.bm) + (long long)t * a.ldbc + (long long)g * a.N + n;
+    if (e >= bufl || n >= a.N || g >= a.G) t = 1 << 30;
+  };
+  const bool pre = bufl <= STAGE * nthr;
+  const T *e_src[STAGE];
+  int e_t[STAGE];
+#pragma unroll
+  for (int k = 0; k < STAGE; ++k) element(tid + k * nthr, e_t[k], e_src[k]);
 
   for (int b = blockIdx.z; b < a.B; b += gridDim.z) {
     int len = a.S;
@@ -109,61 +165,158 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(ScanArgs a, ScanPlan pl)
     if (t0 >= len && chunk > 0) continue;
     const int t1 = min(t0 + pl.chunk_len, len);
     const long long r0 = (long long)b * a.S;
+    T xr[SLOTS], dr[SLOTS], zr[SLOTS], er[STAGE];
+    const long long rl = r0 + (t0 < t1 ? min(t0 + tj, t1 - 1) : 0);  // this lane's first row
+    const T *px = (const T *)a.x + rl * a.ldx + d, *pd = (const T *)a.dt + rl * a.lddt + d;
+    // without a gate its loads are those of x again and its factor is 1: no branch in the loop
+    const T *pz = gated ? (const T *)a.z + rl * a.ldz + d : px;
+    T *py = (T *)a.y + (r0 + t0 + (J > 1 ? tj : 0)) * a.ldy + d;
+    // this lane's next row (slots and tiles in order, ts the tile's first position); behind the end the
+    // last row of the lane again (more: the row after it lies before the end)
+    auto fetch_row = [&](bool more, int ts, int i) {
+      xr[i] = *px;
+      dr[i] = *pd;
+      if (FINAL) zr[i] = *pz;
+      const bool in = more || ts + (i + 1) * J + tj < t1;
+      px += in ? J * a.ldx : 0;
+      pd += in ? J * a.lddt : 0;
+      if (FINAL) pz += in ? J * ldz : 0;
+    };
+    const long long ob = (r0 + t0) * a.ldbc;
+    auto fetch_bc = [&](int ts) {
+      const long long o = ob + (ts - t0) * a.ldbc;
+#pragma unroll
+      for (int k = 0; k < STAGE; ++k) {
+        er[k] = (T)0.f;
+        if (e_t[k] < t1 - ts) er[k] = e_src[k][o];
+      }
+    };
+    auto stage_bc = [&](int ts, float *buf) {
+      if (pre) {
+#pragma unroll
+        for (int k = 0; k < STAGE; ++k)
+          if (tid + k * nthr < bufl) buf[tid + k * nthr] = (float)er[k];
+      } else {
+        for (int e = tid; e < bufl; e += nthr) {
+          int t;
+          const T *src;
+          element(e, t, src);
+          buf[e] = t < t1 - ts ? (float)src[ob + (ts - t0) * a.ldbc] : 0.f;
+        }
+      }
+    };
     float h[NS];
 #pragma unroll
     for (int i = 0; i < NS; ++i) h[i] = 0.f;
+    if (FINAL && chunk > 0)  // as scan_join_kernel left it
+      load_states<NS>(pl.part + (((long long)b * (pl.chunks - 1) + chunk - 1) * a.D + d) * Np + n0, NS, true, h);
+    else if (FINAL && a.state_in)
+      load_states<NS>(a.state_in + ((long long)b * a.D + d) * a.N + n0, nn, wide, h);
     float ds = 0.f;
-    if constexpr (FINAL) {
-      if (a.state_in) load_states<NS>(a.state_in + ((long long)b * a.D + d) * a.N + n0, nn, wide, h);
-      for (int c = 0; c < chunk; ++c) {
-        const long long o = (long long)b * (pl.chunks - 1) + c;
-        float s[NS];
-        load_states<NS>(pl.part + (o * a.D + d) * a.Np + n0, NS, true, s);
-        const float q = pl.dsum[o * a.D + d];
+    __syncthreads();  // the last tile of another prompt
+    if (t0 < t1) {
 #pragma unroll
-        for (int i = 0; i < NS; ++i) h[i] = fmaf(__builtin_amdgcn_exp2f(q * A2[i]), h[i], s[i]);
-      }
+      for (int i = 0; i < SLOTS; ++i) fetch_row(false, t0, i);
+      if (pre) fetch_bc(t0);
+      stage_bc(t0, lds);
     }
-    for (int ts = t0; ts < t1; ts += tile) {
-      const int nt = min(tile, t1 - ts);
-      __syncthreads();
-      const int ne = ngr * a.N;
-      for (int e = tid; e < nt * ne; e += kThreads) {
-        const int t = e / ne, r = e - t * ne, g = r / a.N, n = r - g * a.N;
-        const long long o = (r0 + ts + t) * a.ldbc + (long long)(g0 + g) * a.N + n;
-        lds[(t * 2) * tfl + g * a.Np + n] = (float)((const T *)a.bm)[o];
-        if constexpr (FINAL) lds[(t * 2 + 1) * tfl + g * a.Np + n] = (float)((const T *)a.cm)[o];
-      }
-      __syncthreads();
-      for (int t = 0; t < nt; ++t) {
-        const long long r = r0 + ts + t;
-        const float xv = (float)((const T *)a.x)[r * a.ldx + d];
-        const float dl = softplus((float)((const T *)a.dt)[r * a.lddt + d] + dtb);
-        const float dx = dl * xv;
-        const float *bp = lds + (t * 2) * tfl + gi * a.Np + n0, *cp = bp + tfl;
-        float yv = 0.f;
+    // the positions of a tile.  WHOLE: neither they nor those fetched meanwhile come near the end
+    auto compute = [&](auto whole, int ts, const float *buf) {
+      constexpr bool WHOLE = decltype(whole)::value;
 #pragma unroll
-        for (int i = 0; i < NS; ++i) {
-          h[i] = fmaf(__builtin_amdgcn_exp2f(dl * A2[i]), h[i], dx * bp[i]);
-          if constexpr (FINAL) yv = fmaf(cp[i], h[i], yv);
+      for (int i = 0; i < SLOTS; ++i) {
+        const bool in = WHOLE || ts + i * J + tj < t1;
+        const float xv = (float)xr[i], zv = FINAL ? (float)zr[i] : 0.f;
+        float dl = softplus((float)dr[i] + dtb);
+        fetch_row(WHOLE, ts + kTile, i);
+        dl = in ? dl : 0.f;
+        const float dx = in ? dl * xv : 0.f;
+        float y[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const float *bq = buf + (i * J + j) * nw * Np, *cq = bq + Np;
+          const float dlj = bcast<J>(dl, j), dxj = bcast<J>(dx, j);
+          float ys[2];
+#pragma unroll
+          for (int n = 0; n < NS; ++n) {
+            h[n] = fmaf(__builtin_amdgcn_exp2f(dlj * A2[n]), h[n], dxj * bq[n]);
+            if constexpr (FINAL) ys[n & 1] = n < 2 ? cq[n] * h[n] : fmaf(cq[n], h[n], ys[n & 1]);
+          }
+          if constexpr (FINAL) y[j] = ys[0] + ys[1];
+          // the next position's B and C are read when this one's states are done: the compiler would
+          // otherwise read those of many positions at once and spill
+#pragma unroll
+          for (int n = 0; n < NS; ++n) asm volatile("" : "+v"(h[n])::"memory");
         }
         if constexpr (FINAL) {
-          yv = fmaf(skip, xv, group_sum<LPC>(yv));
-          if (a.z) yv *= silu((float)((const T *)a.z)[r * a.ldz + d]);
-          if (owner && sub == 0) ((T *)a.y)[r * a.ldy + d] = (T)yv;
+          const float yv = fmaf(skip, xv, transpose_sum<LPC, J>(y, sub)), g = silu(zv);
+          // lanes past the last channel, and the lanes of a channel past its first J, hold the value
+          // of another lane and store it again
+          if (in) *py = (T)(yv * (gated ? g : 1.f));
+          py += J * a.ldy;
         } else {
           ds += dl;
         }
       }
+    };
+    int p = 0;
+    for (int ts = t0; ts < t1; ts += kTile) {
+      __syncthreads();  // this tile is staged, and nobody reads the other buffer any more
+      const bool more = ts + kTile < t1;
+      if (more && pre) fetch_bc(ts + kTile);
+      const float *buf = lds + p * bufl + gi * grpl + n0;
+      if (ts + 2 * kTile < t1)
+        compute(std::true_type(), ts, buf);
+      else
+        compute(std::false_type(), ts, buf);
+      p ^= 1;
+      if (more) stage_bc(ts + kTile, lds + p * bufl);
     }
     if constexpr (FINAL) {
       if (owner && a.state_out && t1 == len && nn > 0)
         store_states<NS>(a.state_out + ((long long)b * a.D + d) * a.N + n0, nn, wide, h);
     } else {
       const long long o = (long long)b * (pl.chunks - 1) + chunk;
+      ds = group_sum<J>(ds);
       if (owner) {
-        store_states<NS>(pl.part + (o * a.D + d) * a.Np + n0, NS, true, h);
+        store_states<NS>(pl.part + (o * a.D + d) * Np + n0, NS, true, h);
         if (sub == 0) pl.dsum[o * a.D + d] = ds;
+      }
+    }
+  }
+}
+
+// Joins the pieces: part[c] becomes the state after pieces 0 .. c.  A thread takes one state of a
+// channel and requests sixteen pieces' values at a time: the pass is a chain of those round trips (64
+// pieces of 2048 x 16 states: 6 us; eight at a time with four states per thread: 10.5).
+__global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs a, ScanPlan pl) {
+  constexpr int R = 16;
+  const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+  const int d = (int)(id / a.Np), n = (int)(id - (long long)d * a.Np);
+  if (d >= a.D) return;
+  const float A2 = a.A2[id];
+  const int nc = pl.chunks - 1;
+  for (int b = blockIdx.y; b < a.B; b += gridDim.y) {
+    int len = a.len ? a.len[b] : a.S;
+    len = len < 0 ? 0 : len > a.S ? a.S : len;
+    const int live = min(nc, (len - 1) / pl.chunk_len);  // pieces that another one follows
+    float h = a.state_in && n < a.N ? a.state_in[((long long)b * a.D + d) * a.N + n] : 0.f;
+    float *part = pl.part + (long long)b * nc * a.D * a.Np + id;
+    const float *dsum = pl.dsum + (long long)b * nc * a.D + d;
+    const long long sp = (long long)a.D * a.Np;
+    for (int c0 = 0; c0 < live; c0 += R) {
+      float s[R], w[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const int c = min(c0 + i, live - 1);
+        s[i] = part[c * sp];
+        w[i] = dsum[(long long)c * a.D];
+      }
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        if (c0 + i >= live) break;
+        h = fmaf(__builtin_amdgcn_exp2f(w[i] * A2), h, s[i]);
+        part[(c0 + i) * sp] = h;
       }
     }
   }
@@ -211,44 +364,73 @@ __global__ void __launch_bounds__(kThreads) scan_step_kernel(ScanArgs a) {
   }
 }
 
-// lanes per channel of the prompt form
-int scan_lanes(int Np) { return Np <= 16 ? 1 : Np / 16; }
+// groups that n neighbouring channels can touch
+int scan_groups(int n, int per, int G) { return std::min({G, n, (n - 1) / per + 2}); }
 
-ScanPlan scan_plan(int B, int S, int D, int N, int num_cu) {
-  ScanPlan p{};
-  const int Np = scan_padded_states(N), lanes = scan_lanes(Np);
-  const long long waves = (long long)B * ((D * (long long)lanes + 255) / 256) * 4;
-  const long long want = (long long)num_cu * 8;
-  const long long chunks = std::max(1ll, std::min({want / waves, (long long)S / 64, 32ll}));
-  p.chunk_len = (int)((S + chunks - 1) / chunks + 15) / 16 * 16;
-  p.chunks = (S + p.chunk_len - 1) / p.chunk_len;
-  return p;
+// Lanes per channel and pieces of the axis, by the time they are expected to take: with k waves on a
+// SIMD a wave's position takes hypot(0.14, 0.083 k) us with four states per lane and hypot(0.19, 0.16 k)
+// with eight (fitted to 2048 channels x 16 states, 8192 positions, k = 1 to 8).  Cutting the axis adds
+// a first pass over it (0.75 of the second's time) and the join.  Measured, four and eight states: 1 x 8192
+// in one piece 1353 and 1869 us, in 16 pieces 196 and 230, 32: 159 and 165, 64: 158 and 156; 64 x 80
+// (ragged) whole 33 and 39 us.  Four states win a tie: prompts of different lengths end with a few waves,
+// which they finish earlier.
+ScanPlan scan_plan(int B, int S, int D, int N, int G, int num_cu) {
+  const int Np = scan_padded_states(N);
+  ScanPlan best{};
+  double best_us = 1e30;
+  for (int ns = 4; ns <= 8; ns *= 2) {
+    int lanes = std::max(1, Np / ns);
+    if (lanes > 16) lanes = 16;
+    if (ns == 8 && lanes == best.lanes) continue;  // the same form
+    // B and C of a wave's channels have to fit into LDS twice (four states per lane always do)
+    if (ns == 8 && scan_groups(64 / lanes, D / G, G) * Np > 512) continue;
+    const double alone = ns == 4 ? 0.14 : 0.19, busy = ns == 4 ? 0.083 : 0.16;
+    const double waves = (double)B * ((D * (long long)lanes + 63) / 64) / (num_cu * 4);
+    for (int chunks = 1; chunks <= 256; chunks *= 2) {
+      const int len = chunks == 1 ? S : ((S + chunks - 1) / chunks + kTile - 1) / kTile * kTile;
+      if (chunks > 1 && len < 2 * kTile) break;
+      const double us = len * std::hypot(alone, std::max(1.0, waves * chunks) * busy) * (chunks > 1 ? 1.75 : 1.0) +
+                        (chunks > 1 ? 6.0 + 0.05 * chunks : 0.0);
+      if (us < best_us * 0.95) {
+        best_us = us;
+        best.lanes = lanes;
+        best.chunk_len = len;
+        best.chunks = (S + len - 1) / len;
+      }
+    }
+  }
+  return best;
 }
 
 template <typename T, int NS, int LPC>
 hipError_t run_scan(const ScanArgs &a, ScanPlan pl, hipStream_t st) {
-  constexpr int CPB = kThreads / LPC;
   const int per = a.D / a.G;
-  pl.ngr = std::min(a.G, (CPB - 1) / per + 2);
-  const int per_pos = pl.ngr * a.Np * 2 * 4;
-  pl.tile = std::max(1, std::min(16, 32768 / per_pos));
-  const size_t lds = (size_t)pl.tile * per_pos;
-  const unsigned gx = (unsigned)((a.D + CPB - 1) / CPB), gz = (unsigned)std::min(a.B, 32768);
-  if (pl.chunks > 1)
-    hipLaunchKernelGGL((scan_kernel<T, NS, LPC, false>), dim3(gx, pl.chunks - 1, gz), dim3(kThreads), lds, st, a, pl);
-  hipLaunchKernelGGL((scan_kernel<T, NS, LPC, true>), dim3(gx, pl.chunks, gz), dim3(kThreads), lds, st, a, pl);
+  // a workgroup's channels: fewer where their groups' B and C would not fit into LDS twice
+  size_t lds;
+  for (pl.threads = std::min(256, (a.D * LPC + 63) / 64 * 64);; pl.threads -= 64) {
+    pl.ngr = scan_groups(pl.threads / LPC, per, a.G);
+    lds = (size_t)pl.ngr * a.Np * 8 * kTile * 2;
+    if (lds <= 65536 || pl.threads == 64) break;
+  }
+  const unsigned gx = (unsigned)((a.D * LPC + pl.threads - 1) / pl.threads), gz = (unsigned)std::min(a.B, 32768);
+  if (pl.chunks > 1) {
+    hipLaunchKernelGGL((scan_kernel<T, NS, LPC, false>), dim3(gx, pl.chunks - 1, gz), dim3(pl.threads), lds / 2, st, a, pl);
+    hipLaunchKernelGGL(scan_join_kernel, dim3((unsigned)(((long long)a.D * a.Np + 255) / 256), gz), dim3(256), 0, st, a, pl);
+  }
+  hipLaunchKernelGGL((scan_kernel<T, NS, LPC, true>), dim3(gx, pl.chunks, gz), dim3(pl.threads), lds, st, a, pl);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t scan_by_states(const ScanArgs &a, const ScanPlan &pl, hipStream_t st) {
+  const bool four = pl.lanes * 4 == a.Np;  // four states per lane, or eight
   switch (a.Np) {
     case 4: return run_scan<T, 4, 1>(a, pl, st);
-    case 8: return run_scan<T, 8, 1>(a, pl, st);
-    case 16: return run_scan<T, 16, 1>(a, pl, st);
-    case 32: return run_scan<T, 16, 2>(a, pl, st);
-    case 64: return run_scan<T, 16, 4>(a, pl, st);
-    case 128: return run_scan<T, 16, 8>(a, pl, st);
+    case 8: return four ? run_scan<T, 4, 2>(a, pl, st) : run_scan<T, 8, 1>(a, pl, st);
+    case 16: return four ? run_scan<T, 4, 4>(a, pl, st) : run_scan<T, 8, 2>(a, pl, st);
+    case 32: return four ? run_scan<T, 4, 8>(a, pl, st) : run_scan<T, 8, 4>(a, pl, st);
+    case 64: return four ? run_scan<T, 4, 16>(a, pl, st) : run_scan<T, 8, 8>(a, pl, st);
+    case 128: return run_scan<T, 8, 16>(a, pl, st);
     default: return run_scan<T, 16, 16>(a, pl, st);
   }
 }
@@ -282,14 +464,14 @@ int scan_padded_states(int N) {
   return p;
 }
 
-size_t scan_workspace_bytes(int B, int S, int D, int N, int num_cu) {
-  const ScanPlan p = scan_plan(B, S, D, N, num_cu);
+size_t scan_workspace_bytes(int B, int S, int D, int N, int G, int num_cu) {
+  const ScanPlan p = scan_plan(B, S, D, N, G, num_cu);
   const size_t n = (size_t)B * (p.chunks - 1) * D;
   return n * 4 * (scan_padded_states(N) + 1) + 256;
 }
 
 hipError_t launch_scan(const ScanArgs &a, hipStream_t st) {
-  ScanPlan p = scan_plan(a.B, a.S, a.D, a.N, a.num_cu);
+  ScanPlan p = scan_plan(a.B, a.S, a.D, a.N, a.G, a.num_cu);
   const size_t n = (size_t)a.B * (p.chunks - 1) * a.D;
   p.part = (float *)a.ws;
   p.dsum = p.part + n * a.Np;

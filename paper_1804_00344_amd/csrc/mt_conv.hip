@@ -2,18 +2,15 @@
 // y[t, d] = act(b[d] + sum_j w[d, j] x[t - W + 1 + j, d]).
 //
 // Memory-bound: every input is used W times, from registers.  A thread takes VEC neighbouring
-// channels (16 bytes where the rows are aligned for it) over a run of kRun positions and keeps the
-// last W - 1 inputs in registers, so the inputs are read (1 + (W - 1) / kRun) times, the second time
-// mostly from the caches.  Threads are numbered channel first, so a wave's accesses are consecutive
-// for any channel count.  A prompt's first thread of a channel reads the state before it and is the
-// one that writes the state after it.
+// channels (16 bytes where the rows are aligned for it) over RUN positions: it requests all their inputs
+// and the W - 1 before them at once, then computes.  Threads are numbered channel first, so a wave's
+// accesses are consecutive for any channel count.  A prompt's first thread of a channel reads the state
+// before it and is the one that writes the state after it.
 #include "mt_layer_dev.h"
 
 namespace mt {
 
 namespace {
-
-constexpr int kRun = 16;
 
 template <typename T, int VEC, int W>
 __device__ __forceinline__ void load_taps(const ConvArgs &a, int d, float (&w)[W][VEC], float (&b)[VEC]) {
@@ -25,11 +22,11 @@ __device__ __forceinline__ void load_taps(const ConvArgs &a, int d, float (&w)[W
   }
 }
 
-template <typename T, int VEC, int W>
+template <typename T, int VEC, int W, int RUN, bool STREAM>
 __global__ void __launch_bounds__(256) conv_kernel(ConvArgs a) {
   using V = Vec<T, VEC>;
   const int dv = a.D / VEC;
-  const int runs = (a.S + kRun - 1) / kRun;
+  const int runs = (a.S + RUN - 1) / RUN;
   const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
   if (id >= (long long)runs * dv) return;
   const int run = (int)(id / dv), d = (int)(id - (long long)run * dv) * VEC;
@@ -48,47 +45,35 @@ __global__ void __launch_bounds__(256) conv_kernel(ConvArgs a) {
     T *y = (T *)a.y + (long long)b * a.S * a.ldy + d;
     const T *st = a.state_in ? (const T *)a.state_in + (long long)b * (W - 1) * a.D + d : nullptr;
     // the input at position t >= 1 - W of this prompt
-    auto input = [&](int t, float (&f)[VEC]) {
-      typename V::Raw r;
-      if (t >= 0)
-        r = V::raw(x + (long long)t * a.ldx);
-      else if (st)
-        r = V::raw(st + (long long)(t + W - 1) * a.D);
-      else
-        r = {};
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) f[v] = (float)r.v[v];
+    auto input = [&](int t) -> typename V::Raw {
+      if (t >= 0) return V::raw(x + (long long)t * a.ldx);
+      if (st) return V::raw(st + (long long)(t + W - 1) * a.D);
+      return {};
     };
-    const int t0 = run * kRun, t1 = t0 + kRun < len ? t0 + kRun : len;
+    const int t0 = run * RUN, t1 = t0 + RUN < len ? t0 + RUN : len;
     if (t0 < t1) {
-      float h[W][VEC];  // h[j]: the input of tap j
+      typename V::Raw in[RUN + W - 1];  // positions t0 - W + 1 .. t0 + RUN - 1, behind the end the last one
 #pragma unroll
-      for (int j = 0; j + 1 < W; ++j) input(t0 - W + 1 + j, h[j + 1]);
-      for (int t = t0; t < t1; ++t) {
+      for (int j = 0; j + 1 < W; ++j) in[j] = input(t0 - W + 1 + j);
 #pragma unroll
-        for (int j = 0; j + 1 < W; ++j)
+      for (int i = 0; i < RUN; ++i) in[W - 1 + i] = V::raw(x + (long long)min(t0 + i, t1 - 1) * a.ldx);
 #pragma unroll
-          for (int v = 0; v < VEC; ++v) h[j][v] = h[j + 1][v];
-        input(t, h[W - 1]);
+      for (int i = 0; i < RUN; ++i) {
         float o[VEC];
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
           o[v] = bias[v];
 #pragma unroll
-          for (int j = 0; j < W; ++j) o[v] = fmaf(w[j][v], h[j][v], o[v]);
+          for (int j = 0; j < W; ++j) o[v] = fmaf(w[j][v], (float)in[i + j].v[v], o[v]);
           if (a.silu) o[v] = silu(o[v]);
         }
-        V::put(y + (long long)t * a.ldy, o);
+        if (t0 + i < t1) V::template put<STREAM>(y + (long long)(t0 + i) * a.ldy, o);
       }
     }
     if (run == 0 && W > 1 && a.state_out) {
       T *so = (T *)a.state_out + (long long)b * (W - 1) * a.D + d;
 #pragma unroll
-      for (int j = 0; j + 1 < W; ++j) {
-        float f[VEC];
-        input(len - W + 1 + j, f);
-        V::put(so + (long long)j * a.D, f);
-      }
+      for (int j = 0; j + 1 < W; ++j) *(typename V::Raw *)(so + (long long)j * a.D) = input(len - W + 1 + j);
     }
   }
 }
@@ -133,18 +118,29 @@ __global__ void __launch_bounds__(256) conv_step_kernel(ConvArgs a) {
   }
 }
 
+template <typename T, int VEC, int W, int RUN, bool STREAM>
+hipError_t run_prompts(const ConvArgs &a, hipStream_t st) {
+  const long long n = ((a.S + RUN - 1) / RUN * (long long)(a.D / VEC) + 255) / 256;
+  hipLaunchKernelGGL((conv_kernel<T, VEC, W, RUN, STREAM>), dim3((unsigned)n, (unsigned)(a.B < 32768 ? a.B : 32768)),
+                     dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+// Runs of 8 positions once those of 4 fill the chip four times over (4 x 8192 x 2048, W = 4: 60 us, runs of 4
+// and 16: 71 and 62; 3 x 61 x 333: 3.1 us with runs of 4, 6.5 with one position after the other).
+// Outputs larger than the L2s together are stored past them (60 -> 56 us); smaller ones stay for
+// the product that reads them.
 template <typename T, int VEC, int W>
 hipError_t run_conv(const ConvArgs &a, bool step, hipStream_t st) {
   const long long dv = a.D / VEC;
   if (step) {
-    const long long n = (a.B * dv + 255) / 256;
-    hipLaunchKernelGGL((conv_step_kernel<T, VEC, W>), dim3((unsigned)n), dim3(256), 0, st, a);
-  } else {
-    const long long n = ((a.S + kRun - 1) / kRun * dv + 255) / 256;
-    hipLaunchKernelGGL((conv_kernel<T, VEC, W>), dim3((unsigned)n, (unsigned)(a.B < 32768 ? a.B : 32768)), dim3(256),
-                       0, st, a);
+    hipLaunchKernelGGL((conv_step_kernel<T, VEC, W>), dim3((unsigned)((a.B * dv + 255) / 256)), dim3(256), 0, st, a);
+    return hipGetLastError();
   }
-  return hipGetLastError();
+  const double n = (double)a.B * a.S * dv;  // vectors
+  if (VEC > 1 && n * 16 > 32e6) return run_prompts<T, VEC, W, 8, VEC != 1>(a, st);
+  if (n >= 4.0 * 64 * 16 * a.num_cu) return run_prompts<T, VEC, W, 8, false>(a, st);
+  return run_prompts<T, VEC, W, 4, false>(a, st);
 }
 
 template <typename T, int VEC>

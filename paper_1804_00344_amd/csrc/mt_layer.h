@@ -47,6 +47,7 @@ struct ConvArgs {
   const void *state_in; // [rows][W-1][D] or NULL
   void *state_out;
   int32_t *err;
+  int num_cu;
 };
 hipError_t launch_conv(const ConvArgs &a, hipStream_t st);
 hipError_t launch_conv_step(const ConvArgs &a, hipStream_t st);

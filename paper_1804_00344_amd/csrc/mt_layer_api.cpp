@@ -335,6 +335,7 @@ static mt_status conv_args(mt_ssm *c, int rows, int S, const void *x, int64_t ld
   a->x = x; a->ldx = ldx; a->y = y; a->ldy = ldy;
   a->state_in = state_in; a->state_out = state_out;
   a->err = c->err;
+  a->num_cu = c->num_cu;
   return MT_OK;
 }
 

@@ -14,11 +14,21 @@ struct Vec {
     T v[VEC];
   };
   __device__ __forceinline__ static Raw raw(const T *p) { return *(const Raw *)p; }
+  // STREAM: past the L2
+  template <bool STREAM = false>
   __device__ __forceinline__ static void put(T *p, const float (&f)[VEC]) {
     Raw r;
 #pragma unroll
     for (int i = 0; i < VEC; ++i) r.v[i] = (T)f[i];
-    *(Raw *)p = r;
+    if constexpr (STREAM) {
+      static_assert(sizeof(Raw) == 16, "streamed in whole vectors");
+      typedef int v4 __attribute__((ext_vector_type(4)));
+      v4 q;
+      __builtin_memcpy(&q, &r, 16);
+      __builtin_nontemporal_store(q, (v4 *)p);
+    } else {
+      *(Raw *)p = r;
+    }
   }
 };
 

@@ -322,15 +322,22 @@ __global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs a, ScanPlan pl)
   }
 }
 
-// One token of a hypothesis
-template <typename T, int LPC>
+// One token of a hypothesis: LPC lanes share a channel, four states each.  Bound by the states' traffic:
+// each is read and written once, 16 bytes a lane (two and four hypotheses per thread were no faster).
+// WIDE: B, C and the states are aligned for one access of four (768 x 2048 x 16 element by element: 83
+// us).  STREAM: the new states are stored past the L2.  For states larger than the L2s together that is
+// the faster form wherever something else runs between two steps: 768 x 2048 x 16 takes 38.5 us (5.6 TB/s)
+// against 54 from the same states again, and 49 against 57 with a 154 MB matrix of logits written between
+// a step and the next; only steps back to back, which find their states in the last-level cache, lose (50
+// against 38).
+template <typename T, int LPC, bool WIDE, bool STREAM>
 __global__ void __launch_bounds__(kThreads) scan_step_kernel(ScanArgs a) {
   constexpr int NS = 4, CPB = kThreads / LPC;
   const int tid = threadIdx.x, sub = tid % LPC, n0 = sub * NS;
   const int c = blockIdx.x * CPB + tid / LPC, d = min(c, a.D - 1);
   const int g = d / (a.D / a.G);
   const int nn = min(NS, a.N - n0);
-  const bool wide = a.N % 4 == 0;
+  const bool gated = a.z != nullptr;
   for (int m = blockIdx.y; m < a.B; m += gridDim.y) {
     int row = m;
     if (a.row) {
@@ -340,25 +347,48 @@ __global__ void __launch_bounds__(kThreads) scan_step_kernel(ScanArgs a) {
         row = row < 0 ? 0 : a.n_rows - 1;
       }
     }
-    float h[NS];
-    load_states<NS>(a.state_in + ((long long)row * a.D + d) * a.N + n0, nn, wide, h);
+    float h[NS], bv[NS], cv[NS];
+    load_states<NS>(a.state_in + ((long long)row * a.D + d) * a.N + n0, nn, WIDE, h);
     const float xv = (float)((const T *)a.x)[(long long)m * a.ldx + d];
-    const float dl = softplus((float)((const T *)a.dt)[(long long)m * a.lddt + d] + a.dt_bias[d]);
-    const float dx = dl * xv;
+    const float dv = (float)((const T *)a.dt)[(long long)m * a.lddt + d];
+    const float zv = gated ? (float)((const T *)a.z)[(long long)m * a.ldz + d] : 0.f;
+    const float4 A2 = *(const float4 *)(a.A2 + (size_t)d * a.Np + n0);
+    const float dtb = a.dt_bias[d], skip = a.skip[d];
     const long long o = (long long)m * a.ldbc + (long long)g * a.N + n0;
+    if constexpr (WIDE) {
+      typename Vec<T, NS>::Raw b4{}, c4{};
+      if (nn > 0) {
+        b4 = Vec<T, NS>::raw((const T *)a.bm + o);
+        c4 = Vec<T, NS>::raw((const T *)a.cm + o);
+      }
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        bv[i] = (float)b4.v[i];
+        cv[i] = (float)c4.v[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        bv[i] = i < nn ? (float)((const T *)a.bm)[o + i] : 0.f;
+        cv[i] = i < nn ? (float)((const T *)a.cm)[o + i] : 0.f;
+      }
+    }
+    const float dl = softplus(dv + dtb), dx = dl * xv;
+    const float A[NS] = {A2.x, A2.y, A2.z, A2.w};
     float yv = 0.f;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
-      if (i < nn) {
-        const float bv = (float)((const T *)a.bm)[o + i], cv = (float)((const T *)a.cm)[o + i];
-        h[i] = fmaf(__builtin_amdgcn_exp2f(dl * a.A2[(size_t)d * a.Np + n0 + i]), h[i], dx * bv);
-        yv = fmaf(cv, h[i], yv);
-      }
+      h[i] = fmaf(__builtin_amdgcn_exp2f(dl * A[i]), h[i], dx * bv[i]);
+      yv = fmaf(cv[i], h[i], yv);
     }
-    yv = fmaf(a.skip[d], xv, group_sum<LPC>(yv));
-    if (a.z) yv *= silu((float)((const T *)a.z)[(long long)m * a.ldz + d]);
+    yv = fmaf(skip, xv, group_sum<LPC>(yv));
+    if (gated) yv *= silu(zv);
     if (c < a.D) {
-      if (nn > 0) store_states<NS>(a.state_out + ((long long)m * a.D + d) * a.N + n0, nn, wide, h);
+      float *so = a.state_out + ((long long)m * a.D + d) * a.N + n0;
+      if (STREAM && nn > 0)
+        Vec<float, NS>::template put<true>(so, h);
+      else if (nn > 0)
+        store_states<NS>(so, nn, WIDE, h);
       if (sub == 0) ((T *)a.y)[(long long)m * a.ldy + d] = (T)yv;
     }
   }
@@ -438,8 +468,14 @@ hipError_t scan_by_states(const ScanArgs &a, const ScanPlan &pl, hipStream_t st)
 template <typename T, int LPC>
 hipError_t run_step(const ScanArgs &a, hipStream_t st) {
   constexpr int CPB = kThreads / LPC;
-  hipLaunchKernelGGL((scan_step_kernel<T, LPC>), dim3((a.D + CPB - 1) / CPB, (unsigned)std::min(a.B, 32768)),
-                     dim3(kThreads), 0, st, a);
+  const dim3 grid((a.D + CPB - 1) / CPB, (unsigned)std::min(a.B, 32768));
+  const bool wide = a.N % 4 == 0 && ((uintptr_t)a.bm | (uintptr_t)a.cm) % (4 * sizeof(T)) == 0 && a.ldbc % 4 == 0;
+  if (wide && (double)a.B * a.D * a.N * 4 > 32e6)
+    hipLaunchKernelGGL((scan_step_kernel<T, LPC, true, true>), grid, dim3(kThreads), 0, st, a);
+  else if (wide)
+    hipLaunchKernelGGL((scan_step_kernel<T, LPC, true, false>), grid, dim3(kThreads), 0, st, a);
+  else
+    hipLaunchKernelGGL((scan_step_kernel<T, LPC, false, false>), grid, dim3(kThreads), 0, st, a);
   return hipGetLastError();
 }
 

@@ -7,6 +7,7 @@
 // by one direct load of a wave and from LDS to registers by one 16-byte read per lane, both without
 // bank conflicts and without any arithmetic on addresses.
 #include <algorithm>
+#include <cmath>
 
 #include "mt_layer_dev.h"
 
@@ -39,51 +40,89 @@ __device__ __forceinline__ size_t frag_offset(int row, int kg, int KB) {
   return ((size_t)(row >> 5) * KB + (kg >> 1)) * 1024 + (kg & 1) * 512 + (row & 31) * 16;
 }
 
-// 16 values of a row from k0 on, zero from K on
+// 8 values of a row from k0 on, zero from K on
 template <typename T>
-__device__ __forceinline__ void load16(const T *row, int k0, int K, bool wide, float (&f)[16]) {
-  if (wide && k0 + 16 <= K) {
-    constexpr int E = 16 / sizeof(T);
+struct Row8 {
+  static constexpr int E = 16 / sizeof(T);
+  typename Vec<T, E>::Raw v[8 / E];
+  __device__ __forceinline__ void load(const T *row, int k0, int K, bool wide) {
+    if (wide && k0 + 8 <= K) {
 #pragma unroll
-    for (int i = 0; i < 16; i += E) {
-      const typename Vec<T, E>::Raw q = Vec<T, E>::raw(row + k0 + i);
+      for (int i = 0; i < 8 / E; ++i) v[i] = Vec<T, E>::raw(row + k0 + i * E);
+    } else {
 #pragma unroll
-      for (int j = 0; j < E; ++j) f[i + j] = (float)q.v[j];
+      for (int i = 0; i < 8; ++i) v[i / E].v[i % E] = k0 + i < K ? row[k0 + i] : (T)0.f;
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) f[i] = k0 + i < K ? (float)row[k0 + i] : 0.f;
   }
-}
+  __device__ __forceinline__ float at(int i) const { return (float)v[i / E].v[i % E]; }
+  __device__ __forceinline__ uint32_t magnitude() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(at(i)) & 0x7fffffffu);
+    return m;
+  }
+  __device__ __forceinline__ int2 packed(float r) const {
+    return make_int2(pack4(quant(at(0), r), quant(at(1), r), quant(at(2), r), quant(at(3), r)),
+                     pack4(quant(at(4), r), quant(at(5), r), quant(at(6), r), quant(at(7), r)));
+  }
+  // the eight 8-bit values at their place of row m
+  __device__ __forceinline__ void store(int8_t *xq, int m, int k0, int KB, float r) const {
+    *(int2 *)(xq + frag_offset(m, k0 >> 4, KB) + (k0 & 8)) = packed(r);
+  }
+};
 
-// One wave per row: its largest magnitude, then its values in 8 bits.  Groups of k past K and rows past
-// M of the last blocks are left as they are: they meet zero columns or rows that are not stored.
-template <typename T>
+// One wave per row, eight neighbouring values per lane and pass: the row's largest magnitude, then its
+// values in 8 bits.  A row of up to 512 R values is read once and waits in registers (longer ones, R = 0,
+// are read twice).  Values of k past K and rows past M of the last blocks are left as they are: they
+// meet zero columns or rows that are not stored.
+template <typename T, int R>
 __global__ void __launch_bounds__(256) quant_rows_kernel(I8Problem p, int wide) {
   const int lane = threadIdx.x & 63, m = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (m >= p.M) return;
   const T *row = (const T *)p.x + (long long)m * p.ldx;
-  const int ng = (p.K + 15) / 16, KB = p.Kp / 32;
+  const int KB = p.Kp / 32;
   uint32_t mx = 0;
-  for (int g = lane; g < ng; g += 64) {
-    float f[16];
-    load16<T>(row, g * 16, p.K, wide, f);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) mx = max(mx, __float_as_uint(f[i]) & 0x7fffffffu);
-  }
-  mx = wave_ext<uint32_t, true>(mx);
   float r, s;
-  row_scales(mx, r, s);
-  if (lane == 0) p.xs[m] = s;
-  for (int g = lane; g < ng; g += 64) {
-    float f[16];
-    load16<T>(row, g * 16, p.K, wide, f);
-    i32x4 q;
+  if constexpr (R > 0) {
+    Row8<T> q[R];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      q[i] = pack4(quant(f[4 * i], r), quant(f[4 * i + 1], r), quant(f[4 * i + 2], r), quant(f[4 * i + 3], r));
-    *(i32x4 *)(p.xq + frag_offset(m, g, KB)) = q;
+    for (int i = 0; i < R; ++i) q[i].load(row, (i * 64 + lane) * 8, p.K, wide);
+#pragma unroll
+    for (int i = 0; i < R; ++i) mx = max(mx, q[i].magnitude());
+    row_scales(wave_ext<uint32_t, true>(mx), r, s);
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      if ((i * 64 + lane) * 8 < p.K) q[i].store(p.xq, m, (i * 64 + lane) * 8, KB, r);
+  } else {
+    Row8<T> q;
+    for (int k = lane * 8; k < p.K; k += 512) {
+      q.load(row, k, p.K, wide);
+      mx = max(mx, q.magnitude());
+    }
+    row_scales(wave_ext<uint32_t, true>(mx), r, s);
+    for (int k = lane * 8; k < p.K; k += 512) {
+      q.load(row, k, p.K, wide);
+      q.store(p.xq, m, k, KB, r);
+    }
   }
+  if (lane == 0) p.xs[m] = s;
+}
+
+template <typename T>
+hipError_t run_quant(const I8Problem &p, hipStream_t st) {
+  const int wide = (uintptr_t)p.x % 16 == 0 && p.ldx % (16 / (int)sizeof(T)) == 0;
+  const dim3 grid((unsigned)((p.M + 3) / 4)), block(256);
+  if (p.K <= 512)
+    hipLaunchKernelGGL((quant_rows_kernel<T, 1>), grid, block, 0, st, p, wide);
+  else if (p.K <= 1024)
+    hipLaunchKernelGGL((quant_rows_kernel<T, 2>), grid, block, 0, st, p, wide);
+  else if (p.K <= 2048)
+    hipLaunchKernelGGL((quant_rows_kernel<T, 4>), grid, block, 0, st, p, wide);
+  else if (p.K <= 4096)
+    hipLaunchKernelGGL((quant_rows_kernel<T, 8>), grid, block, 0, st, p, wide);
+  else
+    hipLaunchKernelGGL((quant_rows_kernel<T, 0>), grid, block, 0, st, p, wide);
+  return hipGetLastError();
 }
 
 // ---- packing of the columns at load ----
@@ -130,8 +169,8 @@ constexpr int waitcnt(int vm, int lgkm) { return (vm & 15) | (vm >> 4) << 14 | 7
 
 // A workgroup of WM x WN waves computes a tile of 32 MF WM rows by 32 NF WN columns, k in stages of 64
 // through a ring of ST stages in LDS that direct loads fill ST - 1 stages ahead.
-template <int MF, int NF, int WM, int WN, int ST, bool BF>
-__global__ void __launch_bounds__(64 * WM * WN) i8_tile_kernel(I8Problem p, int tilesM, int tilesN) {
+template <int MF, int NF, int WM, int WN, int ST, bool BF, bool STREAM>
+__global__ void __launch_bounds__(64 * WM * WN) i8_tile_kernel(I8Problem p, int tilesM, int tilesN, int wide) {
   constexpr int AB = MF * WM, BB = NF * WN;       // blocks of 32 rows and columns
   constexpr int STAGE = (AB + BB) * 2 * 1024;     // a stage: two blocks of k of each
   constexpr int NL = (AB + BB) * 2 / (WM * WN);   // direct loads of a wave per stage
@@ -146,17 +185,14 @@ __global__ void __launch_bounds__(64 * WM * WN) i8_tile_kernel(I8Problem p, int 
   const int tm = grp * 8 + (w - grp * gsz) % gm, tn = (w - grp * gsz) / gm;
   const char *ga = (const char *)p.xq + (size_t)tm * AB * KB * 1024 + lane * 16;
   const char *gb = (const char *)p.wq + (size_t)tn * BB * KB * 1024 + lane * 16;
-  auto load = [&](int s) {
+  auto load = [&](int s, int i) {  // the i-th direct load of this wave for stage s
     char *dst = lds + (s % ST) * STAGE;
     const int sk = s < stages ? s : stages - 1;  // past the end: a load that nobody reads
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int f = wave * NL + i, blk = f >> 1;  // blocks 0 .. AB-1 of rows, then of columns
-      const char *src = (blk < AB ? ga + (size_t)blk * KB * 1024 : gb + (size_t)(blk - AB) * KB * 1024) +
-                        (size_t)(sk * 2 + (f & 1)) * 1024;
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
-                                       (__attribute__((address_space(3))) void *)(dst + f * 1024), 16, 0, 0);
-    }
+    const int f = wave * NL + i, blk = f >> 1;   // blocks 0 .. AB-1 of rows, then of columns
+    const char *src = (blk < AB ? ga + (size_t)blk * KB * 1024 : gb + (size_t)(blk - AB) * KB * 1024) +
+                      (size_t)(sk * 2 + (f & 1)) * 1024;
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
+                                     (__attribute__((address_space(3))) void *)(dst + f * 1024), 16, 0, 0);
   };
   i32x16 acc[MF][NF];
 #pragma unroll
@@ -171,89 +207,275 @@ __global__ void __launch_bounds__(64 * WM * WN) i8_tile_kernel(I8Problem p, int 
 #pragma unroll
     for (int j = 0; j < NF; ++j) fb[h][j] = *(const i32x4 *)(src + (AB + wn * NF + j) * 2048);
   };
-  auto mma = [&](int h) {
+  // the MFMAs of block h of k, the wave's loads i0 .. i1-1 for stage s spread among them: right after the
+  // barrier all waves' loads would queue before their first MFMA
+  auto mma = [&](int h, int s, int i0, int i1) {
+    constexpr int every = MF * NF / ((NL + 1) / 2) > 0 ? MF * NF / ((NL + 1) / 2) : 1;
 #pragma unroll
-    for (int i = 0; i < MF; ++i)
-#pragma unroll
-      for (int j = 0; j < NF; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa[h][i], fb[h][j], acc[i][j], 0, 0, 0);
+    for (int q = 0; q < MF * NF; ++q) {
+      const int i = q / NF, j = q % NF;
+      acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[h][j], fa[h][i], acc[i][j], 0, 0, 0);
+      if (q % every == 0 && i0 + q / every < i1) {
+        __builtin_amdgcn_sched_barrier(0);
+        load(s, i0 + q / every);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
   };
 #pragma unroll
-  for (int s = 0; s < ST; ++s) load(s);
-  __builtin_amdgcn_s_waitcnt(waitcnt((ST - 1) * NL, 15));
+  for (int s = 0; s < ST; ++s)
+#pragma unroll
+    for (int i = 0; i < (s + 1 < ST ? NL : NL / 2); ++i) load(s, i);
+  __builtin_amdgcn_s_waitcnt(waitcnt((ST - 2) * NL + NL / 2, 15));
   __builtin_amdgcn_s_barrier();
   read(0, 0);
   for (int s = 0; s < stages; ++s) {
+    // the first block's reads were issued a block of MFMAs ago; waited for here, the ones that follow
+    // are not waited for with them
+    __builtin_amdgcn_s_waitcnt(waitcnt(63, 0));
     read(s, 1);
     __builtin_amdgcn_sched_barrier(0);
-    mma(0);
+    mma(0, s + ST - 1, NL / 2, NL);
     // every wave holds all of stage s in registers and its part of stage s + 1 has arrived: past the
     // barrier that stage can be read and this one's buffer filled again
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(waitcnt((ST - 2) * NL, 0));
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    load(s + ST);
     read(s + 1 < stages ? s + 1 : s, 0);
     __builtin_amdgcn_sched_barrier(0);
-    mma(1);
+    mma(1, s + ST, 0, NL / 2);
   }
-  // no direct load may still be on its way when the workgroup gives its LDS back
+  // no direct load may still be on its way when the ring is used for the results (or given back)
   __builtin_amdgcn_s_waitcnt(waitcnt(0, 0));
-  // ---- lane holds rows 8 (r / 4) + 4 (lane / 32) + r % 4, column lane % 32 of each block ----
-  const int m0 = (tm * AB + wm * MF) * 32 + 4 * (lane >> 5), n0 = (tn * BB + wn * NF) * 32 + (lane & 31);
-  float sw[NF], bias[NF];
-#pragma unroll
-  for (int j = 0; j < NF; ++j) {
-    sw[j] = p.ws[n0 + j * 32];
-    bias[j] = p.bias && n0 + j * 32 < p.N ? p.bias[n0 + j * 32] : 0.f;
-  }
+  __builtin_amdgcn_s_barrier();
+  // ---- the columns are the MFMAs' first operand, so a lane holds row lane % 32 and columns 8 (r / 4) +
+  // 4 (lane / 32) + r % 4 of each block: four neighbours at a time.  They pass through the wave's part
+  // of LDS (32 rows at a time, 16-byte chunks of a row permuted by its number against bank conflicts) to
+  // be stored as whole vectors of consecutive columns.
+  typedef typename std::conditional<BF, bf16, float>::type Y;
+  constexpr int ES = sizeof(Y), ROWB = NF * 32 * ES, CPR = ROWB / 16, EPC = 16 / ES;  // chunks of a row, elements
+  static_assert(WM * WN * 32 * ROWB <= ST * STAGE, "the results of 32 rows of every wave fit into the ring");
+  char *own = lds + wave * 32 * ROWB;
+  const int n0 = (tn * BB + wn * NF) * 32, lr = lane & 31;
 #pragma unroll
   for (int i = 0; i < MF; ++i) {
+    const int mb = (tm * AB + wm * MF + i) * 32;
+    const float sx = p.xs[min(mb + lr, p.M - 1)];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int m = m0 + i * 32 + 8 * (r >> 2) + (r & 3);
-      if (m >= p.M) continue;
-      const float sx = p.xs[m];
+    for (int j = 0; j < NF; ++j)
 #pragma unroll
-      for (int j = 0; j < NF; ++j) {
-        const int n = n0 + j * 32;
-        if (n >= p.N) continue;
-        const float v = fmaf((float)acc[i][j][r] * sw[j], sx, bias[j]);
-        if constexpr (BF)
-          ((bf16 *)p.y)[(long long)m * p.ldy + n] = (bf16)v;
+      for (int q = 0; q < 4; ++q) {
+        const int nq = j * 32 + 8 * q + 4 * (lane >> 5);
+        const float4 sw = *(const float4 *)(p.ws + n0 + nq);
+        const float4 bias = p.bias ? *(const float4 *)(p.bias + n0 + nq) : make_float4(0.f, 0.f, 0.f, 0.f);
+        float v[4];
+        v[0] = fmaf((float)acc[i][j][4 * q] * sw.x, sx, bias.x);
+        v[1] = fmaf((float)acc[i][j][4 * q + 1] * sw.y, sx, bias.y);
+        v[2] = fmaf((float)acc[i][j][4 * q + 2] * sw.z, sx, bias.z);
+        v[3] = fmaf((float)acc[i][j][4 * q + 3] * sw.w, sx, bias.w);
+        const int byte = nq * ES;
+        Vec<Y, 4>::put((Y *)(own + lr * ROWB + (((byte >> 4) ^ (lr % CPR)) << 4) + (byte & 15)), v);
+      }
+    __builtin_amdgcn_s_waitcnt(waitcnt(63, 0));  // the wave's own part: no barrier
+    __builtin_amdgcn_wave_barrier();
+    Y *const yb = (Y *)p.y + (long long)mb * p.ldy + n0;
+    if (wide) {
+#pragma unroll
+      for (int u = 0; u < 32 * CPR / 64; ++u) {
+        const int c = lane + u * 64;
+        const int r = c / CPR, k = c % CPR, n = n0 + k * EPC;
+        const typename Vec<Y, EPC>::Raw v = *(const typename Vec<Y, EPC>::Raw *)(own + r * ROWB + ((k ^ (r % CPR)) << 4));
+        if (mb + r >= p.M) continue;
+        Y *dst = yb + (long long)r * p.ldy + k * EPC;
+        if (n + EPC <= p.N)
+          Vec<Y, EPC>::template store<STREAM>(dst, v);
         else
-          ((float *)p.y)[(long long)m * p.ldy + n] = v;
+          for (int e = 0; e < EPC; ++e)
+            if (n + e < p.N) dst[e] = v.v[e];
+      }
+    } else {
+      for (int c = lane; c < 32 * NF * 32; c += 64) {
+        const int r = c / (NF * 32), k = c % (NF * 32);
+        const Y v = *(const Y *)(own + r * ROWB + (((k * ES >> 4) ^ (r % CPR)) << 4) + (k * ES & 15));
+        if (mb + r < p.M && n0 + k < p.N) yb[(long long)r * p.ldy + k] = v;
       }
     }
+    __builtin_amdgcn_s_waitcnt(waitcnt(63, 0));
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
 template <int MF, int NF, int WM, int WN, int ST>
 hipError_t run_tiles(const I8Problem &p, hipStream_t st) {
   const int tm = (p.M + 32 * MF * WM - 1) / (32 * MF * WM), tn = (p.N + 32 * NF * WN - 1) / (32 * NF * WN);
-  if (p.y_bf16)
-    hipLaunchKernelGGL((i8_tile_kernel<MF, NF, WM, WN, ST, true>), dim3((unsigned)(tm * tn)), dim3(64 * WM * WN), 0, st,
-                       p, tm, tn);
+  const int wide = (uintptr_t)p.y % 16 == 0 && p.ldy % (p.y_bf16 ? 8 : 4) == 0;
+  const dim3 grid((unsigned)(tm * tn)), block(64 * WM * WN);
+  // results larger than the L2s together are stored past them: 768 x 512 x 50000 fp32 71 -> 53 us
+  const bool stream = wide && (double)p.M * p.N * (p.y_bf16 ? 2 : 4) > 32e6;
+#define MT_TILES(BF, S) hipLaunchKernelGGL((i8_tile_kernel<MF, NF, WM, WN, ST, BF, S>), grid, block, 0, st, p, tm, tn, wide)
+  if (p.y_bf16 && stream)
+    MT_TILES(true, true);
+  else if (p.y_bf16)
+    MT_TILES(true, false);
+  else if (stream)
+    MT_TILES(false, true);
   else
-    hipLaunchKernelGGL((i8_tile_kernel<MF, NF, WM, WN, ST, false>), dim3((unsigned)(tm * tn)), dim3(64 * WM * WN), 0,
-                       st, p, tm, tn);
+    MT_TILES(false, false);
+#undef MT_TILES
   return hipGetLastError();
+}
+
+// ---- one to four rows ----
+
+// A pass over the weights in one launch: a wave takes 32 columns and one of KW parts of k, eight blocks of k
+// on their way at a time, straight into registers.  Every workgroup quantises the rows itself, one per wave,
+// into LDS ([16 values of k][row][16 bytes]); the row's loads are issued before the weights', so that they
+// return first.  The parts are summed in LDS, in whole numbers.  Bound by the weights' traffic and
+// the latency of a launch (1 x 512 x 50000 fp32: see the rule below).
+template <typename T, int R>
+__global__ void __launch_bounds__(256) i8_few_kernel(I8Problem p, int KW, int wide) {
+  constexpr int U = 8;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  __shared__ float xs[4];
+  __shared__ int red[3][16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, KB = p.Kp / 32, M = p.M;
+  const int part = wave % KW, blk = blockIdx.x * (4 / KW) + wave / KW;
+  const int nblk = (p.N + 31) / 32;
+  const int per = (KB + KW - 1) / KW, k0 = min(part * per, KB), k1 = min(k0 + per, KB);
+  Row8<T> q[R];
+  if (wave < M) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) q[i].load((const T *)p.x + wave * p.ldx, (i * 64 + lane) * 8, p.K, wide);
+  }
+  const char *wp = (const char *)p.wq + (size_t)min(blk, nblk - 1) * KB * 1024 + lane * 16;
+  i32x4 fb[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) fb[u] = *(const i32x4 *)(wp + (size_t)min(k0 + u, KB - 1) * 1024);
+  if (wave < M) {
+    uint32_t mx = 0;
+    float r, s;
+#pragma unroll
+    for (int i = 0; i < R; ++i) mx = max(mx, q[i].magnitude());
+    row_scales(wave_ext<uint32_t, true>(mx), r, s);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int k = (i * 64 + lane) * 8;
+      if (k < p.Kp) *(int2 *)(lds + ((k >> 4) * M + wave) * 16 + (k & 8)) = q[i].packed(r);
+    }
+    if (lane == 0) xs[wave] = s;
+  }
+  __syncthreads();
+  // lanes of rows past the last read row 0: their results are not stored
+  const char *xp = lds + ((lane >> 5) * M + ((lane & 31) < M ? lane & 31 : 0)) * 16;
+  i32x16 acc = (i32x16)(0);
+  for (int k = k0; k < k1; k += U) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (k + u >= k1) break;
+      const i32x4 fa = *(const i32x4 *)(xp + (k + u) * 2 * M * 16), b = fb[u];
+      fb[u] = *(const i32x4 *)(wp + (size_t)min(k + u + U, KB - 1) * 1024);
+      acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(b, fa, acc, 0, 0, 0);
+    }
+  }
+  if (KW > 1) {
+    if (part > 0) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) red[wave - 1][r][lane] = acc[r];
+    }
+    __syncthreads();
+    if (part > 0) return;
+    for (int w = 1; w < KW; ++w)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[r] += red[wave + w - 1][r][lane];
+  }
+  // lane holds row lane % 32, columns 8 (r / 4) + 4 (lane / 32) + r % 4
+  const int m = lane & 31;
+  if (blk >= nblk || m >= M) return;
+  const float sx = xs[m];
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int n = blk * 32 + 8 * c + 4 * (lane >> 5) + e;
+      if (n >= p.N) continue;
+      const float v = fmaf((float)acc[4 * c + e] * p.ws[n], sx, p.bias ? p.bias[n] : 0.f);
+      if (p.y_bf16)
+        ((bf16 *)p.y)[(long long)m * p.ldy + n] = (bf16)v;
+      else
+        ((float *)p.y)[(long long)m * p.ldy + n] = v;
+    }
+}
+
+constexpr int kFewRows = 4, kFewK = 4096;
+
+template <typename T>
+hipError_t run_few(const I8Problem &p, hipStream_t st) {
+  const int nblk = (p.N + 31) / 32, KB = p.Kp / 32;
+  int KW = 1;  // parts of k: until there are eight waves per unit, of at least two blocks
+  while (KW < 4 && (long long)nblk * KW < 8ll * p.num_cu && KB / (KW * 2) >= 2) KW *= 2;
+  const int wide = (uintptr_t)p.x % 16 == 0 && p.ldx % (16 / (int)sizeof(T)) == 0;
+  const dim3 grid((unsigned)((nblk + 4 / KW - 1) / (4 / KW))), block(256);
+  const size_t lds = (size_t)p.M * p.Kp;
+#define MT_FEW(R) hipLaunchKernelGGL((i8_few_kernel<T, R>), grid, block, lds, st, p, KW, wide)
+  if (p.Kp <= 512)
+    MT_FEW(1);
+  else if (p.Kp <= 1024)
+    MT_FEW(2);
+  else if (p.Kp <= 2048)
+    MT_FEW(4);
+  else
+    MT_FEW(8);
+#undef MT_FEW
+  return hipGetLastError();
+}
+
+// The tile by the time it is expected to take (us): a fixed part, per 64 k the longer of one tile's
+// latency and its units' share of the tiles' throughput, and the results at 5.2 TB/s with a factor for how
+// little their stores overlap with other tiles.  Fitted to rows 96 to 8192, K 512 to 4096, columns 512 to
+// 50000 (bf16; the largest misprediction of the best tile costs 10%).
+struct TileCost {
+  int rows, cols;
+  double fixed, latency, share, out;
+};
+constexpr TileCost kTiles[] = {{64, 64, 6.4, 0.170, 0.113, 1.5},
+                               {64, 128, 7.1, 0.190, 0.180, 1.5},
+                               {128, 128, 8.6, 0.275, 0.273, 1.1},
+                               {128, 256, 9.5, 0.367, 0.510, 1.0},
+                               {256, 256, 12.6, 0.580, 0.957, 1.35}};
+
+int i8_tile(int M, int N, int Kp, int es, int num_cu) {
+  int best = 0;
+  double best_us = 1e30;
+  for (int i = 0; i < 5; ++i) {
+    const TileCost &t = kTiles[i];
+    const double tiles = std::ceil((double)M / t.rows) * std::ceil((double)N / t.cols);
+    const double us = t.fixed + Kp / 64 * std::max(t.latency, std::ceil(tiles / num_cu) * t.share) +
+                      t.out * M * (double)N * es / 5.2e6;
+    if (us < best_us) {
+      best_us = us;
+      best = i;
+    }
+  }
+  return best;
 }
 
 }  // namespace
 
 hipError_t launch_i8_product(const I8Problem &p, hipStream_t st) {
-  const int ev = p.x_bf16 ? 8 : 4;
-  const int wide = (uintptr_t)p.x % 16 == 0 && p.ldx % ev == 0;
-  const unsigned rows = (unsigned)((p.M + 3) / 4);
-  if (p.x_bf16)
-    hipLaunchKernelGGL(quant_rows_kernel<bf16>, dim3(rows), dim3(256), 0, st, p, wide);
-  else
-    hipLaunchKernelGGL(quant_rows_kernel<float>, dim3(rows), dim3(256), 0, st, p, wide);
-  const hipError_t e = hipGetLastError();
+  // Few rows: one launch instead of two.  bf16, one and four rows x 512 x 2048: 6.4 and 6.9 us (tiles 6.8 and
+  // 7.2), x 2048 x 8192: 9.5 and 10.0 (11.4 and 11.5), 512 x 50000: 8.7 and 9.2 (9.7 and 9.4); sixteen rows are
+  // slower than tiles.
+  if (p.M <= kFewRows && p.Kp <= kFewK) return p.x_bf16 ? run_few<bf16>(p, st) : run_few<float>(p, st);
+  const hipError_t e = p.x_bf16 ? run_quant<bf16>(p, st) : run_quant<float>(p, st);
   if (e != hipSuccess) return e;
-  return run_tiles<2, 2, 2, 2, 3>(p, st);
+  switch (i8_tile(p.M, p.N, p.Kp, p.y_bf16 ? 2 : 4, p.num_cu)) {
+    case 0: return run_tiles<1, 1, 2, 2, 4>(p, st);
+    case 1: return run_tiles<1, 2, 2, 2, 4>(p, st);
+    case 2: return run_tiles<2, 2, 2, 2, 3>(p, st);
+    case 3: return run_tiles<2, 2, 2, 4, 3>(p, st);
+    default: return run_tiles<4, 2, 2, 4, 4>(p, st);
+  }
 }
 
 hipError_t launch_i8_pack(const float *W, int K, int N, int Kp, int Np, int8_t *wq, float *s, int *bad,

@@ -17,7 +17,7 @@ struct I8Problem {
   int x_bf16;
   const int8_t *wq;     // packed columns in fragment order
   const float *ws;      // [Np] column scales, zero padded
-  const float *bias;    // [N] or NULL
+  const float *bias;    // [Np] zero padded, or NULL
   void *y;              // [M][ldy]
   long long ldy;
   int y_bf16;

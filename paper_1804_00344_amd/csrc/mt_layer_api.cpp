@@ -26,7 +26,7 @@ struct mt_i8_matrix {
   int K, N, Kp, Np;
   int8_t *wq = nullptr;
   float *scale = nullptr;  // [Np]
-  float *bias = nullptr;   // [N] or NULL
+  float *bias = nullptr;   // [Np], zero padded, or NULL
   int device, num_cu;
 };
 
@@ -170,7 +170,8 @@ mt_status mt_i8_load(int K, int N, const float *W, const float *bias, mt_i8_matr
     const int zero = 0;
     HIP_TRY(hipMemcpy(bad, &zero, 4, hipMemcpyHostToDevice));
     if (bias) {
-      CHECK(alloc((void **)&w->bias, (size_t)N * 4));
+      CHECK(alloc((void **)&w->bias, (size_t)w->Np * 4));
+      HIP_TRY(hipMemset(w->bias, 0, (size_t)w->Np * 4));
       HIP_TRY(hipMemcpy(w->bias, bias, (size_t)N * 4, hipMemcpyDefault));
     }
     const size_t bytes = (size_t)K * N * 4;

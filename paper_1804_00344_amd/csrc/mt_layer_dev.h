@@ -15,11 +15,8 @@ struct Vec {
   };
   __device__ __forceinline__ static Raw raw(const T *p) { return *(const Raw *)p; }
   // STREAM: past the L2
-  template <bool STREAM = false>
-  __device__ __forceinline__ static void put(T *p, const float (&f)[VEC]) {
-    Raw r;
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) r.v[i] = (T)f[i];
+  template <bool STREAM>
+  __device__ __forceinline__ static void store(T *p, const Raw &r) {
     if constexpr (STREAM) {
       static_assert(sizeof(Raw) == 16, "streamed in whole vectors");
       typedef int v4 __attribute__((ext_vector_type(4)));
@@ -29,6 +26,13 @@ struct Vec {
     } else {
       *(Raw *)p = r;
     }
+  }
+  template <bool STREAM = false>
+  __device__ __forceinline__ static void put(T *p, const float (&f)[VEC]) {
+    Raw r;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) r.v[i] = (T)f[i];
+    store<STREAM>(p, r);
   }
 };
 

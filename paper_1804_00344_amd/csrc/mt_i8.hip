@@ -462,14 +462,20 @@ int i8_tile(int M, int N, int Kp, int es, int num_cu) {
 
 }  // namespace
 
-hipError_t launch_i8_product(const I8Problem &p, hipStream_t st) {
+int i8_form(int M, int N, int K, int y_bytes, int num_cu) {
+  const int Kp = (K + kI8KPad - 1) / kI8KPad * kI8KPad;
   // Few rows: one launch instead of two.  bf16, one and four rows x 512 x 2048: 6.4 and 6.9 us (tiles 6.8 and
   // 7.2), x 2048 x 8192: 9.5 and 10.0 (11.4 and 11.5), 512 x 50000: 8.7 and 9.2 (9.7 and 9.4); sixteen rows are
   // slower than tiles.
-  if (p.M <= kFewRows && p.Kp <= kFewK) return p.x_bf16 ? run_few<bf16>(p, st) : run_few<float>(p, st);
+  return M <= kFewRows && Kp <= kFewK ? -1 : i8_tile(M, N, Kp, y_bytes, num_cu);
+}
+
+hipError_t launch_i8_product(const I8Problem &p, hipStream_t st) {
+  const int form = i8_form(p.M, p.N, p.K, p.y_bf16 ? 2 : 4, p.num_cu);
+  if (form < 0) return p.x_bf16 ? run_few<bf16>(p, st) : run_few<float>(p, st);
   const hipError_t e = p.x_bf16 ? run_quant<bf16>(p, st) : run_quant<float>(p, st);
   if (e != hipSuccess) return e;
-  switch (i8_tile(p.M, p.N, p.Kp, p.y_bf16 ? 2 : 4, p.num_cu)) {
+  switch (form) {
     case 0: return run_tiles<1, 1, 2, 2, 4>(p, st);
     case 1: return run_tiles<1, 2, 2, 2, 4>(p, st);
     case 2: return run_tiles<2, 2, 2, 2, 3>(p, st);

@@ -26,6 +26,8 @@ struct I8Problem {
   float *xs;            // and their scales
   int num_cu;
 };
+// tile of a product (0..4: 64 x 64, 64 x 128, 128 x 128, 128 x 256, 256 x 256); -1: the form of few rows
+int i8_form(int M, int N, int K, int y_bytes, int num_cu);
 hipError_t launch_i8_product(const I8Problem &p, hipStream_t st);
 // quantises W [K][N] (device memory) into wq [Np/32][Kp/32][1024] and s [Np]; *bad is set to 1 where
 // W holds a NaN or an infinity
@@ -71,7 +73,8 @@ struct ScanArgs {
   int num_cu;
 };
 int scan_padded_states(int N);
-size_t scan_workspace_bytes(int B, int S, int D, int N, int G, int num_cu);
+int scan_pieces(int B, int S, int D, int N, int num_cu);  // pieces that the axis is cut into
+size_t scan_workspace_bytes(int B, int S, int D, int N, int num_cu);
 hipError_t launch_scan(const ScanArgs &a, hipStream_t st);
 hipError_t launch_scan_step(const ScanArgs &a, hipStream_t st);
 

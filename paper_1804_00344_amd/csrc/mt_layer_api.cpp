@@ -320,7 +320,7 @@ mt_status mt_ssm_free(mt_ssm *c) {
 
 size_t mt_ssm_workspace_bytes(const mt_ssm *c, int B, int S) {
   if (!valid(c) || B < 1 || S < 1 || (long long)B * S > kMaxRows) return 0;
-  return scan_workspace_bytes(B, S, c->cfg.D, c->cfg.N, c->cfg.G, c->num_cu);
+  return scan_workspace_bytes(B, S, c->cfg.D, c->cfg.N, c->num_cu);
 }
 
 static mt_status conv_args(mt_ssm *c, int rows, int S, const void *x, int64_t ldx, const void *state_in, void *y,

@@ -109,7 +109,8 @@ __device__ __forceinline__ float transpose_sum(float (&y)[J], int sub) {
   }
 }
 
-constexpr int kTile = 8;  // positions of B and C staged together
+// positions of B and C staged together: two tiles of 64 / LPC groups fit into 64 KiB
+constexpr int tile_positions(int NS) { return NS <= 8 ? 8 : 4; }
 
 // A workgroup takes the channels of its threads / LPC in one piece of a prompt; LPC lanes share a channel,
 // NS states each.  The work per position and channel (softplus, gate, skip) is spread over the lanes:
@@ -118,7 +119,7 @@ constexpr int kTile = 8;  // positions of B and C staged together
 // behind the end the steps D_t are zero, which keeps the state as it is.
 template <typename T, int NS, int LPC, bool FINAL>
 __global__ void __launch_bounds__(256, NS == 16 ? 2 : 4) scan_kernel(ScanArgs a, ScanPlan pl) {
-  constexpr int J = LPC < 4 ? LPC : 4, Np = NS * LPC, SLOTS = kTile / J;
+  constexpr int J = LPC < 4 ? LPC : 4, Np = NS * LPC, kTile = tile_positions(NS), SLOTS = kTile / J;
   constexpr int STAGE = Np / 16 > 4 ? Np / 16 : 4;  // elements of B and C that a thread holds for the next tile
   extern __shared__ __attribute__((aligned(16))) float lds[];
   const int tid = threadIdx.x, nthr = blockDim.x, cpb = nthr / LPC, sub = tid % LPC, n0 = sub * NS, tj = sub % J;
@@ -397,36 +398,32 @@ __global__ void __launch_bounds__(kThreads) scan_step_kernel(ScanArgs a) {
 // groups that n neighbouring channels can touch
 int scan_groups(int n, int per, int G) { return std::min({G, n, (n - 1) / per + 2}); }
 
-// Lanes per channel and pieces of the axis, by the time they are expected to take: with k waves on a
-// SIMD a wave's position takes hypot(0.14, 0.083 k) us with four states per lane and hypot(0.19, 0.16 k)
-// with eight (fitted to 2048 channels x 16 states, 8192 positions, k = 1 to 8).  Cutting the axis adds
-// a first pass over it (0.75 of the second's time) and the join.  Measured, four and eight states: 1 x 8192
-// in one piece 1353 and 1869 us, in 16 pieces 196 and 230, 32: 159 and 165, 64: 158 and 156; 64 x 80
-// (ragged) whole 33 and 39 us.  Four states win a tie: prompts of different lengths end with a few waves,
-// which they finish earlier.
-ScanPlan scan_plan(int B, int S, int D, int N, int G, int num_cu) {
+// Lanes of a channel: four states each, more where they exceed a row of 16 lanes.  (16 states per lane, one
+// lane a channel, spilled or left a SIMD two waves: 1 x 8192 x 2048 x 16 176 us and more; eight per lane
+// 156, four 158; 64 x 80 ragged 39 and 33.)
+int scan_lanes(int Np) { return std::min(Np / 4, 16); }
+
+// Pieces of the axis, by the time they are expected to take: with k waves on a SIMD a wave's position takes
+// hypot(0.14, 0.083 k) us, and as much more as a lane holds more than four states (fitted to 2048
+// channels x 16 states, 8192 positions, k = 1 to 8).  Cutting the axis adds a first pass over it (0.75 of
+// the second's time) and the join.  Measured, 1 x 8192 x 2048 x 16 in one piece 1353 us, in 16 pieces 196,
+// 32: 159, 64: 158, 128: 168; 64 x 80 whole 33, cut 62 and more; 7 x 97 x 330 x 24 whole 21, cut 16.
+ScanPlan scan_plan(int B, int S, int D, int N, int num_cu) {
   const int Np = scan_padded_states(N);
   ScanPlan best{};
+  best.lanes = scan_lanes(Np);
+  const int ns = Np / best.lanes, tile = tile_positions(ns);
+  const double waves = (double)B * ((D * (long long)best.lanes + 63) / 64) / (num_cu * 4);
   double best_us = 1e30;
-  for (int ns = 4; ns <= 8; ns *= 2) {
-    int lanes = std::max(1, Np / ns);
-    if (lanes > 16) lanes = 16;
-    if (ns == 8 && lanes == best.lanes) continue;  // the same form
-    // B and C of a wave's channels have to fit into LDS twice (four states per lane always do)
-    if (ns == 8 && scan_groups(64 / lanes, D / G, G) * Np > 512) continue;
-    const double alone = ns == 4 ? 0.14 : 0.19, busy = ns == 4 ? 0.083 : 0.16;
-    const double waves = (double)B * ((D * (long long)lanes + 63) / 64) / (num_cu * 4);
-    for (int chunks = 1; chunks <= 256; chunks *= 2) {
-      const int len = chunks == 1 ? S : ((S + chunks - 1) / chunks + kTile - 1) / kTile * kTile;
-      if (chunks > 1 && len < 2 * kTile) break;
-      const double us = len * std::hypot(alone, std::max(1.0, waves * chunks) * busy) * (chunks > 1 ? 1.75 : 1.0) +
-                        (chunks > 1 ? 6.0 + 0.05 * chunks : 0.0);
-      if (us < best_us * 0.95) {
-        best_us = us;
-        best.lanes = lanes;
-        best.chunk_len = len;
-        best.chunks = (S + len - 1) / len;
-      }
+  for (int chunks = 1; chunks <= 256; chunks *= 2) {
+    const int len = chunks == 1 ? S : ((S + chunks - 1) / chunks + tile - 1) / tile * tile;
+    if (chunks > 1 && len < 2 * tile) break;
+    const double us = len * (ns / 4) * std::hypot(0.14, 0.083 * std::max(1.0, waves * chunks)) * (chunks > 1 ? 1.75 : 1.0) +
+                      (chunks > 1 ? 6.0 + 0.05 * chunks : 0.0);
+    if (us < best_us) {
+      best_us = us;
+      best.chunk_len = len;
+      best.chunks = (S + len - 1) / len;
     }
   }
   return best;
@@ -439,7 +436,7 @@ hipError_t run_scan(const ScanArgs &a, ScanPlan pl, hipStream_t st) {
   size_t lds;
   for (pl.threads = std::min(256, (a.D * LPC + 63) / 64 * 64);; pl.threads -= 64) {
     pl.ngr = scan_groups(pl.threads / LPC, per, a.G);
-    lds = (size_t)pl.ngr * a.Np * 8 * kTile * 2;
+    lds = (size_t)pl.ngr * a.Np * 8 * tile_positions(NS) * 2;
     if (lds <= 65536 || pl.threads == 64) break;
   }
   const unsigned gx = (unsigned)((a.D * LPC + pl.threads - 1) / pl.threads), gz = (unsigned)std::min(a.B, 32768);
@@ -453,13 +450,12 @@ hipError_t run_scan(const ScanArgs &a, ScanPlan pl, hipStream_t st) {
 
 template <typename T>
 hipError_t scan_by_states(const ScanArgs &a, const ScanPlan &pl, hipStream_t st) {
-  const bool four = pl.lanes * 4 == a.Np;  // four states per lane, or eight
   switch (a.Np) {
     case 4: return run_scan<T, 4, 1>(a, pl, st);
-    case 8: return four ? run_scan<T, 4, 2>(a, pl, st) : run_scan<T, 8, 1>(a, pl, st);
-    case 16: return four ? run_scan<T, 4, 4>(a, pl, st) : run_scan<T, 8, 2>(a, pl, st);
-    case 32: return four ? run_scan<T, 4, 8>(a, pl, st) : run_scan<T, 8, 4>(a, pl, st);
-    case 64: return four ? run_scan<T, 4, 16>(a, pl, st) : run_scan<T, 8, 8>(a, pl, st);
+    case 8: return run_scan<T, 4, 2>(a, pl, st);
+    case 16: return run_scan<T, 4, 4>(a, pl, st);
+    case 32: return run_scan<T, 4, 8>(a, pl, st);
+    case 64: return run_scan<T, 4, 16>(a, pl, st);
     case 128: return run_scan<T, 8, 16>(a, pl, st);
     default: return run_scan<T, 16, 16>(a, pl, st);
   }
@@ -500,14 +496,16 @@ int scan_padded_states(int N) {
   return p;
 }
 
-size_t scan_workspace_bytes(int B, int S, int D, int N, int G, int num_cu) {
-  const ScanPlan p = scan_plan(B, S, D, N, G, num_cu);
+int scan_pieces(int B, int S, int D, int N, int num_cu) { return scan_plan(B, S, D, N, num_cu).chunks; }
+
+size_t scan_workspace_bytes(int B, int S, int D, int N, int num_cu) {
+  const ScanPlan p = scan_plan(B, S, D, N, num_cu);
   const size_t n = (size_t)B * (p.chunks - 1) * D;
   return n * 4 * (scan_padded_states(N) + 1) + 256;
 }
 
 hipError_t launch_scan(const ScanArgs &a, hipStream_t st) {
-  ScanPlan p = scan_plan(a.B, a.S, a.D, a.N, a.G, a.num_cu);
+  ScanPlan p = scan_plan(a.B, a.S, a.D, a.N, a.num_cu);
   const size_t n = (size_t)a.B * (p.chunks - 1) * a.D;
   p.part = (float *)a.ws;
   p.dsum = p.part + n * a.Np;

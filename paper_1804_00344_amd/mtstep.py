@@ -413,9 +413,9 @@ class Ssm:
     def __init__(self, handle: int, cfg: mt_ssm_config, device):
         import torch
         self.handle, self.cfg, self.device = handle, cfg, device
-        self.D, self.W = cfg.D, cfg.W
-        self.GN, self.state_shape = cfg.G * cfg.N, (cfg.D, cfg.N)
+        self.D, self.W, self.N, self.GN = cfg.D, cfg.W, cfg.N, cfg.G * cfg.N
         self.dtype = torch.bfloat16 if cfg.dtype == MT_BF16 else torch.float32
+        self.f32, self.i32 = torch.float32, torch.int32
 
     def __del__(self):
         if getattr(self, "handle", None):
@@ -431,20 +431,21 @@ def _current_device():
     return torch.device("cuda", torch.cuda.current_device()) if torch.cuda.is_available() else None
 
 
-def _rows(t, name, lead, width, dtype, device):
-    """(address, row stride) of a row matrix of shape lead + (width,)."""
-    if tuple(t.shape) != lead + (width,):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}: need {lead + (width,)}")
-    if t.dtype != dtype:
-        raise ValueError(f"{name} is {t.dtype}: need {dtype}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}: need {device}")
-    st = t.stride()
-    if width > 1 and st[-1] != 1:
+def _bad(t, name, shape, dtype, device):
+    return ValueError(f"{name}: need a {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype} "
+                      f"{tuple(t.shape)} on {t.device}")
+
+
+def _rows(t, name, shape, dtype, device):
+    """(address, row stride) of a row matrix of two or three dimensions."""
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
+        raise _bad(t, name, shape, dtype, device)
+    st, width = t.stride(), shape[-1]
+    if st[-1] != 1 and width > 1:
         raise ValueError(f"the last dimension of {name} must be contiguous")
-    if len(lead) == 1:
-        return t.data_ptr(), st[0] if lead[0] > 1 else width
-    B, S = lead
+    if len(st) == 2:
+        return t.data_ptr(), st[0] if shape[0] > 1 else width
+    B, S = shape[0], shape[1]
     ld = st[1] if S > 1 else (st[0] if B > 1 else width)
     if B > 1 and st[0] != S * ld:
         raise ValueError(f"the rows of {name} must be equally spaced")
@@ -455,14 +456,9 @@ def _packed(t, name, shape, dtype, device):
     """Address of a contiguous tensor of a given shape, or None."""
     if t is None:
         return None
-    if tuple(t.shape) != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name}: need a contiguous {dtype} tensor of shape {shape} on {device}")
+    if t.shape != shape or t.dtype is not dtype or t.device != device or not t.is_contiguous():
+        raise _bad(t, name + " (contiguous)", shape, dtype, device)
     return t.data_ptr()
-
-
-def _index(t, name, n, device):
-    import torch
-    return _packed(t, name, (n,), torch.int32, device)
 
 
 def _host_or_device(a):
@@ -508,15 +504,14 @@ def _io(t, name):
 
 def mt_i8_product(mat: I8Matrix, x, y, ws, stream=None):
     """y = x W + bias with both operands in 8 bits; x [..., K], y [..., N] of the same leading shape."""
-    lead = tuple(x.shape[:-1])
-    if len(lead) not in (1, 2):
+    lead, dev = x.shape[:-1], mat.device
+    if len(lead) != 1 and len(lead) != 2:
         raise ValueError("x must have two or three dimensions")
     xt, yt = _io(x, "x"), _io(y, "y")
-    xp, ldx = _rows(x, "x", lead, mat.K, x.dtype, mat.device)
-    yp, ldy = _rows(y, "y", lead, mat.N, y.dtype, mat.device)
-    M = lead[0] if len(lead) == 1 else lead[0] * lead[1]
-    _check(lib().mt_i8_product(mat.handle, M, xp, xt, ldx, yp, yt, ldy, _ptr(ws), ws.numel() * ws.element_size(),
-                               _stream(stream)))
+    xp, ldx = _rows(x, "x", lead + (mat.K,), x.dtype, dev)
+    yp, ldy = _rows(y, "y", lead + (mat.N,), y.dtype, dev)
+    _check(lib().mt_i8_product(mat.handle, lead.numel(), xp, xt, ldx, yp, yt, ldy, _ptr(ws),
+                               ws.numel() * ws.element_size(), _stream(stream)))
 
 
 def make_ssm_config(D, N, *, groups=1, conv=0, conv_silu=True, dtype="f32"):
@@ -561,63 +556,61 @@ def mt_ssm_device_errors(cell: Ssm) -> int:
 
 def mt_ssm_conv(cell: Ssm, x, y, *, lens=None, state_in=None, state_out=None, stream=None):
     """x, y [B, S, D]; lens [B] int32; state_in, state_out [B, W-1, D]."""
-    dt, dev = cell.dtype, cell.device
-    B, S = lead = tuple(x.shape[:-1])
-    st = (B, max(cell.W - 1, 0), cell.D)
-    xp, ldx = _rows(x, "x", lead, cell.D, dt, dev)
-    yp, ldy = _rows(y, "y", lead, cell.D, dt, dev)
-    _check(lib().mt_ssm_conv(cell.handle, B, S, _index(lens, "lens", B, dev), xp, ldx,
+    dt, dev, D = cell.dtype, cell.device, cell.D
+    B, S = x.shape[:-1]
+    st, rows = (B, max(cell.W - 1, 0), D), (B, S, D)
+    xp, ldx = _rows(x, "x", rows, dt, dev)
+    yp, ldy = _rows(y, "y", rows, dt, dev)
+    _check(lib().mt_ssm_conv(cell.handle, B, S, _packed(lens, "lens", (B,), cell.i32, dev), xp, ldx,
                              _packed(state_in, "state_in", st, dt, dev), yp, ldy,
                              _packed(state_out, "state_out", st, dt, dev), _stream(stream)))
 
 
 def mt_ssm_conv_step(cell: Ssm, x, y, state_in, state_out, *, src_row=None, stream=None):
     """x, y [M, D]; state_in [rows, W-1, D], state_out [M, W-1, D]; src_row [M] int32."""
-    dt, dev, W1 = cell.dtype, cell.device, max(cell.W - 1, 0)
-    M, = lead = tuple(x.shape[:-1])
-    rows = state_in.shape[0] if state_in is not None else M
-    xp, ldx = _rows(x, "x", lead, cell.D, dt, dev)
-    yp, ldy = _rows(y, "y", lead, cell.D, dt, dev)
-    _check(lib().mt_ssm_conv_step(cell.handle, M, _index(src_row, "src_row", M, dev), rows, xp, ldx,
-                                  _packed(state_in, "state_in", (rows, W1, cell.D), dt, dev), yp, ldy,
-                                  _packed(state_out, "state_out", (M, W1, cell.D), dt, dev), _stream(stream)))
+    dt, dev, D, W1 = cell.dtype, cell.device, cell.D, max(cell.W - 1, 0)
+    M, = x.shape[:-1]
+    n, rows = state_in.shape[0] if state_in is not None else M, (M, D)
+    xp, ldx = _rows(x, "x", rows, dt, dev)
+    yp, ldy = _rows(y, "y", rows, dt, dev)
+    _check(lib().mt_ssm_conv_step(cell.handle, M, _packed(src_row, "src_row", (M,), cell.i32, dev), n, xp, ldx,
+                                  _packed(state_in, "state_in", (n, W1, D), dt, dev), yp, ldy,
+                                  _packed(state_out, "state_out", (M, W1, D), dt, dev), _stream(stream)))
 
 
 def _scan_rows(cell, lead, x, dt, bmat, cmat, y, z):
     """The row-matrix arguments of the scan in the order of the C calls, without the states."""
-    t, dev, D = cell.dtype, cell.device, cell.D
-    xp, ldx = _rows(x, "x", lead, D, t, dev)
-    dp, ldd = _rows(dt, "dt", lead, D, t, dev)
-    bp, ldb = _rows(bmat, "bmat", lead, cell.GN, t, dev)
-    cp, ldc = _rows(cmat, "cmat", lead, cell.GN, t, dev)
+    t, dev = cell.dtype, cell.device
+    rows, bc = lead + (cell.D,), lead + (cell.GN,)
+    xp, ldx = _rows(x, "x", rows, t, dev)
+    dp, ldd = _rows(dt, "dt", rows, t, dev)
+    bp, ldb = _rows(bmat, "bmat", bc, t, dev)
+    cp, ldc = _rows(cmat, "cmat", bc, t, dev)
     if ldb != ldc:
         raise ValueError("bmat and cmat must have the same row stride")
-    zp, ldz = _rows(z, "z", lead, D, t, dev) if z is not None else (None, 0)
-    yp, ldy = _rows(y, "y", lead, D, t, dev)
-    return (xp, ldx, dp, ldd, bp, cp, ldb, zp, ldz), (yp, ldy)
+    zp, ldz = _rows(z, "z", rows, t, dev) if z is not None else (None, 0)
+    yp, ldy = _rows(y, "y", rows, t, dev)
+    return xp, ldx, dp, ldd, bp, cp, ldb, zp, ldz, yp, ldy
 
 
 def mt_ssm_scan(cell: Ssm, x, dt, bmat, cmat, y, *, z=None, lens=None, state_in=None, state_out=None, ws, stream=None):
     """x, dt, z, y [B, S, D]; bmat, cmat [B, S, G*N]; lens [B] int32; state_in, state_out [B, D, N] fp32."""
-    import torch
     dev = cell.device
-    B, S = lead = tuple(x.shape[:-1])
-    ins, out = _scan_rows(cell, lead, x, dt, bmat, cmat, y, z)
-    st = (B,) + cell.state_shape
-    _check(lib().mt_ssm_scan(cell.handle, B, S, _index(lens, "lens", B, dev), *ins,
-                             _packed(state_in, "state_in", st, torch.float32, dev), *out,
-                             _packed(state_out, "state_out", st, torch.float32, dev), _ptr(ws),
+    B, S = lead = x.shape[:-1]
+    r = _scan_rows(cell, lead, x, dt, bmat, cmat, y, z)
+    st = (B, cell.D, cell.N)
+    _check(lib().mt_ssm_scan(cell.handle, B, S, _packed(lens, "lens", (B,), cell.i32, dev), *r[:9],
+                             _packed(state_in, "state_in", st, cell.f32, dev), r[9], r[10],
+                             _packed(state_out, "state_out", st, cell.f32, dev), _ptr(ws),
                              ws.numel() * ws.element_size(), _stream(stream)))
 
 
 def mt_ssm_step(cell: Ssm, x, dt, bmat, cmat, y, state_in, state_out, *, z=None, src_row=None, stream=None):
     """x, dt, z, y [M, D]; bmat, cmat [M, G*N]; state_in [rows, D, N], state_out [M, D, N] fp32; src_row [M] int32."""
-    import torch
     dev = cell.device
-    M, = lead = tuple(x.shape[:-1])
-    rows = state_in.shape[0]
-    ins, out = _scan_rows(cell, lead, x, dt, bmat, cmat, y, z)
-    _check(lib().mt_ssm_step(cell.handle, M, _index(src_row, "src_row", M, dev), rows, *ins,
-                             _packed(state_in, "state_in", (rows,) + cell.state_shape, torch.float32, dev), *out,
-                             _packed(state_out, "state_out", (M,) + cell.state_shape, torch.float32, dev),
-                             _stream(stream)))
+    M, = lead = x.shape[:-1]
+    n = state_in.shape[0]
+    r = _scan_rows(cell, lead, x, dt, bmat, cmat, y, z)
+    _check(lib().mt_ssm_step(cell.handle, M, _packed(src_row, "src_row", (M,), cell.i32, dev), n, *r[:9],
+                             _packed(state_in, "state_in", (n, cell.D, cell.N), cell.f32, dev), r[9], r[10],
+                             _packed(state_out, "state_out", (M, cell.D, cell.N), cell.f32, dev), _stream(stream)))

@@ -108,6 +108,24 @@ def test_conv_pieces_and_tokens_are_the_whole():
     assert torch.equal(y, whole) and torch.equal(prev, st)
 
 
+@pytest.mark.parametrize("dtype,B,S,D,W,lens", [("bf16", 2, 2100, 2048, 4, [2100, 1999]), ("f32", 3, 1400, 1028, 3, None),
+                                                ("bf16", 3, 4099, 1504, 8, [4099, 0, 4098]), ("f32", 2, 4100, 1200, 2, None)])
+def test_conv_of_many_positions(dtype, B, S, D, W, lens):
+    """Runs of eight positions; results above and below the size from which they are stored past the L2s."""
+    cell, w, b = conv_cell(D, W, dtype)
+    x = torch.randn(B, S, D, generator=torch.Generator(device=DEV).manual_seed(S), device=DEV).to(IO[dtype])
+    ln = None if lens is None else torch.tensor(lens, dtype=torch.int32, device=DEV)
+    y = torch.full((B, S, D), 7.0, dtype=x.dtype, device=DEV)
+    so = torch.empty(B, W - 1, D, dtype=x.dtype, device=DEV)
+    mt.mt_ssm_conv(cell, x, y, lens=ln, state_out=so)
+    for i in range(B):
+        n = lens[i] if lens else S
+        want, state, err = ref.conv(x[i, :n].double(), w.to(DEV), b.to(DEV), True,
+                                    torch.zeros(W - 1, D, dtype=torch.float64, device=DEV))
+        check(y[i, :n], want.cpu(), err.cpu(), "y")
+        assert torch.equal(so[i].double(), state) and bool((y[i, n:] == 7.0).all())
+
+
 # ---- scan ---------------------------------------------------------------------------------------
 
 def scan_cell(D, N, G, dtype, seed=0, bias=True):
@@ -148,7 +166,7 @@ SCANS = [
 def run_scan(cell, x, dt, z, bc, GN, lens, st, left=0, y_fill=7.0, stream=None):
     B, S, D = x.shape
     y = torch.full((B, S, D), y_fill, dtype=x.dtype, device=DEV)
-    so = torch.empty(B, *cell.state_shape, device=DEV)
+    so = torch.empty(B, cell.D, cell.N, device=DEV)
     ws = torch.full((mt.mt_ssm_workspace_bytes(cell, B, S),), 255, dtype=torch.uint8, device=DEV)
     r = 2 if left else 0
     w = wide(bc, left, r)
@@ -200,6 +218,30 @@ def test_step(M, n, D, N, G, gate, left, dtype):
                                    st[row[m]].double())
         check(y[s], want, ye, "y")
         check(so[m], h, he, "state")
+
+
+@pytest.mark.parametrize("M,D,N", [(300, 2000, 16), (1100, 120, 64)])
+def test_step_of_large_states(M, D, N):
+    """States of more than 32 MB, which are stored past the L2s."""
+    cell, A, dtb, skip = scan_cell(D, N, 1, "bf16")
+    x, dt, z, bc = scan_inputs((M,), D, N, 1, "bf16", M)
+    st = torch.randn(M, D, N, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV)
+    row = torch.randint(0, M, (M,), generator=gen(4), dtype=torch.int32)
+    y, so = torch.empty(M, D, dtype=x.dtype, device=DEV), torch.empty(M, D, N, device=DEV)
+    w = dev(bc)
+    mt.mt_ssm_step(cell, dev(x), dev(dt), w[:, :N], w[:, N:], y, st, so, z=dev(z), src_row=dev(row))
+    for m in (0, 1, M // 2, M - 1):
+        s = slice(m, m + 1)
+        want, h, ye, he = ref.scan(x[s].double(), dt[s].double(), per_channel(bc[s], D, N, 1, False),
+                                   per_channel(bc[s], D, N, 1, True), z[s].double(), A, dtb, skip,
+                                   st[row[m].item()].cpu().double())
+        check(y[s], want, ye, "y")
+        check(so[m], h, he, "state")
+    # the same rows in place, by a smaller call: the same bits
+    sub = st[row[:4].long().to(DEV)].clone()
+    y2 = torch.empty(4, D, dtype=x.dtype, device=DEV)
+    mt.mt_ssm_step(cell, dev(x[:4]), dev(dt[:4]), w[:4, :N], w[:4, N:], y2, sub, sub, z=dev(z[:4]))
+    assert torch.equal(y2, y[:4]) and torch.equal(sub, so[:4])
 
 
 def test_step_in_place_and_bad_rows():
@@ -303,12 +345,16 @@ def product(x, W, bias, ydt, left=0, pad=0):
     return y
 
 
-@pytest.mark.parametrize("xdt,ydt", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
-@pytest.mark.parametrize("M,K,N,bias,left", [
+PRODUCTS = [
     (1, 1, 1, True, 0), (1, 16, 32, False, 0), (2, 17, 33, True, 1), (5, 64, 257, True, 0), (16, 128, 64, False, 8),
     (31, 100, 96, True, 0), (32, 512, 40, True, 0), (33, 333, 300, False, 5), (63, 65, 129, True, 0), (64, 256, 1000, True, 0),
     (65, 130, 255, True, 0), (127, 200, 128, True, 0), (129, 1024, 513, True, 8), (257, 96, 600, False, 0),
-    (300, 2000, 77, True, 0), (1, 4096, 200, True, 0), (3, 5000, 31, False, 0), (20, 65536, 48, False, 0)])
+    (300, 2000, 77, True, 0), (1, 4096, 200, True, 0), (3, 5000, 31, False, 0), (20, 65536, 48, False, 0),
+    (4, 600, 70, True, 0), (3, 1500, 33, False, 1), (4, 3000, 2500, True, 0)]
+
+
+@pytest.mark.parametrize("xdt,ydt", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("M,K,N,bias,left", PRODUCTS)
 def test_product(M, K, N, bias, left, xdt, ydt):
     g = gen(M + K + N)
     x = (torch.randn(M, K, generator=g) * torch.exp(2 * torch.randn(M, 1, generator=g))).to(IO[xdt])
@@ -317,6 +363,33 @@ def test_product(M, K, N, bias, left, xdt, ydt):
     y = product(x, W.numpy(), b, IO[ydt], left, 3 if left else 0)
     want, err = ref.product(x.float().numpy(), W.numpy(), None if b is None else b.numpy())
     check(y, torch.from_numpy(want), torch.from_numpy(err), "y")
+
+
+# (M, K, N): the larger tiles, with part of the last one in rows and columns; results above and below the
+# size from which they are stored past the L2s
+LARGE_PRODUCTS = [(1100, 200, 2001), (70, 500, 50001), (4000, 2000, 500), (770, 513, 20002), (3000, 300, 4100), (2000, 6000, 8000)]
+
+
+@pytest.mark.parametrize("ydt", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", LARGE_PRODUCTS)
+def test_large_products(M, K, N, ydt):
+    g = torch.Generator(device=DEV).manual_seed(M)
+    x, W = torch.randn(M, K, generator=g, device=DEV), torch.randn(K, N, generator=g, device=DEV)
+    b = torch.randn(N, generator=g, device=DEV)
+    mat = mt.mt_i8_load(W, b)
+    ws = torch.full((mt.mt_i8_workspace_bytes(mat, M),), 255, dtype=torch.uint8, device=DEV)
+    outs = []
+    for ld in (N, (N + 15) // 8 * 8):  # rows of odd length; rows aligned for vectors
+        y = torch.full((M + 1, ld), 7.0, dtype=IO[ydt], device=DEV)
+        mt.mt_i8_product(mat, x, y[:M, :N], ws)
+        assert bool((y[M] == 7.0).all()) and bool((y[:, N:] == 7.0).all())  # nothing beside the result
+        outs.append(y[:M, :N])
+    assert torch.equal(*outs)
+    qx, sx = (torch.from_numpy(t) for t in ref.quantise(x.cpu().numpy(), 1))
+    qw, sw = (torch.from_numpy(t) for t in ref.quantise(W.cpu().numpy(), 0))
+    p = (qx.double().to(DEV) @ qw.double().to(DEV)) * sw.double().to(DEV) * sx.double().to(DEV)  # sums exact in 64 bits
+    want = p + b.double()
+    check(outs[0], want.cpu(), (4 * ref.U * (p.abs() + want.abs())).cpu(), "y")
 
 
 def test_product_edges():

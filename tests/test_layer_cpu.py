@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from paper_1804_00344_amd import mtstep as mt
+from routes import _fn
 
 P = 1 << 20  # addresses that are never followed: every call below ends before a launch
 
@@ -223,14 +224,57 @@ def test_no_convolution():
 # ---- the binding --------------------------------------------------------------------------------
 
 def test_binding_refuses_tensors():
-    rows = lambda t, lead, width, dt=torch.float32: mt._rows(t, "x", lead, width, dt, torch.device("cpu"))
+    rows = lambda t, lead, width, dt=torch.float32: mt._rows(t, "x", lead + (width,), dt, torch.device("cpu"))
     t = torch.zeros(3, 5, 16)
     assert rows(t, (3, 5), 16)[1] == 16 and rows(t[..., 4:12], (3, 5), 8)[1] == 16
     assert rows(torch.zeros(1, 16)[:, :3], (1,), 3)[1] == 3
     for bad in (lambda: rows(t, (3, 5), 15), lambda: rows(t.bfloat16(), (3, 5), 16), lambda: rows(t[:, :4], (3, 4), 16),
                 lambda: rows(t[..., ::2], (3, 5), 8), lambda: rows(t.transpose(1, 2), (3, 16), 5),
-                lambda: mt._rows(t, "x", (3, 5), 16, t.dtype, torch.device("cuda", 0)),
+                lambda: mt._rows(t, "x", (3, 5, 16), t.dtype, torch.device("cuda", 0)),
                 lambda: mt._packed(t[:, ::2], "s", (3, 3, 16), t.dtype, t.device),
-                lambda: mt._index(torch.zeros(3, dtype=torch.int64), "lens", 3, t.device)):
+                lambda: mt._packed(torch.zeros(3, dtype=torch.int64), "lens", (3,), torch.int32, t.device)):
         with pytest.raises(ValueError):
             bad()
+
+
+# ---- which form a call takes ----------------------------------------------------------------------
+
+def i8_form(M, N, K, y_bytes=4, num_cu=256):
+    return _fn("_ZN2mt7i8_formEiiiii", C.c_int, 5)(M, N, K, y_bytes, num_cu)
+
+
+def scan_pieces(B, S, D, N, num_cu=256):
+    return _fn("_ZN2mt11scan_piecesEiiiii", C.c_int, 5)(B, S, D, N, num_cu)
+
+
+@pytest.mark.parametrize("M,N,K,form", [(1, 50000, 512, -1), (4, 2048, 4096, -1), (5, 2048, 512, 0), (4, 2048, 4097, 0),
+                                        (64, 2048, 2048, 0), (4096, 512, 2048, 1), (128, 50000, 512, 2), (768, 50000, 512, 3),
+                                        (512, 8192, 2048, 2), (8192, 8192, 4096, 4)])
+def test_product_form(M, N, K, form):
+    assert i8_form(M, N, K, 2 if K == 4096 else 4) == form
+
+
+def test_gpu_product_cases_take_every_form():
+    from test_gpu_layer import LARGE_PRODUCTS, PRODUCTS
+    cases = [(M, N, K) for M, K, N, *_ in PRODUCTS] + [(M, N, K) for M, K, N in LARGE_PRODUCTS]
+    assert {i8_form(M, N, K, es) for M, N, K in cases for es in (2, 4)} == {-1, 0, 1, 2, 3, 4}
+
+
+@pytest.mark.parametrize("B,S,D,N,pieces", [(64, 80, 2048, 16, 1), (1, 8, 2048, 16, 1), (1, 8192, 2048, 16, 64),
+                                            (1, 2 ** 20, 64, 16, 256), (1, 4, 65536, 256, 1)])
+def test_scan_pieces(B, S, D, N, pieces):
+    assert scan_pieces(B, S, D, N) == pieces
+
+
+def test_scan_pieces_cover_the_axis_and_the_workspace_holds_them():
+    for S in (1, 15, 16, 17, 100, 1000, 12345):
+        n = scan_pieces(2, S, 100, 24)
+        assert 1 <= n <= max(1, S // 8)
+        c = cell(D=100, N=24)
+        assert mt.lib().mt_ssm_workspace_bytes(C.addressof(c), 2, S) == 2 * (n - 1) * 100 * 33 * 4 + 256
+
+
+def test_gpu_scan_cases_take_both_forms():
+    from test_gpu_layer import SCANS
+    pieces = [scan_pieces(B, S, D, N) for B, S, D, N, *_ in SCANS]
+    assert min(pieces) == 1 and max(pieces) >= 16

@@ -70,6 +70,7 @@ struct ScanPlan {
   int lanes;              // lanes per channel
   int chunks, chunk_len;  // pieces of the axis
   int threads, ngr;       // of a workgroup; groups of its channels
+  int ordered;            // prompts in the order of longest_first
   float *part;            // [B][chunks - 1][D][Np] state of each piece started from zero
   float *dsum;            // [B][chunks - 1][D] sum of D_t over it
 };
@@ -112,6 +113,17 @@ __device__ __forceinline__ float transpose_sum(float (&y)[J], int sub) {
 // positions of B and C staged together: two tiles of 64 / LPC groups fit into 64 KiB
 constexpr int tile_positions(int NS) { return NS <= 8 ? 8 : 4; }
 
+// The z-th of up to 64 prompts in the order long (more than half of S), middle (more than a quarter),
+// short: workgroups are dispatched in the order of z, and a long prompt that starts last ends last.
+__device__ __forceinline__ int longest_first(const int32_t *len, int B, int S, int z) {
+  const int l = threadIdx.x & 63, n = l < B ? len[l] : 0;
+  const bool c0 = l < B && n > S / 2, c1 = l < B && !c0 && n > S / 4, c2 = l < B && !c0 && !c1;
+  const uint64_t m0 = __ballot(c0), m1 = __ballot(c1), m2 = __ballot(c2), below = (1ull << l) - 1;
+  const int place = c0 ? __popcll(m0 & below) : c1 ? __popcll(m0) + __popcll(m1 & below)
+                                                   : __popcll(m0 | m1) + __popcll(m2 & below);
+  return __ffsll(__ballot(l < B && place == z)) - 1;
+}
+
 // A workgroup takes the channels of its threads / LPC in one piece of a prompt; LPC lanes share a channel,
 // NS states each.  The work per position and channel (softplus, gate, skip) is spread over the lanes:
 // lane j of each J = min(LPC, 4) does it for the j-th of J positions.  B and C of the next tile and x,
@@ -153,7 +165,9 @@ __global__ void __launch_bounds__(256, NS == 16 ? 2 : 4) scan_kernel(ScanArgs a,
 #pragma unroll
   for (int k = 0; k < STAGE; ++k) element(tid + k * nthr, e_t[k], e_src[k]);
 
-  for (int b = blockIdx.z; b < a.B; b += gridDim.z) {
+  for (int bz = blockIdx.z; bz < a.B; bz += gridDim.z) {
+    int b = bz;
+    if (pl.ordered) b = __builtin_amdgcn_readfirstlane(longest_first(a.len, a.B, a.S, bz));
     int len = a.S;
     if (a.len) {
       len = a.len[b];
@@ -247,7 +261,8 @@ __global__ void __launch_bounds__(256, NS == 16 ? 2 : 4) scan_kernel(ScanArgs a,
           // the next position's B and C are read when this one's states are done: the compiler would
           // otherwise read those of many positions at once and spill
 #pragma unroll
-          for (int n = 0; n < NS; ++n) asm volatile("" : "+v"(h[n])::"memory");
+          for (int n = 0; n < NS; ++n)
+            asm volatile("" : "+v"(h[n])::"memory");
         }
         if constexpr (FINAL) {
           const float yv = fmaf(skip, xv, transpose_sum<LPC, J>(y, sub)), g = silu(zv);
@@ -507,6 +522,7 @@ size_t scan_workspace_bytes(int B, int S, int D, int N, int num_cu) {
 hipError_t launch_scan(const ScanArgs &a, hipStream_t st) {
   ScanPlan p = scan_plan(a.B, a.S, a.D, a.N, a.num_cu);
   const size_t n = (size_t)a.B * (p.chunks - 1) * a.D;
+  p.ordered = a.len && a.B > 1 && a.B <= 64 && p.chunks == 1;
   p.part = (float *)a.ws;
   p.dsum = p.part + n * a.Np;
   return a.bf16_io ? scan_by_states<bf16>(a, p, st) : scan_by_states<float>(a, p, st);

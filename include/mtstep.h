@@ -427,7 +427,7 @@ void mt_round_bf16(const float *src, uint16_t *dst, size_t n);
  *   - A call reads its handle and does not change it: one handle serves several streams and
  *     threads at once, each call with its own outputs and workspace.  The current device must
  *     be the one the handle was loaded on (MT_ERR_STATE otherwise).  Calls may be captured into
- *     a graph; they allocate nothing and record kernels only.
+ *     a graph; they allocate nothing and record kernels only.  mt_profile_* does not time them.
  *   - An output that overlaps an input, the workspace or another output is refused (MT_ERR_ARG),
  *     except where a call says otherwise; columns of one wider matrix (the same stride) do not
  *     overlap.

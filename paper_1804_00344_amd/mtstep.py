@@ -461,6 +461,13 @@ def _packed(t, name, shape, dtype, device):
     return t.data_ptr()
 
 
+def _space(ws, device):
+    """(address, bytes) of a workspace."""
+    if ws.device != device or not ws.is_contiguous():
+        raise ValueError(f"ws: need a contiguous tensor on {device}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
 def _host_or_device(a):
     """An fp32 array and its address: a device tensor stays where it is."""
     import torch
@@ -510,8 +517,7 @@ def mt_i8_product(mat: I8Matrix, x, y, ws, stream=None):
     xt, yt = _io(x, "x"), _io(y, "y")
     xp, ldx = _rows(x, "x", lead + (mat.K,), x.dtype, dev)
     yp, ldy = _rows(y, "y", lead + (mat.N,), y.dtype, dev)
-    _check(lib().mt_i8_product(mat.handle, lead.numel(), xp, xt, ldx, yp, yt, ldy, _ptr(ws),
-                               ws.numel() * ws.element_size(), _stream(stream)))
+    _check(lib().mt_i8_product(mat.handle, lead.numel(), xp, xt, ldx, yp, yt, ldy, *_space(ws, dev), _stream(stream)))
 
 
 def make_ssm_config(D, N, *, groups=1, conv=0, conv_silu=True, dtype="f32"):
@@ -601,8 +607,7 @@ def mt_ssm_scan(cell: Ssm, x, dt, bmat, cmat, y, *, z=None, lens=None, state_in=
     st = (B, cell.D, cell.N)
     _check(lib().mt_ssm_scan(cell.handle, B, S, _packed(lens, "lens", (B,), cell.i32, dev), *r[:9],
                              _packed(state_in, "state_in", st, cell.f32, dev), r[9], r[10],
-                             _packed(state_out, "state_out", st, cell.f32, dev), _ptr(ws),
-                             ws.numel() * ws.element_size(), _stream(stream)))
+                             _packed(state_out, "state_out", st, cell.f32, dev), *_space(ws, dev), _stream(stream)))
 
 
 def mt_ssm_step(cell: Ssm, x, dt, bmat, cmat, y, state_in, state_out, *, z=None, src_row=None, stream=None):

@@ -487,3 +487,65 @@ def test_calls_run_on_the_given_stream_and_replay():
         torch.cuda.synchronize()
         for a, b in zip(got, (out, hs, cs, y)):
             assert torch.equal(a, b), i
+
+
+def test_many_short_prompts_and_tokens():
+    """More sentences than a grid dimension holds at once: every one is worked on, and none twice."""
+    B, S, D, N, W = 40000, 2, 12, 4, 3
+    g = gen(21)
+    w = dict(A=-torch.exp(torch.randn(D, N, generator=g)), conv_w=torch.randn(D, W, generator=g))
+    cell = mt.mt_ssm_load(mt.make_ssm_config(D, N, conv=W, dtype="f32"), w)
+    x, dt = torch.randn(B, S, D, generator=g), torch.randn(B, S, D, generator=g)
+    bc = torch.randn(B, S, 2 * N, generator=g)
+    lens = torch.randint(0, S + 1, (B,), generator=g, dtype=torch.int32)
+    st, cs = torch.randn(B, D, N, generator=g), torch.randn(B, W - 1, D, generator=g)
+
+    def calls(i, j):  # sentences i .. j - 1
+        n = j - i
+        y, so = torch.zeros(n, S, D, device=DEV), torch.empty(n, D, N, device=DEV)
+        yc, co = torch.zeros(n, S, D, device=DEV), torch.empty(n, W - 1, D, device=DEV)
+        ys, ss = torch.empty(n, D, device=DEV), torch.empty(n, D, N, device=DEV)
+        ysc, sc = torch.empty(n, D, device=DEV), torch.empty(n, W - 1, D, device=DEV)
+        ws = torch.empty(mt.mt_ssm_workspace_bytes(cell, n, S), dtype=torch.uint8, device=DEV)
+        xd, dd, bd, l, s0, c0 = (dev(t[i:j].contiguous()) for t in (x, dt, bc, lens, st, cs))
+        mt.mt_ssm_scan(cell, xd, dd, bd[..., :N], bd[..., N:], y, lens=l, state_in=s0, state_out=so, ws=ws)
+        mt.mt_ssm_conv(cell, xd, yc, lens=l, state_in=c0, state_out=co)
+        mt.mt_ssm_step(cell, xd[:, 0], dd[:, 0], bd[:, 0, :N], bd[:, 0, N:], ys, s0, ss)
+        mt.mt_ssm_conv_step(cell, xd[:, 0], ysc, c0, sc)
+        return y, so, yc, co, ys, ss, ysc, sc
+
+    parts = [calls(i, min(B, i + 9000)) for i in range(0, B, 9000)]
+    for whole, *pieces in zip(calls(0, B), *parts):
+        assert torch.equal(whole, torch.cat(pieces))
+    assert mt.mt_ssm_device_errors(cell) == 0
+
+
+def test_one_handle_on_two_streams():
+    B, S, D, N = 3, 700, 64, 16
+    cell, *_ = scan_cell(D, N, 1, "f32")
+    mat = mt.mt_i8_load(torch.randn(D, 300, generator=gen(1)))
+    runs = []
+    for seed in (1, 2):
+        x, dt, z, bc = (dev(t) for t in scan_inputs((B, S), D, N, 1, "f32", seed))
+        runs.append(dict(x=x, dt=dt, z=z, bc=bc, y=torch.zeros_like(x), so=torch.empty(B, D, N, device=DEV),
+                         out=torch.empty(B, S, 300, device=DEV), st=torch.cuda.Stream(),
+                         ws=torch.empty(max(mt.mt_ssm_workspace_bytes(cell, B, S), mt.mt_i8_workspace_bytes(mat, B * S)),
+                                        dtype=torch.uint8, device=DEV)))
+
+    def go(r, stream):
+        mt.mt_ssm_scan(cell, r["x"], r["dt"], r["bc"][..., :N], r["bc"][..., N:], r["y"], z=r["z"], state_out=r["so"], ws=r["ws"],
+                       stream=stream)
+        mt.mt_i8_product(mat, r["y"], r["out"], r["ws"], stream=stream)
+
+    want = []
+    for r in runs:
+        go(r, None)
+        want.append([r[k].clone() for k in ("y", "so", "out")])
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for r in runs:
+            go(r, r["st"])
+    torch.cuda.synchronize()
+    for r, w in zip(runs, want):
+        for k, v in zip(("y", "so", "out"), w):
+            assert torch.equal(r[k], v)

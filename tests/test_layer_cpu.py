@@ -231,6 +231,7 @@ def test_binding_refuses_tensors():
     for bad in (lambda: rows(t, (3, 5), 15), lambda: rows(t.bfloat16(), (3, 5), 16), lambda: rows(t[:, :4], (3, 4), 16),
                 lambda: rows(t[..., ::2], (3, 5), 8), lambda: rows(t.transpose(1, 2), (3, 16), 5),
                 lambda: mt._rows(t, "x", (3, 5, 16), t.dtype, torch.device("cuda", 0)),
+                lambda: mt._space(t, torch.device("cuda", 0)), lambda: mt._space(t[:, 1:], t.device),
                 lambda: mt._packed(t[:, ::2], "s", (3, 3, 16), t.dtype, t.device),
                 lambda: mt._packed(torch.zeros(3, dtype=torch.int64), "lens", (3,), torch.int32, t.device)):
         with pytest.raises(ValueError):

@@ -69,7 +69,7 @@ __device__ __forceinline__ void store_states(float *p, int n, bool wide, const f
 struct ScanPlan {
   int lanes;              // lanes per channel
   int chunks, chunk_len;  // pieces of the axis
-  int threads, ngr;       // of a workgroup; groups of its channels
+  int waves, ngr;         // of a workgroup: waves with channels, groups of their channels
   int ordered;            // prompts in the order of longest_first
   float *part;            // [B][chunks - 1][D][Np] state of each piece started from zero
   float *dsum;            // [B][chunks - 1][D] sum of D_t over it
@@ -113,6 +113,9 @@ __device__ __forceinline__ float transpose_sum(float (&y)[J], int sub) {
 // positions of B and C staged together: two tiles of 64 / LPC groups fit into 64 KiB
 constexpr int tile_positions(int NS) { return NS <= 8 ? 8 : 4; }
 
+// elements of B and C of the next tile that a thread holds in registers
+constexpr int scan_stage(int Np) { return Np > 16 ? Np / 16 : 1; }
+
 // The z-th of up to 64 prompts in the order long (more than half of S), middle (more than a quarter),
 // short: workgroups are dispatched in the order of z, and a long prompt that starts last ends last.
 __device__ __forceinline__ int longest_first(const int32_t *len, int B, int S, int z) {
@@ -129,15 +132,24 @@ __device__ __forceinline__ int longest_first(const int32_t *len, int B, int S, i
 // lane j of each J = min(LPC, 4) does it for the j-th of J positions.  B and C of the next tile and x,
 // dt and z of its positions are on their way while a tile is computed.  A tile is always computed whole:
 // behind the end the steps D_t are zero, which keeps the state as it is.
-template <typename T, int NS, int LPC, bool FINAL>
-__global__ void __launch_bounds__(256, NS == 16 ? 2 : 4) scan_kernel(ScanArgs a, ScanPlan pl) {
+// Bound by the issue of vector instructions: 90 to 95% of the cycles with waves on a SIMD issue one, and an
+// exp2 (10 to 11 cycles) does not overlap the products (3 each).
+// MANY: B and C of a tile, of several groups or many states, are more than a thread holds in scan_stage
+// registers.  All 256 threads stage them then, also those of waves without channels, at distances that are
+// the same for all threads.  2 x 500 x 1024 x 16 of 1024 groups took 317 us with the staging of one
+// group and takes 171, 23 x 1595 x 16 x 16 of 8 groups 79 and 37, 2 x 721 x 16 x 128 of 4 groups 50 and 39; the
+// other way round, this staging for one group, 64 x 80 x 2048 x 16 took 32 in place of 29.  Two groups at 32
+// states lose by it: 7 x 97 x 330 x 24 of 3 groups 16 and 18.
+template <typename T, int NS, int LPC, bool FINAL, bool MANY>
+__global__ void __launch_bounds__(256, NS == 4 ? 4 : NS == 8 ? 3 : 2) scan_kernel(ScanArgs a, ScanPlan pl) {
   constexpr int J = LPC < 4 ? LPC : 4, Np = NS * LPC, kTile = tile_positions(NS), SLOTS = kTile / J;
-  constexpr int STAGE = Np / 16 > 4 ? Np / 16 : 4;  // elements of B and C that a thread holds for the next tile
+  constexpr int STAGE = MANY ? (Np <= 64 ? 4 : 8) : scan_stage(Np);  // elements a thread holds for the next tile
   extern __shared__ __attribute__((aligned(16))) float lds[];
-  const int tid = threadIdx.x, nthr = blockDim.x, cpb = nthr / LPC, sub = tid % LPC, n0 = sub * NS, tj = sub % J;
-  const int c0 = blockIdx.x * cpb;
+  const int tid = threadIdx.x, nthr = MANY ? 256 : blockDim.x, sub = tid % LPC, n0 = sub * NS, tj = sub % J;
+  const int cpb = (MANY ? pl.waves * 64 : nthr) / LPC, c0 = blockIdx.x * cpb;
   const int d = min(c0 + tid / LPC, a.D - 1);
   const bool owner = c0 + tid / LPC < a.D;
+  const bool works = !MANY || ((tid >> 6) < pl.waves && c0 + (tid & ~63) / LPC < a.D);  // the wave has channels
   const int per = a.D / a.G, g0 = c0 / per, gi = d / per - g0;
   const int chunk = blockIdx.y;
   constexpr int nw = FINAL ? 2 : 1;        // the first pass reads B only
@@ -151,19 +163,35 @@ __global__ void __launch_bounds__(256, NS == 16 ? 2 : 4) scan_kernel(ScanArgs a,
   for (int i = 0; i < NS; ++i) A2[i] = a.A2[(size_t)d * Np + n0 + i];
   const float dtb = a.dt_bias[d], skip = a.skip[d];
 
-  // A tile in LDS: [group][position][B, C][Np], states that do not exist zero.  Element e of it: its
-  // position (none if there is no such element) and its source.
-  auto element = [&](int e, int &t, const T *&src) {
-    const int n = e % Np, w = e / Np % nw, g = g0 + e / grpl;
-    t = e / (Np * nw) % kTile;
-    src = (const T *)(w ? a.cm : a.bm) + (long long)t * a.ldbc + (long long)g * a.N + n;
-    if (e >= bufl || n >= a.N || g >= a.G) t = 1 << 30;
-  };
-  const bool pre = bufl <= STAGE * nthr;
+  // A tile in LDS: [group][position][B, C][Np], states that do not exist zero.
+  // Not MANY: element k of a thread, number tid + k nthr of the tile: its position (none if there is no
+  // such element) and its source.
   const T *e_src[STAGE];
   int e_t[STAGE];
+  if constexpr (!MANY) {
 #pragma unroll
-  for (int k = 0; k < STAGE; ++k) element(tid + k * nthr, e_t[k], e_src[k]);
+    for (int k = 0; k < STAGE; ++k) {
+      const int e = tid + k * nthr, n = e % Np, w = e / Np % nw, g = g0 + e / grpl;
+      e_t[k] = e / (Np * nw) % kTile;
+      e_src[k] = (const T *)(w ? a.cm : a.bm) + (long long)e_t[k] * a.ldbc + (long long)g * a.N + n;
+      if (e >= bufl || n >= a.N || g >= a.G) e_t[k] = 1 << 30;
+    }
+  }
+  // MANY: passes of 256 elements, one per thread: R passes per group, or GP groups per pass.  The place of a
+  // thread's elements within a group and their distances are the same in every pass.
+  constexpr int R = grpl / 256, GP = R ? 1 : 256 / grpl, ROW = Np * nw, TSTEP = ROW <= 256 ? 256 / ROW : 1;
+  const int passes = R ? pl.ngr * R : (pl.ngr + GP - 1) / GP;
+  const int en = ROW <= 256 ? tid % Np : tid, et = ROW <= 256 ? tid % grpl / ROW : 0, eg = R ? 0 : tid / grpl;
+  const T *const eb = (const T *)a.bm + (long long)g0 * a.N + en, *const ec = (const T *)a.cm + (long long)g0 * a.N + en;
+  const T *const esrc = (ROW <= 256 && tid / Np % nw ? ec : eb) + (long long)et * a.ldbc;
+  auto element = [&](int k, long long o, int left) -> T {  // of pass k; left: positions of the prompt from the tile on
+    const int g = R ? k / (R ? R : 1) : eg + k * GP, q = R ? k % (R ? R : 1) : 0;
+    const int t = ROW <= 256 ? et + q * TSTEP : q / nw;
+    if (en >= a.N || g >= pl.ngr || g0 + g >= a.G || t >= left) return (T)0.f;
+    const T *src = ROW <= 256 ? esrc + (long long)(q * TSTEP) * a.ldbc : (q % nw ? ec : eb) + (long long)t * a.ldbc;
+    return src[o + (long long)g * a.N];
+  };
+  const bool pre = !MANY || passes <= STAGE;
 
   for (int bz = blockIdx.z; bz < a.B; bz += gridDim.z) {
     int b = bz;
@@ -202,8 +230,12 @@ __global__ void __launch_bounds__(256, NS == 16 ? 2 : 4) scan_kernel(ScanArgs a,
       const long long o = ob + (ts - t0) * a.ldbc;
 #pragma unroll
       for (int k = 0; k < STAGE; ++k) {
-        er[k] = (T)0.f;
-        if (e_t[k] < t1 - ts) er[k] = e_src[k][o];
+        if constexpr (MANY) {
+          if (k < passes) er[k] = element(k, o, t1 - ts);
+        } else {
+          er[k] = (T)0.f;
+          if (e_t[k] < t1 - ts) er[k] = e_src[k][o];
+        }
       }
     };
     auto stage_bc = [&](int ts, float *buf) {
@@ -212,11 +244,13 @@ __global__ void __launch_bounds__(256, NS == 16 ? 2 : 4) scan_kernel(ScanArgs a,
         for (int k = 0; k < STAGE; ++k)
           if (tid + k * nthr < bufl) buf[tid + k * nthr] = (float)er[k];
       } else {
-        for (int e = tid; e < bufl; e += nthr) {
-          int t;
-          const T *src;
-          element(e, t, src);
-          buf[e] = t < t1 - ts ? (float)src[ob + (ts - t0) * a.ldbc] : 0.f;
+        for (int k0 = 0; k0 < passes; k0 += STAGE) {
+          T e[STAGE];
+#pragma unroll
+          for (int k = 0; k < STAGE; ++k) e[k] = element(k0 + k, ob + (ts - t0) * a.ldbc, t1 - ts);
+#pragma unroll
+          for (int k = 0; k < STAGE; ++k)
+            if (tid + (k0 + k) * 256 < bufl) buf[tid + (k0 + k) * 256] = (float)e[k];
         }
       }
     };
@@ -230,8 +264,10 @@ __global__ void __launch_bounds__(256, NS == 16 ? 2 : 4) scan_kernel(ScanArgs a,
     float ds = 0.f;
     __syncthreads();  // the last tile of another prompt
     if (t0 < t1) {
+      if (works) {
 #pragma unroll
-      for (int i = 0; i < SLOTS; ++i) fetch_row(false, t0, i);
+        for (int i = 0; i < SLOTS; ++i) fetch_row(false, t0, i);
+      }
       if (pre) fetch_bc(t0);
       stage_bc(t0, lds);
     }
@@ -281,20 +317,22 @@ __global__ void __launch_bounds__(256, NS == 16 ? 2 : 4) scan_kernel(ScanArgs a,
       const bool more = ts + kTile < t1;
       if (more && pre) fetch_bc(ts + kTile);
       const float *buf = lds + p * bufl + gi * grpl + n0;
-      if (ts + 2 * kTile < t1)
+      if (!works) {
+      } else if (ts + 2 * kTile < t1) {
         compute(std::true_type(), ts, buf);
-      else
+      } else {
         compute(std::false_type(), ts, buf);
+      }
       p ^= 1;
       if (more) stage_bc(ts + kTile, lds + p * bufl);
     }
     if constexpr (FINAL) {
-      if (owner && a.state_out && t1 == len && nn > 0)
+      if (works && owner && a.state_out && t1 == len && nn > 0)
         store_states<NS>(a.state_out + ((long long)b * a.D + d) * a.N + n0, nn, wide, h);
     } else {
       const long long o = (long long)b * (pl.chunks - 1) + chunk;
       ds = group_sum<J>(ds);
-      if (owner) {
+      if (works && owner) {
         store_states<NS>(pl.part + (o * a.D + d) * Np + n0, NS, true, h);
         if (sub == 0) pl.dsum[o * a.D + d] = ds;
       }
@@ -411,18 +449,19 @@ __global__ void __launch_bounds__(kThreads) scan_step_kernel(ScanArgs a) {
 }
 
 // groups that n neighbouring channels can touch
-int scan_groups(int n, int per, int G) { return std::min({G, n, (n - 1) / per + 2}); }
+int scan_groups(int n, int per, int G) { return std::min({G, n, per % n == 0 ? 1 : (n - 1) / per + 2}); }
 
 // Lanes of a channel: four states each, more where they exceed a row of 16 lanes.  (16 states per lane, one
 // lane a channel, spilled or left a SIMD two waves: 1 x 8192 x 2048 x 16 176 us and more; eight per lane
-// 156, four 158; 64 x 80 ragged 39 and 33.)
+// 156, four 158; 64 x 80 ragged 39 and 33, before the prompts were ordered.)
 int scan_lanes(int Np) { return std::min(Np / 4, 16); }
 
 // Pieces of the axis, by the time they are expected to take: with k waves on a SIMD a wave's position takes
 // hypot(0.14, 0.083 k) us, and as much more as a lane holds more than four states (fitted to 2048
 // channels x 16 states, 8192 positions, k = 1 to 8).  Cutting the axis adds a first pass over it (0.75 of
-// the second's time) and the join.  Measured, 1 x 8192 x 2048 x 16 in one piece 1353 us, in 16 pieces 196,
-// 32: 159, 64: 158, 128: 168; 64 x 80 whole 33, cut 62 and more; 7 x 97 x 330 x 24 whole 21, cut 16.
+// the second's time) and the join.  Measured, 1 x 8192 x 2048 x 16 in one piece 1343 us, in 16 pieces 187,
+// 32: 152, 64: 148, 128: 154; 64 x 80 x 2048 x 16 whole 29, in 10 pieces 108; 7 x 97 x 330 x 24 whole 23, in 13
+// pieces 18.
 ScanPlan scan_plan(int B, int S, int D, int N, int num_cu) {
   const int Np = scan_padded_states(N);
   ScanPlan best{};
@@ -449,17 +488,30 @@ hipError_t run_scan(const ScanArgs &a, ScanPlan pl, hipStream_t st) {
   const int per = a.D / a.G;
   // a workgroup's channels: fewer where their groups' B and C would not fit into LDS twice
   size_t lds;
-  for (pl.threads = std::min(256, (a.D * LPC + 63) / 64 * 64);; pl.threads -= 64) {
-    pl.ngr = scan_groups(pl.threads / LPC, per, a.G);
+  for (pl.waves = std::min(4, (a.D * LPC + 63) / 64);; --pl.waves) {
+    pl.ngr = scan_groups(pl.waves * 64 / LPC, per, a.G);
     lds = (size_t)pl.ngr * a.Np * 8 * tile_positions(NS) * 2;
-    if (lds <= 65536 || pl.threads == 64) break;
+    if (lds <= 65536 || pl.waves == 1) break;
   }
-  const unsigned gx = (unsigned)((a.D * LPC + pl.threads - 1) / pl.threads), gz = (unsigned)std::min(a.B, 32768);
+  const bool many = pl.ngr * a.Np * 2 * tile_positions(NS) > scan_stage(a.Np) * pl.waves * 64;
+  const int cpb = pl.waves * 64 / LPC;
+  const dim3 first((unsigned)((a.D + cpb - 1) / cpb), pl.chunks - 1, (unsigned)std::min(a.B, 32768)),
+      second(first.x, pl.chunks, first.z), threads(many ? 256 : pl.waves * 64);
+#define MT_SCAN(FINAL, MANY, GRID, LDS) \
+  hipLaunchKernelGGL((scan_kernel<T, NS, LPC, FINAL, MANY>), GRID, threads, LDS, st, a, pl)
   if (pl.chunks > 1) {
-    hipLaunchKernelGGL((scan_kernel<T, NS, LPC, false>), dim3(gx, pl.chunks - 1, gz), dim3(pl.threads), lds / 2, st, a, pl);
-    hipLaunchKernelGGL(scan_join_kernel, dim3((unsigned)(((long long)a.D * a.Np + 255) / 256), gz), dim3(256), 0, st, a, pl);
+    if (many)
+      MT_SCAN(false, true, first, lds / 2);
+    else
+      MT_SCAN(false, false, first, lds / 2);
+    hipLaunchKernelGGL(scan_join_kernel, dim3((unsigned)(((long long)a.D * a.Np + 255) / 256), first.z), dim3(256), 0, st, a,
+                       pl);
   }
-  hipLaunchKernelGGL((scan_kernel<T, NS, LPC, true>), dim3(gx, pl.chunks, gz), dim3(pl.threads), lds, st, a, pl);
+  if (many)
+    MT_SCAN(true, true, second, lds);
+  else
+    MT_SCAN(true, false, second, lds);
+#undef MT_SCAN
   return hipGetLastError();
 }
 

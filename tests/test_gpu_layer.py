@@ -160,7 +160,14 @@ SCANS = [
     (1, 9, 6, 256, 3, None, True, True, 0), (2, 3, 300, 17, 300, None, False, True, 0),
     # long axes of few rows: cut into pieces, some of them behind a prompt's end
     (1, 700, 16, 16, 1, None, True, True, 0), (3, 530, 20, 8, 1, [530, 64, 300], True, True, 0),
-    (2, 400, 9, 40, 3, [65, 400], False, True, 0)]
+    (2, 400, 9, 40, 3, [65, 400], False, True, 0),
+    # one group over workgroups of four waves, the last one not full, whole and cut into pieces
+    (2, 30, 300, 4, 1, [30, 11], True, True, 0), (1, 21, 150, 7, 1, None, False, False, 1),
+    (1, 600, 70, 16, 1, None, True, True, 0), (2, 410, 40, 32, 1, [410, 209], False, True, 0),
+    (1, 300, 37, 64, 1, None, True, False, 0), (1, 260, 34, 128, 1, None, True, True, 0),
+    (1, 170, 40, 250, 1, None, True, True, 0),
+    # several groups of many states, cut
+    (1, 330, 24, 100, 4, None, True, True, 0), (1, 150, 34, 256, 17, None, False, True, 0)]
 
 
 def run_scan(cell, x, dt, z, bc, GN, lens, st, left=0, y_fill=7.0, stream=None):

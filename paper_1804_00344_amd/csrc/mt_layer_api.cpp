@@ -6,6 +6,7 @@
 #include <cmath>
 #include <cstring>
 #include <initializer_list>
+#include <limits>
 #include <new>
 
 #include "mt_host.h"
@@ -276,7 +277,9 @@ mt_status mt_ssm_load(const mt_ssm_config *cfg, const mt_ssm_weights *w, mt_ssm 
     size_t o = 0;
     size_t oA = o, ob = (o += (size_t)D * Np), os = (o += D), ow = (o += D), oc = (o += (size_t)W * D);
     for (int d = 0; d < D; ++d) {
-      for (int n = 0; n < N; ++n) host[oA + (size_t)d * Np + n] = (float)((double)w->A[(size_t)d * N + n] * M_LOG2E);
+      for (int n = 0; n < N; ++n)  // finite, so that a step of zero keeps the state
+        host[oA + (size_t)d * Np + n] =
+            (float)std::max((double)w->A[(size_t)d * N + n] * M_LOG2E, -(double)std::numeric_limits<float>::max());
       if (w->dt_bias) host[ob + d] = w->dt_bias[d];
       if (w->skip) host[os + d] = w->skip[d];
       for (int j = 0; j < W; ++j) host[ow + (size_t)j * D + d] = w->conv_w[(size_t)d * W + j];
@@ -468,6 +471,7 @@ mt_status mt_ssm_device_errors(mt_ssm *c, int32_t *flags) {
   g_err[0] = 0;
   if (!valid(c)) return fail(MT_ERR_ARG, "invalid cell handle");
   if (!flags) return fail(MT_ERR_ARG, "flags is NULL");
+  CHECK(check_device(c->device));
   HIP_TRY(hipDeviceSynchronize());
   HIP_TRY(hipMemcpy(flags, c->err, 4, hipMemcpyDeviceToHost));
   const int32_t zero = 0;

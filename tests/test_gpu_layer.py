@@ -339,6 +339,22 @@ def test_large_and_infinite_steps(value):
         assert bool(torch.isnan(y[0, 2:, 3]).all())
 
 
+def test_rates_up_to_the_largest_float():
+    """A times log2(e) would leave fp32: the states forget in one step, and steps of zero keep them."""
+    D, N, S = 6, 5, 3
+    cell = mt.mt_ssm_load(mt.make_ssm_config(D, N), dict(A=torch.full((D, N), -torch.finfo(torch.float32).max)))
+    x, dt, _, bc = scan_inputs((1, S), D, N, 1, "f32", 1, False)
+    dt[0, 2, 0] = float("-inf")
+    y, so = run_scan(cell, x, dt, None, bc, N, None, dev(torch.randn(1, D, N, generator=gen(2))))
+    d = torch.log1p(torch.exp(dt.double()))
+    for c in range(D):
+        t = 1 if c == 0 else 2
+        want = d[0, t, c] * x[0, t, c].double() * bc[0, t, :N].double()
+        # softplus within 14 roundings, two products
+        check(so[0, c], want, 16 * ref.U * want.abs(), "state")
+    assert bool(torch.isfinite(y).all())
+
+
 # ---- products in 8 bits -------------------------------------------------------------------------
 
 def product(x, W, bias, ydt, left=0, pad=0):

@@ -93,6 +93,12 @@ def test_handles_are_checked():
         assert status("mt_ssm_device_errors", h, C.byref(C.c_int32())) == mt.MT_ERR_ARG
 
 
+def test_device_errors_of_another_device():
+    c = cell()
+    assert reached_device_check(status("mt_ssm_device_errors", C.addressof(c), C.byref(C.c_int32())))
+    assert status("mt_ssm_device_errors", C.addressof(c), None) == mt.MT_ERR_ARG
+
+
 # ---- products in 8 bits -------------------------------------------------------------------------
 
 BIG = 1 << 40

@@ -26,13 +26,20 @@ __device__ __forceinline__ float softplus(float v) {
   return fmaf(s + s, p, fmaxf(v, 0.0f));
 }
 
+// The value of another lane of a row.  All lanes of these patterns exist, and saying so (bound_ctrl) lets the
+// compiler make the move part of the instruction that uses it.
+template <int CTRL>
+__device__ __forceinline__ float lane_mov(float v) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+
 // Sum over the L neighbouring lanes of a channel (a power of two), the result in each
 template <int L>
 __device__ __forceinline__ float group_sum(float v) {
-  if constexpr (L >= 2) v += dpp_mov<kDppQuadSwap1>(v);
-  if constexpr (L >= 4) v += dpp_mov<kDppQuadSwap2>(v);
-  if constexpr (L >= 8) v += dpp_mov<0x141>(v);   // row_half_mirror: the other four lanes of eight
-  if constexpr (L >= 16) v += dpp_mov<0x140>(v);  // row_mirror: the other eight of sixteen
+  if constexpr (L >= 2) v += lane_mov<kDppQuadSwap1>(v);
+  if constexpr (L >= 4) v += lane_mov<kDppQuadSwap2>(v);
+  if constexpr (L >= 8) v += lane_mov<0x141>(v);   // row_half_mirror: the other four lanes of eight
+  if constexpr (L >= 16) v += lane_mov<0x140>(v);  // row_mirror: the other eight of sixteen
   if constexpr (L >= 32) v += __shfl_xor(v, 16, 64);
   if constexpr (L >= 64) v += __shfl_xor(v, 32, 64);
   return v;
@@ -79,12 +86,12 @@ struct ScanPlan {
 template <int J>
 __device__ __forceinline__ float bcast(float v, int j) {
   if constexpr (J == 1) return v;
-  if constexpr (J == 2) return j == 0 ? dpp_mov<0xA0>(v) : dpp_mov<0xF5>(v);
+  if constexpr (J == 2) return j == 0 ? lane_mov<0xA0>(v) : lane_mov<0xF5>(v);
   switch (j) {
-    case 0: return dpp_mov<0x00>(v);
-    case 1: return dpp_mov<0x55>(v);
-    case 2: return dpp_mov<0xAA>(v);
-    default: return dpp_mov<0xFF>(v);
+    case 0: return lane_mov<0x00>(v);
+    case 1: return lane_mov<0x55>(v);
+    case 2: return lane_mov<0xAA>(v);
+    default: return lane_mov<0xFF>(v);
   }
 }
 // lane j of each group of J receives the sum over its channel's L lanes of y[j]
@@ -92,20 +99,20 @@ template <int L, int J>
 __device__ __forceinline__ float transpose_sum(float (&y)[J], int sub) {
   if constexpr (L >= 16)
 #pragma unroll
-    for (int j = 0; j < J; ++j) y[j] += dpp_mov<0x140>(y[j]);  // row_mirror: lane 15 - l
+    for (int j = 0; j < J; ++j) y[j] += lane_mov<0x140>(y[j]);  // row_mirror: lane 15 - l
   if constexpr (L >= 8)
 #pragma unroll
-    for (int j = 0; j < J; ++j) y[j] += dpp_mov<0x141>(y[j]);  // row_half_mirror: lane 7 - l
+    for (int j = 0; j < J; ++j) y[j] += lane_mov<0x141>(y[j]);  // row_half_mirror: lane 7 - l
   if constexpr (J == 1) {
     return y[0];
   } else {
     const bool o1 = sub & 1, o2 = sub & 2;
-    const float a = (o1 ? y[1] : y[0]) + dpp_mov<kDppQuadSwap1>(o1 ? y[0] : y[1]);
+    const float a = (o1 ? y[1] : y[0]) + lane_mov<kDppQuadSwap1>(o1 ? y[0] : y[1]);
     if constexpr (J == 2) {
       return a;
     } else {
-      const float b = (o1 ? y[3] : y[2]) + dpp_mov<kDppQuadSwap1>(o1 ? y[2] : y[3]);
-      return (o2 ? b : a) + dpp_mov<kDppQuadSwap2>(o2 ? a : b);
+      const float b = (o1 ? y[3] : y[2]) + lane_mov<kDppQuadSwap1>(o1 ? y[2] : y[3]);
+      return (o2 ? b : a) + lane_mov<kDppQuadSwap2>(o2 ? a : b);
     }
   }
 }
@@ -132,12 +139,12 @@ __device__ __forceinline__ int longest_first(const int32_t *len, int B, int S, i
 // lane j of each J = min(LPC, 4) does it for the j-th of J positions.  B and C of the next tile and x,
 // dt and z of its positions are on their way while a tile is computed.  A tile is always computed whole:
 // behind the end the steps D_t are zero, which keeps the state as it is.
-// Bound by the issue of vector instructions: 90 to 95% of the cycles with waves on a SIMD issue one, and an
-// exp2 (10 to 11 cycles) does not overlap the products (3 each).
+// Bound by the vector units: they are active in 94% of the cycles (87% of the first pass) of 1 x 8192 x
+// 2048 x 16, at 2.25 GHz; an exp2 takes 10 to 11 cycles and does not overlap the products, 3 each.
 // MANY: B and C of a tile, of several groups or many states, are more than a thread holds in scan_stage
 // registers.  All 256 threads stage them then, also those of waves without channels, at distances that are
 // the same for all threads.  2 x 500 x 1024 x 16 of 1024 groups took 317 us with the staging of one
-// group and takes 171, 23 x 1595 x 16 x 16 of 8 groups 79 and 37, 2 x 721 x 16 x 128 of 4 groups 50 and 39; the
+// group and takes 174, 23 x 1595 x 16 x 16 of 8 groups 79 and 37, 2 x 721 x 16 x 128 of 4 groups 50 and 36; the
 // other way round, this staging for one group, 64 x 80 x 2048 x 16 took 32 in place of 29.  Two groups at 32
 // states lose by it: 7 x 97 x 330 x 24 of 3 groups 16 and 18.
 template <typename T, int NS, int LPC, bool FINAL, bool MANY>
@@ -287,15 +294,21 @@ __global__ void __launch_bounds__(256, NS == 4 ? 4 : NS == 8 ? 3 : 2) scan_kerne
         for (int j = 0; j < J; ++j) {
           const float *bq = buf + (i * J + j) * nw * Np, *cq = bq + Np;
           const float dlj = bcast<J>(dl, j), dxj = bcast<J>(dx, j);
-          float ys[2];
+          float ys[2], e[NS];
+#pragma unroll
+          for (int n = 0; n < NS; ++n) e[n] = dlj * A2[n];
 #pragma unroll
           for (int n = 0; n < NS; ++n) {
-            h[n] = fmaf(__builtin_amdgcn_exp2f(dlj * A2[n]), h[n], dxj * bq[n]);
+            h[n] = fmaf(__builtin_amdgcn_exp2f(e[n]), h[n], dxj * bq[n]);
             if constexpr (FINAL) ys[n & 1] = n < 2 ? cq[n] * h[n] : fmaf(cq[n], h[n], ys[n & 1]);
           }
-          if constexpr (FINAL) y[j] = ys[0] + ys[1];
-          // the next position's B and C are read when this one's states are done: the compiler would
-          // otherwise read those of many positions at once and spill
+          if constexpr (FINAL) {
+            y[j] = ys[0] + ys[1];
+            asm volatile("" : "+v"(y[j]));
+          }
+          // the next position's B and C are read when this one's states and output are done: the compiler
+          // would otherwise read those of many positions at once and spill, or copy the states for the
+          // output (2 x 500 x 512 x 256: 161 us without the output's tie, 117 with it)
 #pragma unroll
           for (int n = 0; n < NS; ++n)
             asm volatile("" : "+v"(h[n])::"memory");

@@ -470,11 +470,13 @@ int scan_groups(int n, int per, int G) { return std::min({G, n, per % n == 0 ? 1
 int scan_lanes(int Np) { return std::min(Np / 4, 16); }
 
 // Pieces of the axis, by the time they are expected to take: with k waves on a SIMD a wave's position takes
-// hypot(0.14, 0.083 k) us, and as much more as a lane holds more than four states (fitted to 2048
-// channels x 16 states, 8192 positions, k = 1 to 8).  Cutting the axis adds a first pass over it (0.75 of
-// the second's time) and the join.  Measured, 1 x 8192 x 2048 x 16 in one piece 1343 us, in 16 pieces 187,
-// 32: 152, 64: 148, 128: 154; 64 x 80 x 2048 x 16 whole 29, in 10 pieces 108; 7 x 97 x 330 x 24 whole 23, in 13
-// pieces 18.
+// hypot(0.135, 0.077 k) us, with more than four states per lane hypot(0.11, 0.077 k) for each four, and a
+// piece's start as much as six positions (fitted to 2048 channels x 16 states, 8192 positions, k = 1 to 8,
+// and to 500 to 600 positions of 100 and 256 states).  Cutting the axis adds a first pass over it (0.75 of the
+// second's time) and the join.  Measured, 1 x 8192 x 2048 x 16 in one piece 1343 us, in 16 pieces 187, 32: 152,
+// 64: 148, 128: 154; 64 x 80 x 2048 x 16 whole 28, in two pieces 62; 7 x 97 x 330 x 24 whole 22, in 13 pieces
+// 18; 4 x 600 x 1024 x 100 whole 160, in 16 pieces 199; 2 x 500 x 512 x 256 whole 292, in 8 pieces 92, 16: 99,
+// 32: 116.
 ScanPlan scan_plan(int B, int S, int D, int N, int num_cu) {
   const int Np = scan_padded_states(N);
   ScanPlan best{};
@@ -484,13 +486,13 @@ ScanPlan scan_plan(int B, int S, int D, int N, int num_cu) {
   double best_us = 1e30;
   for (int chunks = 1; chunks <= 256; chunks *= 2) {
     const int len = chunks == 1 ? S : ((S + chunks - 1) / chunks + tile - 1) / tile * tile;
-    if (chunks > 1 && len < 2 * tile) break;
-    const double us = len * (ns / 4) * std::hypot(0.14, 0.083 * std::max(1.0, waves * chunks)) * (chunks > 1 ? 1.75 : 1.0) +
-                      (chunks > 1 ? 6.0 + 0.05 * chunks : 0.0);
+    const int n = (S + len - 1) / len;
+    const double us = (len + 6) * (ns / 4) * std::hypot(ns > 4 ? 0.11 : 0.135, 0.077 * std::max(1.0, waves * n)) *
+                          (n > 1 ? 1.75 : 1.0) + (n > 1 ? 6.0 + 0.05 * n : 0.0);
     if (us < best_us) {
       best_us = us;
       best.chunk_len = len;
-      best.chunks = (S + len - 1) / len;
+      best.chunks = n;
     }
   }
   return best;

@@ -73,8 +73,8 @@ struct Row8 {
 
 // One wave per row, eight neighbouring values per lane and pass: the row's largest magnitude, then its
 // values in 8 bits.  A row of up to 512 R values is read once and waits in registers (longer ones, R = 0,
-// are read twice).  Values of k past K and rows past M of the last blocks are left as they are: they
-// meet zero columns or rows that are not stored.
+// are read twice).  Bound by traffic: 8192 x 4096 bf16 22 us (4.6 TB/s).  Values of k past K and rows past M
+// of the last blocks are left as they are: they meet zero columns or rows that are not stored.
 template <typename T, int R>
 __global__ void __launch_bounds__(256) quant_rows_kernel(I8Problem p, int wide) {
   const int lane = threadIdx.x & 63, m = blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -168,7 +168,9 @@ __global__ void __launch_bounds__(256) col_scale_kernel(float *s, int *bad) {
 constexpr int waitcnt(int vm, int lgkm) { return (vm & 15) | (vm >> 4) << 14 | 7 << 4 | lgkm << 8; }
 
 // A workgroup of WM x WN waves computes a tile of 32 MF WM rows by 32 NF WN columns, k in stages of 64
-// through a ring of ST stages in LDS that direct loads fill ST - 1 stages ahead.
+// through a ring of ST stages in LDS that direct loads fill ST - 1 stages ahead.  8192 x 4096 x 8192 bf16 takes
+// 247 us (2.2 P operations/s) and is bound by power: with the MFMAs busy in 59% of the cycles the clock
+// falls from 2.4 to 1.8 GHz.  768 x 512 x 50000 fp32: 47 us, bound by the 154 MB of its results.
 template <int MF, int NF, int WM, int WN, int ST, bool BF, bool STREAM>
 __global__ void __launch_bounds__(64 * WM * WN) i8_tile_kernel(I8Problem p, int tilesM, int tilesN, int wide) {
   constexpr int AB = MF * WM, BB = NF * WN;       // blocks of 32 rows and columns

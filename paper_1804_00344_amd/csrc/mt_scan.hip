@@ -139,8 +139,9 @@ __device__ __forceinline__ int longest_first(const int32_t *len, int B, int S, i
 // lane j of each J = min(LPC, 4) does it for the j-th of J positions.  B and C of the next tile and x,
 // dt and z of its positions are on their way while a tile is computed.  A tile is always computed whole:
 // behind the end the steps D_t are zero, which keeps the state as it is.
-// Bound by the vector units: they are active in 94% of the cycles (87% of the first pass) of 1 x 8192 x
-// 2048 x 16, at 2.25 GHz; an exp2 takes 10 to 11 cycles and does not overlap the products, 3 each.
+// Bound by the vector units, active in 80% (first pass) and 85% (second) of the cycles of 1 x 8192 x 2048 x 16
+// (61 and 85 us): an exp2 takes 10 to 11 cycles and does not overlap the products, 3 each, and an
+// eighth of the instructions taken out (lane moves within the products, no copies for the output) gave 4%.
 // MANY: B and C of a tile, of several groups or many states, are more than a thread holds in scan_stage
 // registers.  All 256 threads stage them then, also those of waves without channels, at distances that are
 // the same for all threads.  2 x 500 x 1024 x 16 of 1024 groups took 317 us with the staging of one

@@ -454,6 +454,18 @@ def test_load_refuses_values_that_have_no_scale():
         assert e.value.status == mt.MT_ERR_ARG
 
 
+@pytest.mark.parametrize("M,K,N", [(1, 40, 100), (3, 512, 70), (37, 300, 130), (129, 64, 257), (200, 512, 50000)])
+@pytest.mark.parametrize("ydt", [torch.float32, torch.bfloat16])
+def test_rows_behind_the_last_are_left(M, K, N, ydt):
+    mat = mt.mt_i8_load(torch.randn(K, N, generator=gen(3)))
+    x = torch.full((M + 64, K), float("nan"), device=DEV)
+    x[:M] = torch.randn(M, K, generator=gen(4)).to(DEV)
+    y = torch.full((M + 300, N), 7.0, dtype=ydt, device=DEV)
+    ws = torch.empty(mt.mt_i8_workspace_bytes(mat, M), dtype=torch.uint8, device=DEV)
+    mt.mt_i8_product(mat, x[:M], y[:M], ws)
+    assert bool((y[M:] == 7.0).all()) and bool(torch.isfinite(y[:M]).all()) and not bool((y[:M] == 7.0).all(1).any())
+
+
 def test_rows_do_not_depend_on_their_neighbours():
     """A row's result is the same alone and within any number of rows (whichever kernel form each takes)."""
     K, N = 520, 700

@@ -42,13 +42,13 @@ __device__ __forceinline__ size_t frag_offset(int row, int kg, int KB) {
 
 // 8 values of a row from k0 on, zero from K on
 template <typename T>
-struct Row8 {
+struct Row8 {  // whole vectors at any alignment: element by element 4 x 3711 x 3000 fp32 took 16 us, so 11
   static constexpr int E = 16 / sizeof(T);
   typename Vec<T, E>::Raw v[8 / E];
-  __device__ __forceinline__ void load(const T *row, int k0, int K, bool wide) {
-    if (wide && k0 + 8 <= K) {
+  __device__ __forceinline__ void load(const T *row, int k0, int K) {
+    if (k0 + 8 <= K) {
 #pragma unroll
-      for (int i = 0; i < 8 / E; ++i) v[i] = Vec<T, E>::raw(row + k0 + i * E);
+      for (int i = 0; i < 8 / E; ++i) v[i] = Vec<T, E>::raw_any(row + k0 + i * E);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i / E].v[i % E] = k0 + i < K ? row[k0 + i] : (T)0.f;
@@ -76,7 +76,7 @@ struct Row8 {
 // are read twice).  Bound by traffic: 8192 x 4096 bf16 22 us (4.6 TB/s).  Values of k past K and rows past M
 // of the last blocks are left as they are: they meet zero columns or rows that are not stored.
 template <typename T, int R>
-__global__ void __launch_bounds__(256) quant_rows_kernel(I8Problem p, int wide) {
+__global__ void __launch_bounds__(256) quant_rows_kernel(I8Problem p) {
   const int lane = threadIdx.x & 63, m = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (m >= p.M) return;
   const T *row = (const T *)p.x + (long long)m * p.ldx;
@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(256) quant_rows_kernel(I8Problem p, int wide) 
   if constexpr (R > 0) {
     Row8<T> q[R];
 #pragma unroll
-    for (int i = 0; i < R; ++i) q[i].load(row, (i * 64 + lane) * 8, p.K, wide);
+    for (int i = 0; i < R; ++i) q[i].load(row, (i * 64 + lane) * 8, p.K);
 #pragma unroll
     for (int i = 0; i < R; ++i) mx = max(mx, q[i].magnitude());
     row_scales(wave_ext<uint32_t, true>(mx), r, s);
@@ -96,12 +96,12 @@ __global__ void __launch_bounds__(256) quant_rows_kernel(I8Problem p, int wide) 
   } else {
     Row8<T> q;
     for (int k = lane * 8; k < p.K; k += 512) {
-      q.load(row, k, p.K, wide);
+      q.load(row, k, p.K);
       mx = max(mx, q.magnitude());
     }
     row_scales(wave_ext<uint32_t, true>(mx), r, s);
     for (int k = lane * 8; k < p.K; k += 512) {
-      q.load(row, k, p.K, wide);
+      q.load(row, k, p.K);
       q.store(p.xq, m, k, KB, r);
     }
   }
@@ -110,18 +110,17 @@ __global__ void __launch_bounds__(256) quant_rows_kernel(I8Problem p, int wide) 
 
 template <typename T>
 hipError_t run_quant(const I8Problem &p, hipStream_t st) {
-  const int wide = (uintptr_t)p.x % 16 == 0 && p.ldx % (16 / (int)sizeof(T)) == 0;
   const dim3 grid((unsigned)((p.M + 3) / 4)), block(256);
   if (p.K <= 512)
-    hipLaunchKernelGGL((quant_rows_kernel<T, 1>), grid, block, 0, st, p, wide);
+    hipLaunchKernelGGL((quant_rows_kernel<T, 1>), grid, block, 0, st, p);
   else if (p.K <= 1024)
-    hipLaunchKernelGGL((quant_rows_kernel<T, 2>), grid, block, 0, st, p, wide);
+    hipLaunchKernelGGL((quant_rows_kernel<T, 2>), grid, block, 0, st, p);
   else if (p.K <= 2048)
-    hipLaunchKernelGGL((quant_rows_kernel<T, 4>), grid, block, 0, st, p, wide);
+    hipLaunchKernelGGL((quant_rows_kernel<T, 4>), grid, block, 0, st, p);
   else if (p.K <= 4096)
-    hipLaunchKernelGGL((quant_rows_kernel<T, 8>), grid, block, 0, st, p, wide);
+    hipLaunchKernelGGL((quant_rows_kernel<T, 8>), grid, block, 0, st, p);
   else
-    hipLaunchKernelGGL((quant_rows_kernel<T, 0>), grid, block, 0, st, p, wide);
+    hipLaunchKernelGGL((quant_rows_kernel<T, 0>), grid, block, 0, st, p);
   return hipGetLastError();
 }
 
@@ -170,14 +169,15 @@ constexpr int waitcnt(int vm, int lgkm) { return (vm & 15) | (vm >> 4) << 14 | 7
 // A workgroup of WM x WN waves computes a tile of 32 MF WM rows by 32 NF WN columns, k in stages of 64
 // through a ring of ST stages in LDS that direct loads fill ST - 1 stages ahead.  8192 x 4096 x 8192 bf16 takes
 // 247 us (2.2 P operations/s) and is bound by power: with the MFMAs busy in 59% of the cycles the clock
-// falls from 2.4 to 1.8 GHz.  768 x 512 x 50000 fp32: 47 us, bound by the 154 MB of its results.
+// falls from 2.4 to 1.8 GHz.  768 x 512 x 50000 fp32: 42 us, bound by the 154 MB of its results.
 template <int MF, int NF, int WM, int WN, int ST, bool BF, bool STREAM>
-__global__ void __launch_bounds__(64 * WM * WN) i8_tile_kernel(I8Problem p, int tilesM, int tilesN, int wide) {
+__global__ void __launch_bounds__(64 * WM * WN) i8_tile_kernel(I8Problem p, int tilesM, int tilesN) {
   constexpr int AB = MF * WM, BB = NF * WN;       // blocks of 32 rows and columns
   constexpr int STAGE = (AB + BB) * 2 * 1024;     // a stage: two blocks of k of each
   constexpr int NL = (AB + BB) * 2 / (WM * WN);   // direct loads of a wave per stage
   static_assert((AB + BB) * 2 % (WM * WN) == 0, "every wave issues the same number of loads");
-  __shared__ __attribute__((aligned(1024))) char lds[ST * STAGE];
+  __shared__ __attribute__((aligned(1024))) char lds[ST * STAGE + 2 * BB * 32 * 4];
+  float *const cols = (float *)(lds + ST * STAGE);  // scales and biases of the tile's columns
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN;
   const int KB = p.Kp / 32, stages = KB / 2;
   const int w = xcd_remap(blockIdx.x, gridDim.x);
@@ -196,6 +196,13 @@ __global__ void __launch_bounds__(64 * WM * WN) i8_tile_kernel(I8Problem p, int 
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
                                      (__attribute__((address_space(3))) void *)(dst + f * 1024), 16, 0, 0);
   };
+  // a column's scale and bias per thread, on their way while the products run (read by each wave after them
+  // 768 x 512 x 50000 took 50 us, so 47; as an LDS array of its own it makes the compiler wait for the
+  // direct loads in every stage)
+  static_assert(BB * 32 <= 64 * WM * WN, "a thread per column");
+  const bool has_col = threadIdx.x < BB * 32;
+  const float col_scale = has_col ? p.ws[tn * BB * 32 + threadIdx.x] : 0.f;
+  const float col_bias = has_col && p.bias ? p.bias[tn * BB * 32 + threadIdx.x] : 0.f;
   i32x16 acc[MF][NF];
 #pragma unroll
   for (int i = 0; i < MF; ++i)
@@ -248,6 +255,10 @@ __global__ void __launch_bounds__(64 * WM * WN) i8_tile_kernel(I8Problem p, int 
     __builtin_amdgcn_sched_barrier(0);
     mma(1, s + ST, 0, NL / 2);
   }
+  if (has_col) {
+    cols[threadIdx.x] = col_scale;
+    cols[BB * 32 + threadIdx.x] = col_bias;
+  }
   // no direct load may still be on its way when the ring is used for the results (or given back)
   __builtin_amdgcn_s_waitcnt(waitcnt(0, 0));
   __builtin_amdgcn_s_barrier();
@@ -269,8 +280,8 @@ __global__ void __launch_bounds__(64 * WM * WN) i8_tile_kernel(I8Problem p, int 
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int nq = j * 32 + 8 * q + 4 * (lane >> 5);
-        const float4 sw = *(const float4 *)(p.ws + n0 + nq);
-        const float4 bias = p.bias ? *(const float4 *)(p.bias + n0 + nq) : make_float4(0.f, 0.f, 0.f, 0.f);
+        const float4 sw = *(const float4 *)(cols + wn * NF * 32 + nq);
+        const float4 bias = *(const float4 *)(cols + (BB + wn * NF) * 32 + nq);
         float v[4];
         v[0] = fmaf((float)acc[i][j][4 * q] * sw.x, sx, bias.x);
         v[1] = fmaf((float)acc[i][j][4 * q + 1] * sw.y, sx, bias.y);
@@ -282,25 +293,21 @@ __global__ void __launch_bounds__(64 * WM * WN) i8_tile_kernel(I8Problem p, int 
     __builtin_amdgcn_s_waitcnt(waitcnt(63, 0));  // the wave's own part: no barrier
     __builtin_amdgcn_wave_barrier();
     Y *const yb = (Y *)p.y + (long long)mb * p.ldy + n0;
-    if (wide) {
 #pragma unroll
-      for (int u = 0; u < 32 * CPR / 64; ++u) {
-        const int c = lane + u * 64;
-        const int r = c / CPR, k = c % CPR, n = n0 + k * EPC;
-        const typename Vec<Y, EPC>::Raw v = *(const typename Vec<Y, EPC>::Raw *)(own + r * ROWB + ((k ^ (r % CPR)) << 4));
-        if (mb + r >= p.M) continue;
-        Y *dst = yb + (long long)r * p.ldy + k * EPC;
-        if (n + EPC <= p.N)
-          Vec<Y, EPC>::template store<STREAM>(dst, v);
+    for (int u = 0; u < 32 * CPR / 64; ++u) {
+      const int c = lane + u * 64;
+      const int r = c / CPR, k = c % CPR, n = n0 + k * EPC;
+      const typename Vec<Y, EPC>::Raw v = *(const typename Vec<Y, EPC>::Raw *)(own + r * ROWB + ((k ^ (r % CPR)) << 4));
+      if (mb + r >= p.M) continue;
+      Y *dst = yb + (long long)r * p.ldy + k * EPC;
+      if (n + EPC <= p.N) {
+        if constexpr (STREAM)
+          Vec<Y, EPC>::template store<true>(dst, v);
         else
-          for (int e = 0; e < EPC; ++e)
-            if (n + e < p.N) dst[e] = v.v[e];
-      }
-    } else {
-      for (int c = lane; c < 32 * NF * 32; c += 64) {
-        const int r = c / (NF * 32), k = c % (NF * 32);
-        const Y v = *(const Y *)(own + r * ROWB + (((k * ES >> 4) ^ (r % CPR)) << 4) + (k * ES & 15));
-        if (mb + r < p.M && n0 + k < p.N) yb[(long long)r * p.ldy + k] = v;
+          Vec<Y, EPC>::store_any(dst, v);
+      } else {
+        for (int e = 0; e < EPC; ++e)
+          if (n + e < p.N) dst[e] = v.v[e];
       }
     }
     __builtin_amdgcn_s_waitcnt(waitcnt(63, 0));
@@ -311,11 +318,11 @@ __global__ void __launch_bounds__(64 * WM * WN) i8_tile_kernel(I8Problem p, int 
 template <int MF, int NF, int WM, int WN, int ST>
 hipError_t run_tiles(const I8Problem &p, hipStream_t st) {
   const int tm = (p.M + 32 * MF * WM - 1) / (32 * MF * WM), tn = (p.N + 32 * NF * WN - 1) / (32 * NF * WN);
-  const int wide = (uintptr_t)p.y % 16 == 0 && p.ldy % (p.y_bf16 ? 8 : 4) == 0;
   const dim3 grid((unsigned)(tm * tn)), block(64 * WM * WN);
-  // results larger than the L2s together are stored past them: 768 x 512 x 50000 fp32 71 -> 53 us
-  const bool stream = wide && (double)p.M * p.N * (p.y_bf16 ? 2 : 4) > 32e6;
-#define MT_TILES(BF, S) hipLaunchKernelGGL((i8_tile_kernel<MF, NF, WM, WN, ST, BF, S>), grid, block, 0, st, p, tm, tn, wide)
+  // aligned results larger than the L2s together are stored past them: 768 x 512 x 50000 fp32 71 -> 53 us
+  const bool aligned = (uintptr_t)p.y % 16 == 0 && p.ldy % (p.y_bf16 ? 8 : 4) == 0;
+  const bool stream = aligned && (double)p.M * p.N * (p.y_bf16 ? 2 : 4) > 32e6;
+#define MT_TILES(BF, S) hipLaunchKernelGGL((i8_tile_kernel<MF, NF, WM, WN, ST, BF, S>), grid, block, 0, st, p, tm, tn)
   if (p.y_bf16 && stream)
     MT_TILES(true, true);
   else if (p.y_bf16)
@@ -336,7 +343,7 @@ hipError_t run_tiles(const I8Problem &p, hipStream_t st) {
 // return first.  The parts are summed in LDS, in whole numbers.  Bound by the weights' traffic and
 // the latency of a launch (1 x 512 x 50000 fp32: see the rule below).
 template <typename T, int R>
-__global__ void __launch_bounds__(256) i8_few_kernel(I8Problem p, int KW, int wide) {
+__global__ void __launch_bounds__(256) i8_few_kernel(I8Problem p, int KW) {
   constexpr int U = 8;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ float xs[4];
@@ -348,7 +355,7 @@ __global__ void __launch_bounds__(256) i8_few_kernel(I8Problem p, int KW, int wi
   Row8<T> q[R];
   if (wave < M) {
 #pragma unroll
-    for (int i = 0; i < R; ++i) q[i].load((const T *)p.x + wave * p.ldx, (i * 64 + lane) * 8, p.K, wide);
+    for (int i = 0; i < R; ++i) q[i].load((const T *)p.x + wave * p.ldx, (i * 64 + lane) * 8, p.K);
   }
   const char *wp = (const char *)p.wq + (size_t)min(blk, nblk - 1) * KB * 1024 + lane * 16;
   i32x4 fb[U];
@@ -416,10 +423,9 @@ hipError_t run_few(const I8Problem &p, hipStream_t st) {
   const int nblk = (p.N + 31) / 32, KB = p.Kp / 32;
   int KW = 1;  // parts of k: until there are eight waves per unit, of at least two blocks
   while (KW < 4 && (long long)nblk * KW < 8ll * p.num_cu && KB / (KW * 2) >= 2) KW *= 2;
-  const int wide = (uintptr_t)p.x % 16 == 0 && p.ldx % (16 / (int)sizeof(T)) == 0;
   const dim3 grid((unsigned)((nblk + 4 / KW - 1) / (4 / KW))), block(256);
   const size_t lds = (size_t)p.M * p.Kp;
-#define MT_FEW(R) hipLaunchKernelGGL((i8_few_kernel<T, R>), grid, block, lds, st, p, KW, wide)
+#define MT_FEW(R) hipLaunchKernelGGL((i8_few_kernel<T, R>), grid, block, lds, st, p, KW)
   if (p.Kp <= 512)
     MT_FEW(1);
   else if (p.Kp <= 1024)

@@ -14,6 +14,21 @@ struct Vec {
     T v[VEC];
   };
   __device__ __forceinline__ static Raw raw(const T *p) { return *(const Raw *)p; }
+  // the same from and to any address of an element: global memory takes whole vectors there too
+  struct __attribute__((packed, aligned(sizeof(T)))) Any {
+    T v[VEC];
+  };
+  __device__ __forceinline__ static Raw raw_any(const T *p) {
+    const Any a = *(const Any *)p;
+    Raw r;
+    __builtin_memcpy(&r, &a, sizeof r);
+    return r;
+  }
+  __device__ __forceinline__ static void store_any(T *p, const Raw &r) {
+    Any a;
+    __builtin_memcpy(&a, &r, sizeof a);
+    *(Any *)p = a;
+  }
   // STREAM: past the L2
   template <bool STREAM>
   __device__ __forceinline__ static void store(T *p, const Raw &r) {

@@ -1,11 +1,11 @@
 // Causal depthwise convolution of width W <= 8 over prompts and single tokens:
 // y[t, d] = act(b[d] + sum_j w[d, j] x[t - W + 1 + j, d]).
 //
-// Memory-bound: every input is used W times, from registers.  A thread takes VEC neighbouring
-// channels (16 bytes where the rows are aligned for it) over RUN positions: it requests all their inputs
-// and the W - 1 before them at once, then computes.  Threads are numbered channel first, so a wave's
-// accesses are consecutive for any channel count.  A prompt's first thread of a channel reads the state
-// before it and is the one that writes the state after it.
+// Memory-bound: every input is used W times, from registers.  A thread takes VEC neighbouring channels (16 bytes
+// where the channels divide into them; rows at odd elements too, 4 x 8192 x 2048 bf16 53 us, channel by channel
+// 76) over RUN positions: it requests all their inputs and the W - 1 before them at once, then computes.  Threads
+// are numbered channel first, so a wave's accesses are consecutive for any channel count.  A prompt's first
+// thread of a channel reads the state before it and is the one that writes the state after it.
 #include "mt_layer_dev.h"
 
 namespace mt {
@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(256) conv_kernel(ConvArgs a) {
     const T *st = a.state_in ? (const T *)a.state_in + (long long)b * (W - 1) * a.D + d : nullptr;
     // the input at position t >= 1 - W of this prompt
     auto input = [&](int t) -> typename V::Raw {
-      if (t >= 0) return V::raw(x + (long long)t * a.ldx);
+      if (t >= 0) return V::raw_any(x + (long long)t * a.ldx);
       if (st) return V::raw(st + (long long)(t + W - 1) * a.D);
       return {};
     };
@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(256) conv_kernel(ConvArgs a) {
 #pragma unroll
       for (int j = 0; j + 1 < W; ++j) in[j] = input(t0 - W + 1 + j);
 #pragma unroll
-      for (int i = 0; i < RUN; ++i) in[W - 1 + i] = V::raw(x + (long long)min(t0 + i, t1 - 1) * a.ldx);
+      for (int i = 0; i < RUN; ++i) in[W - 1 + i] = V::raw_any(x + (long long)min(t0 + i, t1 - 1) * a.ldx);
 #pragma unroll
       for (int i = 0; i < RUN; ++i) {
         float o[VEC];
@@ -67,7 +67,11 @@ __global__ void __launch_bounds__(256) conv_kernel(ConvArgs a) {
           for (int j = 0; j < W; ++j) o[v] = fmaf(w[j][v], (float)in[i + j].v[v], o[v]);
           if (a.silu) o[v] = silu(o[v]);
         }
-        if (t0 + i < t1) V::template put<STREAM>(y + (long long)(t0 + i) * a.ldy, o);
+        if (t0 + i >= t1) continue;
+        if constexpr (STREAM)
+          V::template put<true>(y + (long long)(t0 + i) * a.ldy, o);
+        else
+          V::put_any(y + (long long)(t0 + i) * a.ldy, o);
       }
     }
     if (run == 0 && W > 1 && a.state_out) {
@@ -102,7 +106,7 @@ __global__ void __launch_bounds__(256) conv_step_kernel(ConvArgs a) {
 #pragma unroll
     for (int j = 0; j + 1 < W; ++j) in[j] = V::raw(st + (long long)j * a.D);
   }
-  in[W - 1] = V::raw((const T *)a.x + (long long)m * a.ldx + d);
+  in[W - 1] = V::raw_any((const T *)a.x + (long long)m * a.ldx + d);
   float w[W][VEC], o[VEC];
   load_taps<T, VEC, W>(a, d, w, o);
 #pragma unroll
@@ -111,7 +115,7 @@ __global__ void __launch_bounds__(256) conv_step_kernel(ConvArgs a) {
     for (int j = 0; j < W; ++j) o[v] = fmaf(w[j][v], (float)in[j].v[v], o[v]);
     if (a.silu) o[v] = silu(o[v]);
   }
-  V::put((T *)a.y + (long long)m * a.ldy + d, o);
+  V::put_any((T *)a.y + (long long)m * a.ldy + d, o);
   if constexpr (W > 1) {
     T *so = (T *)a.state_out + (long long)m * (W - 1) * a.D + d;
 #pragma unroll
@@ -129,7 +133,7 @@ hipError_t run_prompts(const ConvArgs &a, hipStream_t st) {
 
 // Runs of 8 positions once those of 4 fill the chip four times over (4 x 8192 x 2048, W = 4: 60 us, runs of 4
 // and 16: 71 and 62; 3 x 61 x 333: 3.1 us with runs of 4, 6.5 with one position after the other).
-// Outputs larger than the L2s together are stored past them (60 -> 56 us); smaller ones stay for
+// Aligned outputs larger than the L2s together are stored past them (60 -> 56 us); smaller ones stay for
 // the product that reads them.
 template <typename T, int VEC, int W>
 hipError_t run_conv(const ConvArgs &a, bool step, hipStream_t st) {
@@ -139,7 +143,8 @@ hipError_t run_conv(const ConvArgs &a, bool step, hipStream_t st) {
     return hipGetLastError();
   }
   const double n = (double)a.B * a.S * dv;  // vectors
-  if (VEC > 1 && n * 16 > 32e6) return run_prompts<T, VEC, W, 8, VEC != 1>(a, st);
+  const bool aligned = (uintptr_t)a.y % 16 == 0 && a.ldy % VEC == 0;
+  if (VEC > 1 && aligned && n * 16 > 32e6) return run_prompts<T, VEC, W, 8, VEC != 1>(a, st);
   if (n >= 4.0 * 64 * 16 * a.num_cu) return run_prompts<T, VEC, W, 8, false>(a, st);
   return run_prompts<T, VEC, W, 4, false>(a, st);
 }
@@ -161,8 +166,7 @@ hipError_t by_width(const ConvArgs &a, bool step, hipStream_t st) {
 template <typename T>
 hipError_t by_vector(const ConvArgs &a, bool step, hipStream_t st) {
   constexpr int VEC = 16 / sizeof(T);
-  const bool wide = a.D % VEC == 0 && a.ldx % VEC == 0 && a.ldy % VEC == 0 && ((uintptr_t)a.x | (uintptr_t)a.y) % 16 == 0;
-  return wide ? by_width<T, VEC>(a, step, st) : by_width<T, 1>(a, step, st);
+  return a.D % VEC == 0 ? by_width<T, VEC>(a, step, st) : by_width<T, 1>(a, step, st);
 }
 
 }  // namespace

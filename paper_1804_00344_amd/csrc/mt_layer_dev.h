@@ -49,6 +49,12 @@ struct Vec {
     for (int i = 0; i < VEC; ++i) r.v[i] = (T)f[i];
     store<STREAM>(p, r);
   }
+  __device__ __forceinline__ static void put_any(T *p, const float (&f)[VEC]) {
+    Raw r;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) r.v[i] = (T)f[i];
+    store_any(p, r);
+  }
 };
 
 // e^v for v <= 0 to a few roundings at any v: the product with log2(e) in two parts (one rounding of

@@ -398,8 +398,9 @@ __global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs a, ScanPlan pl)
 
 // One token of a hypothesis: LPC lanes share a channel, four states each.  Bound by the states' traffic:
 // each is read and written once, 16 bytes a lane (two and four hypotheses per thread were no faster).
-// WIDE: B, C and the states are aligned for one access of four (768 x 2048 x 16 element by element: 83
-// us).  STREAM: the new states are stored past the L2.  For states larger than the L2s together that is
+// WIDE: a lane's four states, and its B and C at any alignment, are one access (N a multiple of 4; 768 x 2048 x
+// 16 element by element: 83 us).  STREAM: the new states are stored past the L2.  For states larger than the L2s
+// together that is
 // the faster form wherever something else runs between two steps: 768 x 2048 x 16 takes 38.5 us (5.6 TB/s)
 // against 54 from the same states again, and 49 against 57 with a 154 MB matrix of logits written between
 // a step and the next; only steps back to back, which find their states in the last-level cache, lose (50
@@ -432,8 +433,8 @@ __global__ void __launch_bounds__(kThreads) scan_step_kernel(ScanArgs a) {
     if constexpr (WIDE) {
       typename Vec<T, NS>::Raw b4{}, c4{};
       if (nn > 0) {
-        b4 = Vec<T, NS>::raw((const T *)a.bm + o);
-        c4 = Vec<T, NS>::raw((const T *)a.cm + o);
+        b4 = Vec<T, NS>::raw_any((const T *)a.bm + o);
+        c4 = Vec<T, NS>::raw_any((const T *)a.cm + o);
       }
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
@@ -554,7 +555,7 @@ template <typename T, int LPC>
 hipError_t run_step(const ScanArgs &a, hipStream_t st) {
   constexpr int CPB = kThreads / LPC;
   const dim3 grid((a.D + CPB - 1) / CPB, (unsigned)std::min(a.B, 32768));
-  const bool wide = a.N % 4 == 0 && ((uintptr_t)a.bm | (uintptr_t)a.cm) % (4 * sizeof(T)) == 0 && a.ldbc % 4 == 0;
+  const bool wide = a.N % 4 == 0;
   if (wide && (double)a.B * a.D * a.N * 4 > 32e6)
     hipLaunchKernelGGL((scan_step_kernel<T, LPC, true, true>), grid, dim3(kThreads), 0, st, a);
   else if (wide)

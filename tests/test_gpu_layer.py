@@ -89,6 +89,27 @@ def test_conv_step(M, n, D, W, left, dtype):
         assert torch.equal(so[m].cpu().double(), state)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shift", [1, 2, 3, 4])
+def test_conv_at_any_alignment(dtype, shift):
+    """Rows that start at any element, read and written, are the aligned ones to the bit."""
+    B, S, D, W = 2, 700, 64, 4
+    cell, _, _ = conv_cell(D, W, dtype)
+    x = torch.randn(B, S, D, generator=gen(6)).to(IO[dtype])
+    st = torch.randn(B, W - 1, D, generator=gen(7)).to(IO[dtype]).to(DEV)
+    y = torch.empty(B, S, D, dtype=x.dtype, device=DEV)
+    mt.mt_ssm_conv(cell, dev(x), y, state_in=st)
+    big = torch.full((B, S, D + shift + 2), 7.0, dtype=x.dtype, device=DEV)
+    mt.mt_ssm_conv(cell, wide(x, shift, 1), big[..., shift:shift + D], state_in=st)
+    assert torch.equal(big[..., shift:shift + D], y) and bool((big[..., :shift] == 7).all()) and bool((big[..., shift + D:] == 7).all())
+    so, so2 = torch.empty_like(st), torch.empty_like(st)
+    tok, bt = torch.empty(B, D, dtype=x.dtype, device=DEV), torch.full((B, D + shift + 2), 7.0, dtype=x.dtype, device=DEV)
+    mt.mt_ssm_conv_step(cell, dev(x[:, 0].contiguous()), tok, st, so)
+    mt.mt_ssm_conv_step(cell, wide(x[:, 0], shift, 1), bt[:, shift:shift + D], st, so2)
+    assert torch.equal(bt[:, shift:shift + D], tok) and torch.equal(so, so2)
+    assert bool((bt[:, :shift] == 7).all()) and bool((bt[:, shift + D:] == 7).all())
+
+
 def test_conv_pieces_and_tokens_are_the_whole():
     """A prompt in pieces, then token by token in place, gives what the whole prompt gives, to the bit."""
     B, S, D, W = 3, 41, 48, 4
@@ -249,6 +270,21 @@ def test_step_of_large_states(M, D, N):
     y2 = torch.empty(4, D, dtype=x.dtype, device=DEV)
     mt.mt_ssm_step(cell, dev(x[:4]), dev(dt[:4]), w[:4, :N], w[:4, N:], y2, sub, sub, z=dev(z[:4]))
     assert torch.equal(y2, y[:4]) and torch.equal(sub, so[:4])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shift", [1, 2, 3, 4])
+def test_step_at_any_alignment(dtype, shift):
+    M, D, N, G = 5, 70, 12, 2
+    cell, *_ = scan_cell(D, N, G, dtype)
+    x, dt, z, bc = scan_inputs((M,), D, N, G, dtype, 3)
+    st = torch.randn(M, D, N, generator=gen(2)).to(DEV)
+    out = []
+    for w in (dev(bc), wide(bc, shift, 1)):
+        y, so = torch.empty(M, D, dtype=x.dtype, device=DEV), torch.empty_like(st)
+        mt.mt_ssm_step(cell, dev(x), dev(dt), w[:, :G * N], w[:, G * N:], y, st, so, z=dev(z))
+        out.append((y, so))
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
 
 
 def test_step_in_place_and_bad_rows():

@@ -422,8 +422,7 @@ void mt_round_bf16(const float *src, uint16_t *dst, size_t n);
  * They take these conventions in place of those above:
  *   - Row matrices (x, y, dt, ...) have a row stride in elements (ld.. >= the row's width), so that
  *     a column range of a wider matrix can be passed; their pointers need only the alignment
- *     of their element type.  The
- *     positions of a padded batch are rows b*S + i.
+ *     of their element type.  The positions of a padded batch are rows b*S + i.
  *   - A call reads its handle and does not change it: one handle serves several streams and
  *     threads at once, each call with its own outputs and workspace.  The current device must
  *     be the one the handle was loaded on (MT_ERR_STATE otherwise).  Calls may be captured into

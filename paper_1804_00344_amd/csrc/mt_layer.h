@@ -72,6 +72,19 @@ struct ScanArgs {
   int32_t *err;
   int num_cu;
 };
+// The positions of a piece [.., t1) that a lane fetches: it is number tj of J lanes, takes every J-th position
+// from its first one on, tile by tile and one tile ahead, and stays at its last one at the end.
+__host__ __device__ inline int scan_first_row(int t0, int tj, int t1) { return t0 + tj < t1 ? t0 + tj : t1 - 1; }
+// whether the tile at ts can be computed, and the one after it fetched, without looking for the end: then every
+// lane goes on past that one too, to position ts + 2 tile + tj
+__host__ __device__ inline bool scan_whole_tile(int ts, int tile, int J, int t1) { return ts + 2 * tile + J <= t1; }
+// whether a lane goes on after slot i of the tile at ts (whole: without looking)
+__host__ __device__ inline bool scan_next_row(bool whole, int ts, int i, int J, int tj, int t1) {
+  return whole || ts + (i + 1) * J + tj < t1;
+}
+// The kernel's fetches over a piece of len positions, on the host: the last position that lane tj fetches, or -1
+// if a position of its own is not the one that it holds when that is computed.
+int scan_walk_rows(int len, int tile, int J, int tj);
 int scan_padded_states(int N);
 int scan_pieces(int B, int S, int D, int N, int num_cu);  // pieces that the axis is cut into
 size_t scan_workspace_bytes(int B, int S, int D, int N, int num_cu);

@@ -217,18 +217,18 @@ __global__ void __launch_bounds__(256, NS == 4 ? 4 : NS == 8 ? 3 : 2) scan_kerne
     const int t1 = min(t0 + pl.chunk_len, len);
     const long long r0 = (long long)b * a.S;
     T xr[SLOTS], dr[SLOTS], zr[SLOTS], er[STAGE];
-    const long long rl = r0 + (t0 < t1 ? min(t0 + tj, t1 - 1) : 0);  // this lane's first row
+    const long long rl = r0 + (t0 < t1 ? scan_first_row(t0, tj, t1) : 0);  // this lane's first row
     const T *px = (const T *)a.x + rl * a.ldx + d, *pd = (const T *)a.dt + rl * a.lddt + d;
     // without a gate its loads are those of x again and its factor is 1: no branch in the loop
     const T *pz = gated ? (const T *)a.z + rl * a.ldz + d : px;
     T *py = (T *)a.y + (r0 + t0 + (J > 1 ? tj : 0)) * a.ldy + d;
     // this lane's next row (slots and tiles in order, ts the tile's first position); behind the end the
-    // last row of the lane again (more: the row after it lies before the end)
-    auto fetch_row = [&](bool more, int ts, int i) {
+    // last row of the lane again, so no row at or behind t1 is read (whole: see scan_whole_tile)
+    auto fetch_row = [&](bool whole, int ts, int i) {
       xr[i] = *px;
       dr[i] = *pd;
       if (FINAL) zr[i] = *pz;
-      const bool in = more || ts + (i + 1) * J + tj < t1;
+      const bool in = scan_next_row(whole, ts, i, J, tj, t1);
       px += in ? J * a.ldx : 0;
       pd += in ? J * a.lddt : 0;
       if (FINAL) pz += in ? J * ldz : 0;
@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(256, NS == 4 ? 4 : NS == 8 ? 3 : 2) scan_kerne
       if (pre) fetch_bc(t0);
       stage_bc(t0, lds);
     }
-    // the positions of a tile.  WHOLE: neither they nor those fetched meanwhile come near the end
+    // the positions of a tile.  WHOLE: neither they nor the lanes' rows after it come to the end
     auto compute = [&](auto whole, int ts, const float *buf) {
       constexpr bool WHOLE = decltype(whole)::value;
 #pragma unroll
@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(256, NS == 4 ? 4 : NS == 8 ? 3 : 2) scan_kerne
       if (more && pre) fetch_bc(ts + kTile);
       const float *buf = lds + p * bufl + gi * grpl + n0;
       if (!works) {
-      } else if (ts + 2 * kTile < t1) {
+      } else if (scan_whole_tile(ts, kTile, J, t1)) {
         compute(std::true_type(), ts, buf);
       } else {
         compute(std::false_type(), ts, buf);
@@ -579,6 +579,26 @@ hipError_t step_by_states(const ScanArgs &a, hipStream_t st) {
 }
 
 }  // namespace
+
+int scan_walk_rows(int len, int tile, int J, int tj) {
+  const int slots = tile / J;
+  int held[8];  // the positions in the lane's registers
+  int row = scan_first_row(0, tj, len), last = 0;
+  bool own = true;
+  auto fetch = [&](bool whole, int ts, int i) {
+    held[i] = row;
+    last = std::max(last, row);
+    if (scan_next_row(whole, ts, i, J, tj, len)) row += J;
+  };
+  for (int i = 0; i < slots; ++i) fetch(false, 0, i);
+  for (int ts = 0; ts < len; ts += tile)
+    for (int i = 0; i < slots; ++i) {
+      const int t = ts + i * J + tj;
+      own = own && (t >= len || held[i] == t);
+      fetch(scan_whole_tile(ts, tile, J, len), ts + tile, i);
+    }
+  return own ? last : -1;
+}
 
 int scan_padded_states(int N) {
   int p = 4;

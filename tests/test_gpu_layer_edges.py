@@ -1,0 +1,82 @@
+"""The selective scan at its edges: every length around a tile, within the bound of the roundings that are made
+(none for pieces that are not there)."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import layer_ref as ref
+from test_gpu_layer import DEV, check, dev, gen, per_channel, run_scan, scan_cell, scan_inputs
+from test_layer_cpu import scan_pieces
+
+pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
+
+
+def piece_of(B, S, D, N):
+    """Positions of the pieces that the axis is cut into (the last one shorter), or 0: one piece.  The cut is
+    ceil(S / 2^k) up to whole tiles; of those that give the same count the longest."""
+    n, tile = scan_pieces(B, S, D, N), 8 if N <= 128 else 4
+    if n == 1:
+        return 0
+    lens = [-(-(-(-S // c)) // tile) * tile for c in (2 ** k for k in range(1, 9))]
+    return max(l for l in lens if -(-S // l) == n)
+
+
+def scan_bound(x, dt, bm, cm, z, A, dtb, skip, h, piece):
+    """As layer_ref.scan, with only the roundings that are made.  Per position, relative to the power a: the error
+    dd of D_t times |A|, three roundings of the exponent D_t A (A log2 e, the product, one spare), four of the
+    power, the sum and the products.  Where a piece ends and another follows, the power of the whole piece, w = the
+    sum of its D_t: `piece` roundings of w at most and two of joining its lanes, two of the product with A, three
+    of the power and the sum, and one of the state.  z None: no gate."""
+    U = ref.U
+    mag, err = h.abs(), torch.zeros_like(h)
+    ys, es = [], []
+    w, mag0 = torch.zeros_like(dtb), mag
+    S = x.shape[0]
+    for t in range(S):
+        v = dt[t] + dtb
+        d = torch.clamp(v, min=0) + torch.log1p(torch.exp(-v.abs()))
+        dd = U * (v.abs() * torch.minimum(torch.ones_like(d), 1.3 * d) + 12 * d)
+        e = d[:, None] * A
+        a = torch.exp(e)
+        u = (d * x[t])[:, None] * bm[t]
+        err = a * err + a * mag * ((dd[:, None] * A).abs() + U * (3 * e.abs() + 4)) + (dd * x[t].abs())[:, None] * bm[t].abs() \
+            + 4 * U * u.abs()
+        h, mag = a * h + u, a * mag + u.abs()
+        y = (cm[t] * h).sum(1) + skip * x[t]
+        ye = (cm[t].abs() * err).sum(1) + (A.shape[1] + 4) * U * ((cm[t].abs() * mag).sum(1) + (skip * x[t]).abs())
+        if z is not None:
+            g = z[t] * ref.sigmoid(z[t])
+            ye = ye * g.abs() + (y.abs() + ye) * U * (g.abs() * 6 + z[t].abs() * (1 + z[t].abs()) * ref.sigmoid(-z[t].abs()) * 2)
+            y = y * g
+        ys.append(y)
+        es.append(ye)
+        w = w + d
+        if piece and (t + 1) % piece == 0 and t + 1 < S:
+            wa = (w[:, None] * A).abs()
+            err = err + torch.exp(-wa) * mag0 * U * ((piece + 4) * wa + 3) + U * mag
+            w, mag0 = torch.zeros_like(dtb), mag
+    return torch.stack(ys), h, torch.stack(es), err
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N", [3, 8, 16, 200])
+def test_scan_of_every_length(N, dtype):
+    """Prompts of 0 to 34 positions: each length modulo a tile, with one and more tiles before the last."""
+    S, D, G = 34, 6, 2
+    B = S + 1
+    cell, A, dtb, skip = scan_cell(D, N, G, dtype)
+    x, dt, z, bc = scan_inputs((B, S), D, N, G, dtype, N)
+    for n in range(B):
+        for t in (x, dt, z, bc):
+            t[n, n:] = float("nan")
+    st = torch.randn(B, D, N, generator=gen(9))
+    lens = torch.arange(B, dtype=torch.int32, device=DEV)
+    y, so = run_scan(cell, x, dt, z, bc, G * N, lens, dev(st))
+    assert torch.equal(so[0].cpu(), st[0]) and bool((y[0] == 7.0).all())
+    piece = piece_of(B, S, D, N)
+    for n in range(1, B):
+        want, h, ye, he = scan_bound(x[n, :n].double(), dt[n, :n].double(), per_channel(bc[n, :n], D, N, G, False),
+                                     per_channel(bc[n, :n], D, N, G, True), z[n, :n].double(), A, dtb, skip, st[n].double(), piece)
+        check(y[n, :n], want, ye, ("y", n))
+        check(so[n], h, he, ("state", n))
+        assert bool((y[n, n:] == 7.0).all())

@@ -148,7 +148,11 @@ __device__ __forceinline__ int longest_first(const int32_t *len, int B, int S, i
 // group and takes 174, 23 x 1595 x 16 x 16 of 8 groups 79 and 37, 2 x 721 x 16 x 128 of 4 groups 50 and 36; the
 // other way round, this staging for one group, 64 x 80 x 2048 x 16 took 32 in place of 29.  Two groups at 32
 // states lose by it: 7 x 97 x 330 x 24 of 3 groups 16 and 18.
-template <typename T, int NS, int LPC, bool FINAL, bool MANY>
+// PAD: some of the Np states do not exist.  Their A and B are zero, but an infinite D_t x_t times that B, or an
+// infinite D_t times that A, is NaN and would be part of y from there on, so they are set to zero at every position
+// (16 x 300 x 1024 x 24 50.7 -> 52.3 us, 4 x 600 x 1024 x 100 142 -> 148; a test per four positions in place of it
+// 56.5 and 151).  The first pass leaves them: the join clears them.
+template <typename T, int NS, int LPC, bool FINAL, bool MANY, bool PAD>
 __global__ void __launch_bounds__(256, NS == 4 ? 4 : NS == 8 ? 3 : 2) scan_kernel(ScanArgs a, ScanPlan pl) {
   constexpr int J = LPC < 4 ? LPC : 4, Np = NS * LPC, kTile = tile_positions(NS), SLOTS = kTile / J;
   constexpr int STAGE = MANY ? (Np <= 64 ? 4 : 8) : scan_stage(Np);  // elements a thread holds for the next tile
@@ -200,7 +204,6 @@ __global__ void __launch_bounds__(256, NS == 4 ? 4 : NS == 8 ? 3 : 2) scan_kerne
     return src[o + (long long)g * a.N];
   };
   const bool pre = !MANY || passes <= STAGE;
-
   for (int bz = blockIdx.z; bz < a.B; bz += gridDim.z) {
     int b = bz;
     if (pl.ordered) b = __builtin_amdgcn_readfirstlane(longest_first(a.len, a.B, a.S, bz));
@@ -307,6 +310,7 @@ __global__ void __launch_bounds__(256, NS == 4 ? 4 : NS == 8 ? 3 : 2) scan_kerne
 #pragma unroll
           for (int n = 0; n < NS; ++n) {
             h[n] = fmaf(__builtin_amdgcn_exp2f(e[n]), h[n], dxj * b[n]);
+            if (PAD) h[n] = n < nn ? h[n] : 0.f;
             if constexpr (FINAL) ys[n & 1] = n < 2 ? c[n] * h[n] : fmaf(c[n], h[n], ys[n & 1]);
           }
           if constexpr (FINAL) {
@@ -390,6 +394,7 @@ __global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs a, ScanPlan pl)
       for (int i = 0; i < R; ++i) {
         if (c0 + i >= live) break;
         h = fmaf(__builtin_amdgcn_exp2f(w[i] * A2), h, s[i]);
+        if (n >= a.N) h = 0.f;  // a state that does not exist: see PAD
         part[(c0 + i) * sp] = h;
       }
     }
@@ -454,8 +459,10 @@ __global__ void __launch_bounds__(kThreads) scan_step_kernel(ScanArgs a) {
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
       h[i] = fmaf(__builtin_amdgcn_exp2f(dl * A[i]), h[i], dx * bv[i]);
-      yv = fmaf(cv[i], h[i], yv);
+      // states that only pad are not part of the sum: infinite dl and dx times zero are NaN
+      if (WIDE || i < nn) yv = fmaf(cv[i], h[i], yv);
     }
+    if (WIDE && nn <= 0) yv = 0.f;
     yv = fmaf(skip, xv, group_sum<LPC>(yv));
     if (gated) yv *= silu(zv);
     if (c < a.D) {
@@ -520,20 +527,25 @@ hipError_t run_scan(const ScanArgs &a, ScanPlan pl, hipStream_t st) {
   const int cpb = pl.waves * 64 / LPC;
   const dim3 first((unsigned)((a.D + cpb - 1) / cpb), pl.chunks - 1, (unsigned)std::min(a.B, 32768)),
       second(first.x, pl.chunks, first.z), threads(many ? 256 : pl.waves * 64);
-#define MT_SCAN(FINAL, MANY, GRID, LDS) \
-  hipLaunchKernelGGL((scan_kernel<T, NS, LPC, FINAL, MANY>), GRID, threads, LDS, st, a, pl)
+#define MT_SCAN(FINAL, MANY, PAD, GRID, LDS) \
+  hipLaunchKernelGGL((scan_kernel<T, NS, LPC, FINAL, MANY, PAD>), GRID, threads, LDS, st, a, pl)
   if (pl.chunks > 1) {
     if (many)
-      MT_SCAN(false, true, first, lds / 2);
+      MT_SCAN(false, true, false, first, lds / 2);
     else
-      MT_SCAN(false, false, first, lds / 2);
+      MT_SCAN(false, false, false, first, lds / 2);
     hipLaunchKernelGGL(scan_join_kernel, dim3((unsigned)(((long long)a.D * a.Np + 255) / 256), first.z), dim3(256), 0, st, a,
                        pl);
   }
-  if (many)
-    MT_SCAN(true, true, second, lds);
+  const bool pad = a.N != a.Np;
+  if (many && pad)
+    MT_SCAN(true, true, true, second, lds);
+  else if (many)
+    MT_SCAN(true, true, false, second, lds);
+  else if (pad)
+    MT_SCAN(true, false, true, second, lds);
   else
-    MT_SCAN(true, false, second, lds);
+    MT_SCAN(true, false, false, second, lds);
 #undef MT_SCAN
   return hipGetLastError();
 }

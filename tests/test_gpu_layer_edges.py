@@ -1,10 +1,11 @@
 """The selective scan at its edges: every length around a tile, within the bound of the roundings that are made
-(none for pieces that are not there)."""
+(none for pieces that are not there); infinite and NaN inputs at state counts that the kernels pad."""
 import pytest
 
 torch = pytest.importorskip("torch")
 
 import layer_ref as ref
+from paper_1804_00344_amd import mtstep as mt
 from test_gpu_layer import DEV, check, dev, gen, per_channel, run_scan, scan_cell, scan_inputs
 from test_layer_cpu import scan_pieces
 
@@ -80,3 +81,41 @@ def test_scan_of_every_length(N, dtype):
         check(y[n, :n], want, ye, ("y", n))
         check(so[n], h, he, ("state", n))
         assert bool((y[n, n:] == 7.0).all())
+
+
+def run_steps(cell, x, dt, z, bc, N, st):
+    """The same prompts [1, S, ..] token by token."""
+    ys, h = [], dev(st).clone()
+    for t in range(x.shape[1]):
+        y = torch.empty(1, cell.D, dtype=x.dtype, device=DEV)
+        w = dev(bc[:, t].contiguous())
+        mt.mt_ssm_step(cell, dev(x[:, t].contiguous()), dev(dt[:, t].contiguous()), w[:, :N], w[:, N:], y, h, h,
+                       z=None if z is None else dev(z[:, t].contiguous()))
+        ys.append(y)
+    return torch.stack(ys, 1), h
+
+
+@pytest.mark.parametrize("N", [1, 5, 16, 24, 100, 200])
+@pytest.mark.parametrize("S", [6, 300])  # whole; cut into pieces
+@pytest.mark.parametrize("which,value", [("x", float("inf")), ("x", float("-inf")), ("x", float("nan")), ("dt", float("inf")),
+                                         ("dt", float("nan"))])
+def test_infinite_inputs(which, value, S, N):
+    """An infinite or NaN input makes of its channel what the formula makes of it, whether or not the states are
+    padded: B and C are positive here, so that the formula's sums of infinities have a sign."""
+    D, c, at = 8, 3, min(4, S - 2)
+    cell, A, dtb, skip = scan_cell(D, N, 1, "f32")
+    x, dt, z, bc = scan_inputs((1, S), D, N, 1, "f32", 3)
+    bc, z = bc.abs() + 0.1, z.abs() + 0.1
+    (x if which == "x" else dt)[0, at, c] = value
+    st = torch.randn(1, D, N, generator=gen(2))
+    want, h, _, _ = ref.scan(x[0].double(), dt[0].double(), per_channel(bc[0], D, N, 1, False), per_channel(bc[0], D, N, 1, True),
+                             z[0].double(), A, dtb, skip, st[0].double())
+    wild = ~torch.isfinite(want)
+    assert bool(wild[at:, c].all()) and not bool(wild[:, [d for d in range(D) if d != c]].any())
+    forms = [run_scan(cell, x, dt, z, bc, N, None, dev(st))] + ([run_steps(cell, x, dt, z, bc, N, st)] if S < 10 else [])
+    for y, so in forms:
+        for got, w in ((y[0].cpu().double(), want), (so[0].cpu().double(), h)):
+            assert torch.equal(torch.isnan(got), torch.isnan(w))
+            assert torch.equal(got[torch.isinf(w)], w[torch.isinf(w)])
+            fin = torch.isfinite(w)
+            assert bool(((got - w)[fin].abs() <= 1e-4 * (1 + w[fin].abs())).all())

@@ -1,5 +1,6 @@
 """The selective scan at its edges: every length around a tile, within the bound of the roundings that are made
-(none for pieces that are not there); infinite and NaN inputs at state counts that the kernels pad."""
+(none for pieces that are not there); infinite and NaN inputs at state counts that the kernels pad;
+steps that keep and that forget the state."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -83,6 +84,23 @@ def test_scan_of_every_length(N, dtype):
         assert bool((y[n, n:] == 7.0).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,S,D,N,cut", [(1, 700, 16, 16, True), (3, 530, 20, 5, True), (1, 600, 12, 100, True),
+                                         (1, 400, 8, 250, True), (64, 60, 300, 16, False), (1, 8, 16, 24, False)])
+def test_scan_within_the_bound_of_its_roundings(B, S, D, N, cut, dtype):
+    piece = piece_of(B, S, D, N)
+    assert bool(piece) == cut
+    cell, A, dtb, skip = scan_cell(D, N, 1, dtype)
+    x, dt, z, bc = scan_inputs((B, S), D, N, 1, dtype, S)
+    st = torch.randn(B, D, N, generator=gen(9))
+    y, so = run_scan(cell, x, dt, z, bc, N, None, dev(st))
+    for b in (0, B - 1):
+        want, h, ye, he = scan_bound(x[b].double(), dt[b].double(), per_channel(bc[b], D, N, 1, False),
+                                     per_channel(bc[b], D, N, 1, True), z[b].double(), A, dtb, skip, st[b].double(), piece)
+        check(y[b], want, ye, "y")
+        check(so[b], h, he, "state")
+
+
 def run_steps(cell, x, dt, z, bc, N, st):
     """The same prompts [1, S, ..] token by token."""
     ys, h = [], dev(st).clone()
@@ -119,3 +137,38 @@ def test_infinite_inputs(which, value, S, N):
             assert torch.equal(got[torch.isinf(w)], w[torch.isinf(w)])
             fin = torch.isfinite(w)
             assert bool(((got - w)[fin].abs() <= 1e-4 * (1 + w[fin].abs())).all())
+
+
+@pytest.mark.parametrize("N", [5, 16, 24, 200])
+def test_steps_that_keep_and_forget_the_state(N):
+    """dt far below zero is a step of zero, which keeps the state to the bit; a large one leaves nothing of it."""
+    D, S, at = 8, 5, 2
+    cell, A, dtb, skip = scan_cell(D, N, 1, "f32")
+    x, dt, z, bc = scan_inputs((1, S), D, N, 1, "f32", 3)
+    st = torch.randn(1, D, N, generator=gen(2))
+    _, before = run_scan(cell, *(t[:, :at].contiguous() for t in (x, dt, z, bc)), N, None, dev(st))
+    bound = lambda n: scan_bound(x[0, :n].double(), dt[0, :n].double(), per_channel(bc[0, :n], D, N, 1, False),
+                                 per_channel(bc[0, :n], D, N, 1, True), z[0, :n].double(), A, dtb, skip, st[0].double(), 0)
+    kept = []
+    for value in (-1e4, -3e38, float("-inf")):
+        dt[0, at] = value
+        y, after = run_scan(cell, *(t[:, :at + 1].contiguous() for t in (x, dt, z, bc)), N, None, dev(st))
+        assert torch.equal(after, before)
+        kept.append(y)
+    assert torch.equal(kept[0], kept[1]) and torch.equal(kept[0], kept[2])
+    dt[0, at] = -1e4
+    want, _, ye, _ = bound(at + 1)
+    check(kept[0][0], want, ye, "kept")
+    # D A below -200 for every rate: the powers are below the smallest float
+    dt[0, at] = 200 / float(A.abs().min()) + 10
+    y, after = run_scan(cell, x, dt, z, bc, N, None, dev(st))
+    want, h, ye, he = bound(S)
+    check(y[0], want, ye, "forgotten")
+    check(after[0], h, he, "state")
+    other, after2 = run_scan(cell, x, dt, z, bc, N, None, dev(st * 3 + 1))  # from another state: nothing of it is left
+    assert torch.equal(y[:, at:], other[:, at:]) and torch.equal(after, after2)
+    dt[0, at] = 1e20
+    y, after = run_scan(cell, *(t[:, :at + 1].contiguous() for t in (x, dt, z, bc)), N, None, dev(st))
+    want, h, ye, he = bound(at + 1)
+    check(y[0], want, ye, "large")
+    check(after[0], h, he, "state")

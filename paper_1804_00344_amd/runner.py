@@ -368,11 +368,15 @@ class SsmLayer:
                 torch.zeros(rows, self.D, self.N, dtype=torch.float32, device=self.device))
 
     def set_batch(self, B: int, S: int, K: int):
-        """Buffers for B prompts of padded length S and K hypotheses of each."""
+        """Buffers for B prompts of padded length S and K hypotheses of each.  Waits for the device (unless it is
+        captured into a graph): prompt and step may then run on any stream, and the last batch's work, wherever it
+        ran, has ended when its buffers are given back."""
+        pb, sb = self._buffers((B, S)), self._buffers((B * K,))
+        prompt_state, beam_state = self._states(B), [self._states(B * K) for _ in range(2)]
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.synchronize(self.device)
         self.B, self.S, self.K, self.M = B, S, K, B * K
-        self.pb, self.sb = self._buffers((B, S)), self._buffers((B * K,))
-        self.prompt_state = self._states(B)
-        self.beam_state = [self._states(B * K) for _ in range(2)]
+        self.pb, self.sb, self.prompt_state, self.beam_state = pb, sb, prompt_state, beam_state
         self.cur = -1  # the states a step reads: the prompts' (-1), or those of the last step
 
     def _project(self, u, f, stream):

@@ -331,7 +331,8 @@ class Ensemble:
 
 class SsmLayer:
     """A recurrent layer of the state space kind for serving: over a padded batch of prompts, then
-    token by token for hypotheses whose states are gathered along the beam, as the Decoder's are.
+    token by token for hypotheses whose states are gathered along the beam, as the Decoder's are.  Its calls run on
+    its own device, whichever is current.
 
         [x' | z] = u Win,  x = conv(x'),  [r | B | C] = x Wx,  dt = r Wdt,  y = scan(x, dt, B, C; z),  out = y Wout
 
@@ -343,6 +344,8 @@ class SsmLayer:
         self.E, self.D, self.R = w["Win"].shape[0], w["Wout"].shape[0], w["Wdt"].shape[0]
         self.N, self.GN, self.W = w["A"].shape[1], groups * w["A"].shape[1], w["conv_w"].shape[1]
         self.device = torch.device(device)
+        if self.device.index is None:  # the device that is current now, for good
+            self.device = torch.device("cuda", torch.cuda.current_device())
         self.io_dtype = torch.bfloat16 if dtype == "bf16" else torch.float32
         cfg = mt.make_ssm_config(self.D, self.N, groups=groups, conv=self.W, conv_silu=conv_silu, dtype=dtype)
         with torch.cuda.device(self.device):
@@ -371,10 +374,11 @@ class SsmLayer:
         """Buffers for B prompts of padded length S and K hypotheses of each.  Waits for the device (unless it is
         captured into a graph): prompt and step may then run on any stream, and the last batch's work, wherever it
         ran, has ended when its buffers are given back."""
-        pb, sb = self._buffers((B, S)), self._buffers((B * K,))
-        prompt_state, beam_state = self._states(B), [self._states(B * K) for _ in range(2)]
-        if not torch.cuda.is_current_stream_capturing():
-            torch.cuda.synchronize(self.device)
+        with torch.cuda.device(self.device):
+            pb, sb = self._buffers((B, S)), self._buffers((B * K,))
+            prompt_state, beam_state = self._states(B), [self._states(B * K) for _ in range(2)]
+            if not torch.cuda.is_current_stream_capturing():
+                torch.cuda.synchronize(self.device)
         self.B, self.S, self.K, self.M = B, S, K, B * K
         self.pb, self.sb, self.prompt_state, self.beam_state = pb, sb, prompt_state, beam_state
         self.cur = -1  # the states a step reads: the prompts' (-1), or those of the last step
@@ -391,11 +395,12 @@ class SsmLayer:
     def prompt(self, u, lens=None, stream=None):
         """u [B, S, E] in the io type, lens [B] int32: out [B, S, E] (valid positions); keeps the states."""
         f, (cs, hs) = self.pb, self.prompt_state
-        xp, z = self._project(u, f, stream)
-        mt.mt_ssm_conv(self.cell, xp, f["x"], lens=lens, state_out=cs, stream=stream)
-        x, dt, bm, cm = self._inputs(f, stream)
-        mt.mt_ssm_scan(self.cell, x, dt, bm, cm, f["y"], z=z, lens=lens, state_out=hs, ws=f["ws"], stream=stream)
-        mt.mt_i8_product(self.wout, f["y"], f["out"], f["ws"], stream=stream)
+        with torch.cuda.device(self.device):
+            xp, z = self._project(u, f, stream)
+            mt.mt_ssm_conv(self.cell, xp, f["x"], lens=lens, state_out=cs, stream=stream)
+            x, dt, bm, cm = self._inputs(f, stream)
+            mt.mt_ssm_scan(self.cell, x, dt, bm, cm, f["y"], z=z, lens=lens, state_out=hs, ws=f["ws"], stream=stream)
+            mt.mt_i8_product(self.wout, f["y"], f["out"], f["ws"], stream=stream)
         self.cur = -1
         return f["out"]
 
@@ -406,10 +411,11 @@ class SsmLayer:
         ci, hi = self.prompt_state if self.cur < 0 else self.beam_state[self.cur]
         nxt = 0 if self.cur != 0 else 1
         co, ho = self.beam_state[nxt]
-        xp, z = self._project(u, f, stream)
-        mt.mt_ssm_conv_step(self.cell, xp, f["x"], ci, co, src_row=src_row, stream=stream)
-        x, dt, bm, cm = self._inputs(f, stream)
-        mt.mt_ssm_step(self.cell, x, dt, bm, cm, f["y"], hi, ho, z=z, src_row=src_row, stream=stream)
-        mt.mt_i8_product(self.wout, f["y"], f["out"], f["ws"], stream=stream)
+        with torch.cuda.device(self.device):
+            xp, z = self._project(u, f, stream)
+            mt.mt_ssm_conv_step(self.cell, xp, f["x"], ci, co, src_row=src_row, stream=stream)
+            x, dt, bm, cm = self._inputs(f, stream)
+            mt.mt_ssm_step(self.cell, x, dt, bm, cm, f["y"], hi, ho, z=z, src_row=src_row, stream=stream)
+            mt.mt_i8_product(self.wout, f["y"], f["out"], f["ws"], stream=stream)
         self.cur = nxt
         return f["out"]

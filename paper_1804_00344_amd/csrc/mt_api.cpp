@@ -197,7 +197,7 @@ std::vector<char> pack_host(const std::vector<Seg> &segs, int K, int esize, int 
 mt_status dev_upload(mt_model *m, const void *host, size_t bytes, void **out) {
   void *d = nullptr;
   const hipError_t e = hipMalloc(&d, bytes ? bytes : 16);
-  if (e != hipSuccess) return fail(MT_ERR_OOM, "hipMalloc(%zu): %s", bytes, hipGetErrorString(e));
+  if (e != hipSuccess) return fail(MT_ERR_OOM, "hipMalloc(%zu): %s", bytes, hip_error(e));
   m->allocs.push_back(d);
   if (bytes && host) HIP_TRY(hipMemcpy(d, host, bytes, hipMemcpyHostToDevice));
   *out = d;
@@ -317,7 +317,7 @@ mt_status scratch_for_device(int dev, void **out) {
     void *ptr = nullptr;
     const hipError_t e = hipGetSymbolAddress((void **)&ptr, HIP_SYMBOL(scratch));
     if (e != hipSuccess || !ptr)
-      return fail(MT_ERR_HIP, "hipGetSymbolAddress(scratch) on device %d: %s", dev, hipGetErrorString(e));
+      return fail(MT_ERR_HIP, "hipGetSymbolAddress(scratch) on device %d: %s", dev, hip_error(e));
     g_scratch[dev] = ptr;
   }
   *out = g_scratch[dev];
@@ -379,7 +379,7 @@ struct Timed {  // records events around one launch when profiling is on
       Timed tm_(model, kid, st, on);                                                        \
       e_ = (expr);                                                                          \
     }                                                                                       \
-    if (e_ != hipSuccess) return fail(MT_ERR_HIP, "%s: %s", #expr, hipGetErrorString(e_)); \
+    if (e_ != hipSuccess) return fail(MT_ERR_HIP, "%s: %s", #expr, hip_error(e_));         \
   } while (0)
 #define LAUNCH(kid, expr) LAUNCH_IF(kid, true, expr)
 

@@ -64,7 +64,7 @@ mt_status alloc(void **p, size_t bytes) {
   const hipError_t e = hipMalloc(p, bytes);
   if (e != hipSuccess) {
     *p = nullptr;
-    return fail(MT_ERR_OOM, "hipMalloc(%zu): %s", bytes, hipGetErrorString(e));
+    return fail(MT_ERR_OOM, "hipMalloc(%zu): %s", bytes, hip_error(e));
   }
   return MT_OK;
 }

@@ -420,7 +420,7 @@ void mt_round_bf16(const float *src, uint16_t *dst, size_t n);
  *   [r | B | C] = x Wx, dt = r Wdt  mt_i8_product   y  = scan(...)   mt_ssm_scan, mt_ssm_step
  *   out = y Wout                mt_i8_product       (and the output layer, for mt_beam_topk)
  * They take these conventions in place of those above:
- *   - Row matrices (x, y, dt, ...) have a row stride in elements (ld.. >= the row's width), so that
+ *   - Row matrices (x, y, dt, ...) have a row stride in elements (the row's width <= ld.. <= 2^32), so that
  *     a column range of a wider matrix can be passed; their pointers need only the alignment
  *     of their element type.  The positions of a padded batch are rows b*S + i.
  *   - A call reads its handle and does not change it: one handle serves several streams and
@@ -456,7 +456,7 @@ size_t mt_i8_workspace_bytes(const mt_i8_matrix *w, int M);
  * the call as the columns of W are (qx = rint(x * (127 / a_m)), s_m = a_m / 127): the sums are
  * exact, and the two scales and the bias are applied in fp32 in this order.  A row that holds a
  * NaN or an infinity gives NaN throughout.  x_dtype and y_dtype: MT_F32 or MT_BF16, each.
- * 1 <= M <= 2^24. */
+ * 1 <= M <= 2^24, M*N <= 2^36. */
 mt_status mt_i8_product(mt_i8_matrix *w, int M, const void *x, int x_dtype, int64_t ldx, void *y, int y_dtype,
                         int64_t ldy, void *ws, size_t ws_bytes, void *stream);
 
@@ -499,7 +499,7 @@ size_t mt_ssm_workspace_bytes(const mt_ssm *cell, int B, int S);
  *     mt_ssm_device_errors).  Positions behind them are neither read nor written.
  *   x, y [B*S, D]; state_in, state_out [B, W-1, D] (16-byte aligned; state_out or both NULL): the
  *     last W-1 inputs after the prompt, oldest first, for the next piece of it or mt_ssm_conv_step.
- * MT_ERR_STATE for a cell without a convolution.  B, S >= 1, B*S <= 2^24. */
+ * MT_ERR_STATE for a cell without a convolution.  B, S >= 1, B*S <= 2^24, S*D <= 2^34. */
 mt_status mt_ssm_conv(mt_ssm *cell, int B, int S, const int32_t *len, const void *x, int64_t ldx,
                       const void *state_in, void *y, int64_t ldy, void *state_out, void *stream);
 
@@ -507,7 +507,7 @@ mt_status mt_ssm_conv(mt_ssm *cell, int B, int S, const int32_t *len, const void
  * (NULL: its own row m), x, y [M, D], state_in [n_state_rows, W-1, D], state_out [M, W-1, D] (both
  * ignored for W = 1).  src_row out of range is clamped and reported by mt_ssm_device_errors.
  * Without src_row state_out may be state_in.  1 <= M, n_state_rows <= 2^24 (n_state_rows >= M
- * without src_row). */
+ * without src_row), M*D <= 2^31. */
 mt_status mt_ssm_conv_step(mt_ssm *cell, int M, const int32_t *src_row, int n_state_rows, const void *x, int64_t ldx,
                            const void *state_in, void *y, int64_t ldy, void *state_out, void *stream);
 
@@ -519,7 +519,7 @@ mt_status mt_ssm_conv_step(mt_ssm *cell, int M, const int32_t *src_row, int n_st
  *   state_in [B, D, N] fp32 (NULL: zeros): the state before the first position;
  *   state_out [B, D, N] fp32 or NULL: the state after the last valid one (a prompt of length 0
  *     copies its state_in).  Both 16-byte aligned.
- * B, S >= 1, B*S <= 2^24. */
+ * B, S >= 1, B*S <= 2^24, S*D <= 2^34. */
 mt_status mt_ssm_scan(mt_ssm *cell, int B, int S, const int32_t *len, const void *x, int64_t ldx, const void *dt,
                       int64_t lddt, const void *bmat, const void *cmat, int64_t ldbc, const void *z, int64_t ldz,
                       const float *state_in, void *y, int64_t ldy, float *state_out, void *ws, size_t ws_bytes,

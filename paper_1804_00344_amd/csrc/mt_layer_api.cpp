@@ -19,6 +19,9 @@ namespace {
 constexpr uint32_t kMagicI8 = 0x4d543849u;   // "MT8I"
 constexpr uint32_t kMagicSsm = 0x4d545353u;  // "MTSS"
 constexpr long long kMaxRows = 1ll << 24;
+constexpr long long kMaxPromptElements = 1ll << 34;   // S*D: a grid dimension of blocks
+constexpr long long kMaxTokenElements = 1ll << 31;    // M*D
+constexpr long long kMaxProductElements = 1ll << 36;  // M*N
 
 }  // namespace
 
@@ -111,13 +114,13 @@ mt_status check_rows(const void *p, const char *name, int64_t ld, int64_t width,
 mt_status check_prompts(int B, int S, int D) {
   if (B < 1 || S < 1 || (long long)B * S > kMaxRows)
     return fail(MT_ERR_SHAPE, "B=%d S=%d: need B, S >= 1 and B*S <= 2^24", B, S);
-  if ((long long)S * D > (1ll << 34)) return fail(MT_ERR_SHAPE, "S*D exceeds 2^34");
+  if ((long long)S * D > kMaxPromptElements) return fail(MT_ERR_SHAPE, "S*D exceeds 2^34");
   return MT_OK;
 }
 
 mt_status check_tokens(int M, int D, const int32_t *src_row, int n_rows) {
   if (M < 1 || M > kMaxRows) return fail(MT_ERR_SHAPE, "M=%d: need 1..2^24", M);
-  if ((long long)M * D > (1ll << 31)) return fail(MT_ERR_SHAPE, "M*D exceeds 2^31");
+  if ((long long)M * D > kMaxTokenElements) return fail(MT_ERR_SHAPE, "M*D exceeds 2^31");
   if (n_rows < 1 || n_rows > kMaxRows) return fail(MT_ERR_SHAPE, "n_state_rows=%d: need 1..2^24", n_rows);
   if (!src_row && n_rows < M) return fail(MT_ERR_SHAPE, "n_state_rows=%d < M=%d without src_row", n_rows, M);
   if (src_row) CHECK(check_dev_ptr(src_row, "src_row", 4));
@@ -218,7 +221,7 @@ mt_status mt_i8_free(mt_i8_matrix *w) {
 }
 
 size_t mt_i8_workspace_bytes(const mt_i8_matrix *w, int M) {
-  if (!valid(w) || M < 1 || M > kMaxRows) return 0;
+  if (!valid(w) || M < 1 || M > kMaxRows || (long long)M * w->N > kMaxProductElements) return 0;
   return i8_rows(M) * w->Kp + i8_rows(M) * 4;
 }
 
@@ -227,7 +230,7 @@ mt_status mt_i8_product(mt_i8_matrix *w, int M, const void *x, int x_dtype, int6
   g_err[0] = 0;
   if (!valid(w)) return fail(MT_ERR_ARG, "invalid matrix handle");
   if (M < 1 || M > kMaxRows) return fail(MT_ERR_SHAPE, "M=%d: need 1..2^24", M);
-  if ((long long)M * w->N > (1ll << 36)) return fail(MT_ERR_SHAPE, "M*N exceeds 2^36");
+  if ((long long)M * w->N > kMaxProductElements) return fail(MT_ERR_SHAPE, "M*N exceeds 2^36");
   CHECK(check_io_type(x_dtype, "x_dtype"));
   CHECK(check_io_type(y_dtype, "y_dtype"));
   const int ex = x_dtype == MT_BF16 ? 2 : 4, ey = y_dtype == MT_BF16 ? 2 : 4;
@@ -322,7 +325,7 @@ mt_status mt_ssm_free(mt_ssm *c) {
 }
 
 size_t mt_ssm_workspace_bytes(const mt_ssm *c, int B, int S) {
-  if (!valid(c) || B < 1 || S < 1 || (long long)B * S > kMaxRows) return 0;
+  if (!valid(c) || B < 1 || S < 1 || (long long)B * S > kMaxRows || (long long)S * c->cfg.D > kMaxPromptElements) return 0;
   return scan_workspace_bytes(B, S, c->cfg.D, c->cfg.N, c->num_cu);
 }
 

@@ -442,7 +442,8 @@ typedef struct mt_i8_matrix mt_i8_matrix; /* opaque, library-owned */
 /* Quantise W [K, N] fp32 row-major ([in x out], as the matrices of mt_weights) and copy it and
  * bias [N] fp32 (or NULL) into library-owned memory of the current device.  Both pointers may
  * be host or device memory.  1 <= K <= 65536, 1 <= N <= 2^24; a NaN or an infinity in W is
- * MT_ERR_ARG.  Synchronises the device before (so W may come from any stream) and after. */
+ * MT_ERR_ARG.  Synchronises the device before (so W may come from any of its streams; what another
+ * device still writes has to be waited for by the caller) and after. */
 mt_status mt_i8_load(int K, int N, const float *W, const float *bias, mt_i8_matrix **out);
 
 /* Release a matrix and its device memory (synchronises the device). */

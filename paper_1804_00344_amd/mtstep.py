@@ -486,10 +486,13 @@ def _space(ws, device):
 
 
 def _host_or_device(a):
-    """An fp32 array and its address: a device tensor stays where it is."""
+    """An fp32 array and its address: a device tensor stays where it is.  What another device than the current one
+    still does for it is waited for: the load waits for its own only."""
     import torch
     if isinstance(a, torch.Tensor):
         a = a.detach().to(torch.float32).contiguous()
+        if a.is_cuda and a.device != _current_device():
+            torch.cuda.synchronize(a.device)
         return a, a.data_ptr()
     a = np.ascontiguousarray(a, np.float32)
     return a, a.ctypes.data

@@ -22,3 +22,17 @@ def test_a_failed_load_does_not_fail_the_next_call():
     mt.mt_i8_product(mat, x, y, ws)
     torch.cuda.synchronize()
     assert bool(torch.isfinite(y).all())
+
+
+def test_a_matrix_of_another_device_is_waited_for(monkeypatch):
+    """With another device current the load would read the matrix while its own device may still write it."""
+    waited = []
+    monkeypatch.setattr(torch.cuda, "synchronize", waited.append)
+    W = torch.randn(8, 4, device=DEV)
+    mt._host_or_device(W)
+    assert waited == []
+    monkeypatch.setattr(mt, "_current_device", lambda: torch.device("cuda", 1))
+    _, p = mt._host_or_device(W)
+    assert waited == [W.device] and p == W.data_ptr()
+    mt._host_or_device(W.cpu())
+    assert len(waited) == 1

@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(256) conv_kernel(ConvArgs a) {
 }
 
 // One token of a hypothesis: its state row is read whole before its new one is written (they may be
-// the same one).  A few bytes per thread and no reuse: 768 x 2048, W = 4, bf16 7.5 us (22 MB of traffic, a
+// the same one).  A few bytes per thread and no reuse: 768 x 2048, W = 4, bf16 7.5 us (25 MB of traffic, a
 // launch's latency and 4.9 us at a copy's rate), one row 2.7.
 template <typename T, int VEC, int W>
 __global__ void __launch_bounds__(256) conv_step_kernel(ConvArgs a) {

@@ -169,7 +169,7 @@ constexpr int waitcnt(int vm, int lgkm) { return (vm & 15) | (vm >> 4) << 14 | 7
 // A workgroup of WM x WN waves computes a tile of 32 MF WM rows by 32 NF WN columns, k in stages of 64
 // through a ring of ST stages in LDS that direct loads fill ST - 1 stages ahead.  8192 x 4096 x 8192 bf16 takes
 // 250 us (2.2 P operations/s) and is bound by power: with the MFMAs busy in 59% of the cycles the clock
-// falls from 2.4 to 1.8 GHz.  768 x 512 x 50000 fp32: 42 us, bound by the 154 MB of its results.
+// falls from 2.4 to 1.8 GHz.  768 x 512 x 50000 fp32: 42 to 47 us, bound by the 154 MB of its results.
 template <int MF, int NF, int WM, int WN, int ST, bool BF, bool STREAM>
 __global__ void __launch_bounds__(64 * WM * WN) i8_tile_kernel(I8Problem p, int tilesM, int tilesN) {
   constexpr int AB = MF * WM, BB = NF * WN;       // blocks of 32 rows and columns

@@ -5,7 +5,6 @@
 
 namespace mt {
 
-constexpr int kI8Block = 32;   // rows of a fragment block: 32 rows x 32 k in 1 KiB (see mt_i8.hip)
 constexpr int kI8KPad = 128;   // k padding of both operands
 constexpr int kI8Pad = 256;    // row and column padding of both operands
 constexpr int kI8MaxK = 65536; // 127 * 127 * 65536 < 2^31

@@ -325,7 +325,8 @@ mt_status mt_ssm_free(mt_ssm *c) {
 }
 
 size_t mt_ssm_workspace_bytes(const mt_ssm *c, int B, int S) {
-  if (!valid(c) || B < 1 || S < 1 || (long long)B * S > kMaxRows || (long long)S * c->cfg.D > kMaxPromptElements) return 0;
+  if (!valid(c) || B < 1 || S < 1 || (long long)B * S > kMaxRows) return 0;
+  if ((long long)S * c->cfg.D > kMaxPromptElements) return 0;
   return scan_workspace_bytes(B, S, c->cfg.D, c->cfg.N, c->num_cu);
 }
 

@@ -140,7 +140,7 @@ __device__ __forceinline__ int longest_first(const int32_t *len, int B, int S, i
 // dt and z of its positions are on their way while a tile is computed.  A tile is always computed whole:
 // behind the end the steps D_t are zero, which keeps the state as it is.
 // Bound by the vector units, active in 80% (first pass) and 85% (second) of the cycles of 1 x 8192 x 2048 x 16
-// (61 and 85 us): an exp2 takes 10 to 11 cycles and does not overlap the products, 3 each, and an
+// (62 and 84 us): an exp2 takes 10 to 11 cycles and does not overlap the products, 3 each, and an
 // eighth of the instructions taken out (lane moves within the products, no copies for the output) gave 4%.
 // MANY: B and C of a tile, of several groups or many states, are more than a thread holds in scan_stage
 // registers.  All 256 threads stage them then, also those of waves without channels, at distances that are
@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(256, NS == 4 ? 4 : NS == 8 ? 3 : 2) scan_kerne
 
 // Joins the pieces: part[c] becomes the state after pieces 0 .. c.  A thread takes one state of a
 // channel and requests sixteen pieces' values at a time: the pass is a chain of those round trips (64
-// pieces of 2048 x 16 states: 6 us; eight at a time with four states per thread: 10.5).
+// pieces of 2048 x 16 states: 7.8 us; eight at a time with four states per thread took 4.5 more).
 __global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs a, ScanPlan pl) {
   constexpr int R = 16;
   const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -405,10 +405,9 @@ __global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs a, ScanPlan pl)
 // each is read and written once, 16 bytes a lane (two and four hypotheses per thread were no faster).
 // WIDE: a lane's four states, and its B and C at any alignment, are one access (N a multiple of 4; 768 x 2048 x
 // 16 element by element: 83 us).  STREAM: the new states are stored past the L2.  For states larger than the L2s
-// together that is
-// the faster form wherever something else runs between two steps: 768 x 2048 x 16 takes 38.5 us (5.6 TB/s)
-// against 54 from the same states again, and 49 against 57 with a 154 MB matrix of logits written between
-// a step and the next; only steps back to back, which find their states in the last-level cache, lose (50
+// together that is the faster form wherever something else runs between two steps: 768 x 2048 x 16 takes 39 us
+// (5.5 TB/s; calls in a graph) against 54 from the same states again, and 49 against 57 with a 154 MB matrix of
+// logits written between a step and the next; only steps back to back, which find their states in the last-level cache, lose (50
 // against 38).
 template <typename T, int LPC, bool WIDE, bool STREAM>
 __global__ void __launch_bounds__(kThreads) scan_step_kernel(ScanArgs a) {
@@ -481,7 +480,7 @@ int scan_groups(int n, int per, int G) { return std::min({G, n, per % n == 0 ? 1
 
 // Lanes of a channel: four states each, more where they exceed a row of 16 lanes.  (16 states per lane, one
 // lane a channel, spilled or left a SIMD two waves: 1 x 8192 x 2048 x 16 176 us and more; eight per lane
-// 156, four 158; 64 x 80 ragged 39 and 33, before the prompts were ordered.)
+// 156, four 158; 64 x 80 ragged 39 and 33, before the prompts were ordered and B and C of a position read at once.)
 int scan_lanes(int Np) { return std::min(Np / 4, 16); }
 
 // Pieces of the axis, by the time they are expected to take: with k waves on a SIMD a wave's position takes
@@ -489,9 +488,9 @@ int scan_lanes(int Np) { return std::min(Np / 4, 16); }
 // piece's start as much as six positions (fitted to 2048 channels x 16 states, 8192 positions, k = 1 to 8,
 // and to 500 to 600 positions of 100 and 256 states).  Cutting the axis adds a first pass over it (0.75 of the
 // second's time) and the join.  Measured, 1 x 8192 x 2048 x 16 in one piece 1343 us, in 16 pieces 187, 32: 152,
-// 64: 148, 128: 154; 64 x 80 x 2048 x 16 whole 28, in two pieces 62; 7 x 97 x 330 x 24 whole 22, in 13 pieces
-// 18; 4 x 600 x 1024 x 100 whole 160, in 16 pieces 199; 2 x 500 x 512 x 256 whole 292, in 8 pieces 92, 16: 99,
-// 32: 116.
+// 64: 148, 128: 154; 64 x 80 x 2048 x 16 whole 28, in two pieces 62; 7 x 97 x 330 x 24 whole 22, in 7 pieces
+// 18.5; 4 x 600 x 1024 x 100 whole 160, in 16 pieces 199; 2 x 500 x 512 x 256 whole 292, in 8 pieces 92, 16
+// (which the rule takes): 99, 32: 116.
 ScanPlan scan_plan(int B, int S, int D, int N, int num_cu) {
   const int Np = scan_padded_states(N);
   ScanPlan best{};

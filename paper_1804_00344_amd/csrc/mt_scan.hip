@@ -393,7 +393,9 @@ __global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs a, ScanPlan pl)
 #pragma unroll
       for (int i = 0; i < R; ++i) {
         if (c0 + i >= live) break;
-        h = fmaf(__builtin_amdgcn_exp2f(w[i] * A2), h, s[i]);
+        // an infinite state outlasts a finite sum of steps, also where its power is below the smallest float
+        const float f = fabsf(h) == INFINITY && w[i] < INFINITY ? 1.f : __builtin_amdgcn_exp2f(w[i] * A2);
+        h = fmaf(f, h, s[i]);
         if (n >= a.N) h = 0.f;  // a state that does not exist: see PAD
         part[(c0 + i) * sp] = h;
       }

@@ -172,3 +172,23 @@ def test_steps_that_keep_and_forget_the_state(N):
     want, h, ye, he = bound(at + 1)
     check(y[0], want, ye, "large")
     check(after[0], h, he, "state")
+
+
+@pytest.mark.parametrize("N", [5, 16])
+def test_an_infinite_state_outlasts_a_piece(N):
+    """Steps that each leave something of the state, but a whole piece of them less than the smallest float: an
+    infinite state stays infinite over a cut axis, as it does position by position."""
+    D, S, at, c = 8, 300, 4, 3
+    assert piece_of(1, S, D, N)
+    cell, A, dtb, skip = scan_cell(D, N, 1, "f32")
+    x, dt, z, bc = scan_inputs((1, S), D, N, 1, "f32", 3)
+    bc, z = bc.abs() + 0.1, z.abs() + 0.1
+    dt = (4 - dtb).float().expand(1, S, D).contiguous()  # D_t of 4.02: a power above e^-80, a piece's below e^-110
+    assert float(-A.min()) * 4.02 < 80 and float(-A[c].min()) * 4 * piece_of(1, S, D, N) > 110
+    x[0, at, c] = float("inf")
+    want, h, _, _ = ref.scan(x[0].double(), dt[0].double(), per_channel(bc[0], D, N, 1, False), per_channel(bc[0], D, N, 1, True),
+                             z[0].double(), A, dtb, skip, torch.zeros(D, N, dtype=torch.float64))
+    y, so = run_scan(cell, x, dt, z, bc, N, None, None)
+    for got, w in ((y[0].cpu().double(), want), (so[0].cpu().double(), h)):
+        assert torch.equal(torch.isnan(got), torch.isnan(w)) and torch.equal(got[torch.isinf(w)], w[torch.isinf(w)])
+    assert bool(torch.isinf(want[at:, c]).all())

@@ -409,8 +409,8 @@ __global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs a, ScanPlan pl)
 // 16 element by element: 83 us).  STREAM: the new states are stored past the L2.  For states larger than the L2s
 // together that is the faster form wherever something else runs between two steps: 768 x 2048 x 16 takes 39 us
 // (5.5 TB/s; calls in a graph) against 54 from the same states again, and 49 against 57 with a 154 MB matrix of
-// logits written between a step and the next; only steps back to back, which find their states in the last-level cache, lose (50
-// against 38).
+// logits written between a step and the next; only steps back to back, which find their states in the last-level
+// cache, lose (50 against 38).
 template <typename T, int LPC, bool WIDE, bool STREAM>
 __global__ void __launch_bounds__(kThreads) scan_step_kernel(ScanArgs a) {
   constexpr int NS = 4, CPB = kThreads / LPC;

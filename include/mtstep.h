@@ -537,6 +537,133 @@ mt_status mt_ssm_step(mt_ssm *cell, int M, const int32_t *src_row, int n_state_r
  * out of range, bit 2 = a len out of range. */
 mt_status mt_ssm_device_errors(mt_ssm *cell, int32_t *flags);
 
+/* ---- Attention layers for serving: heads, a cache of keys and values in pages, page tables along the beam ----
+ *
+ * The operators of a decoder's attention layers next to the recurrent cells above, over whole prompts, pieces of
+ * them, and single tokens of hypotheses.  In the order of their use:
+ *   [q | k | v] = u Wqkv         mt_i8_product      tables of this step     mt_pages_advance
+ *   norms, rotation, store       mt_attn_append     y = attention(q, cache) mt_attn_paged
+ *   q' = u' Wq; k', v' from the encoder's states once a sentence (mt_i8_product)
+ *                                                   y' = attention(q', k', v', mask)  mt_attn_cross
+ * They take the recurrent layer's conventions (row strides, alignment of row matrices, handles, streams, devices,
+ * graphs, overlaps) and these:
+ *   - The cache of one layer is k_pages, v_pages [n_pages, Hk, page, Dh] of the handle's dtype, 16-byte aligned.  A
+ *     program with several layers keeps [layers, n_pages, Hk, page, Dh] and gives each call its layer's part; one
+ *     table serves all layers.
+ *   - A page table is [rows, n_blocks] int32: position p of row r is position p % page of page table[r, p / page].
+ *     Rows may hold pages in common.  len [rows] int32 is the number of positions of a row; entries behind its last
+ *     block are not read.  Positions of the cache that no row's len covers may hold anything.
+ *   - n_new [B] int32 (NULL: all S): how many of a row's S new positions there are; they are its last ones, the i-th
+ *     is position len - n_new + i (where that is below 0, nothing is stored or seen: zeros).  Rows b*S + i of the
+ *     row matrices with i >= n_new[b] are neither read nor written.
+ *   - A len, n_new, src_row or page number out of its range is clamped and reported by mt_attn_device_errors.
+ *   - Results do not depend on timing.  Which keys are summed together depends on the call's sizes (B, S, the heads,
+ *     n_blocks) and lengths, which moves results by roundings. */
+
+/* The heads of a layer.
+ *   Hq: 1..1024 query heads.  Hk: 1..Hq, a divisor of Hq: heads of keys and values; query head h reads h / (Hq/Hk).
+ *   Dh: features of a head, a multiple of 8, 8..256.  Hq*Dh <= 65536.
+ *   page: positions of a page: 8, 16, 32, 64, 128 or 256.
+ *   dtype: MT_F32 or MT_BF16, the type of q, k, v, y and the cache.  Parameters and arithmetic are fp32; a bf16
+ *     layer's softmax weights are rounded to bf16 before the products with the values (their sum is not).
+ *   window: a position sees the last `window` ones, itself included; 0: all before it.  (mt_attn_paged)
+ *   scale: of the scores; 0: 1 / sqrt(Dh).
+ *   For mt_attn_append: qk_norm 0/1 — x / sqrt(mean(x^2) + norm_eps) * gain over each head of q and k;
+ *   rot: features of each head of q and k that are rotated, even, 0..Dh, the first ones; rot_pairs 0: feature i
+ *     turns with i + rot/2, 1: feature 2i with 2i + 1; pair i of position p by the angle p * freq[i];
+ *   rot_base: freq[i] = rot_base^(-2i/rot) where no frequencies are given (> 0, finite). */
+typedef struct {
+  int32_t Hq, Hk, Dh;
+  int32_t page;
+  int32_t dtype;
+  int32_t window;
+  int32_t qk_norm;
+  int32_t rot, rot_pairs;
+  float scale;
+  float norm_eps;
+  float rot_base;
+} mt_attn_config;
+
+/* Parameters: HOST pointers to fp32, only read during mt_attn_load; each may be NULL.
+ *   gq, gk [Dh]: gains of the norms (NULL: ones), read only with qk_norm; freq [rot/2], finite. */
+typedef struct {
+  const float *gq, *gk;
+  const float *freq;
+} mt_attn_weights;
+
+typedef struct mt_attn mt_attn; /* opaque, library-owned */
+
+/* Copy the parameters into library-owned memory of the current device.  Synchronous. */
+mt_status mt_attn_load(const mt_attn_config *cfg, const mt_attn_weights *w, mt_attn **out);
+
+/* Release a layer and its device memory (synchronises the device). */
+mt_status mt_attn_free(mt_attn *a);
+
+/* Norms, rotation and store: q_out = R(norm(q)) for every new position, and R(norm(k)), v into the pages that the
+ * tables give them.  q, q_out [B*S, Hq*Dh] (q_out may be q with the same stride), k, v [B*S, Hk*Dh].  No position of a
+ * page may be written by two rows.  Angles are formed in 64 bits: exact to a rounding at any position.
+ * B, S >= 1, B*S <= 2^24; 1 <= n_blocks, n_blocks*page <= 2^30; B*n_blocks <= 2^30; 1 <= n_pages <= 2^24. */
+mt_status mt_attn_append(mt_attn *a, int B, int S, const int32_t *n_new, const int32_t *len, const void *q, int64_t ldq,
+                         const void *k, int64_t ldk, const void *v, int64_t ldv, void *q_out, int64_t ldqo,
+                         const int32_t *table, int n_blocks, int n_pages, void *k_pages, void *v_pages, void *stream);
+
+/* Workspace bytes of mt_attn_paged for B rows of S new positions over n_keys = n_blocks*page positions, or of
+ * mt_attn_cross for B sentences of S queries over n_keys keys (0 on bad input; positive otherwise).  A workspace for
+ * other sizes need not serve. */
+size_t mt_attn_workspace_bytes(const mt_attn *a, int B, int S, int64_t n_keys);
+
+/* Attention over the cache: the query of position p sees the keys j of its row with p - window < j <= p (window 0:
+ * 0 <= j <= p):  y = sum_j softmax_j(scale q.k_j) v_j  for every query head.  q, y [B*S, Hq*Dh].  The new positions'
+ * keys and values are in the cache already (mt_attn_append).  A query that sees nothing, or whose scores are all
+ * minus infinity, gives zeros.  Keys and values that a query does not see have no part in it, NaN and infinities
+ * among them.  Sizes as mt_attn_append; B*S*Hq <= 2^30. */
+mt_status mt_attn_paged(mt_attn *a, int B, int S, const int32_t *n_new, const int32_t *len, const void *q, int64_t ldq,
+                        const int32_t *table, int n_blocks, int n_pages, const void *k_pages, const void *v_pages,
+                        void *y, int64_t ldy, void *ws, size_t ws_bytes, void *stream);
+
+/* Attention to states of another length: the T queries of each of B sentences (hypotheses, or positions of a target)
+ * see the keys i of their sentence with mask[b, i] != 0 (fp32 [B, S] as in mt_precompute_ctx, any pattern; NULL: all).
+ * q, y [B*T, Hq*Dh]; k, v [B*S, Hk*Dh]; n_q [B] int32 (NULL: all T): the queries of each sentence, as n_new.  Masked
+ * positions are not read into results, whatever they hold.  page and window are not used.
+ * B, T, S >= 1, B*T, B*S <= 2^24, B*T*Hq <= 2^30. */
+mt_status mt_attn_cross(mt_attn *a, int B, int T, const int32_t *n_q, int S, const float *mask, const void *q, int64_t ldq,
+                        const void *k, int64_t ldk, const void *v, int64_t ldv, void *y, int64_t ldy, void *ws,
+                        size_t ws_bytes, void *stream);
+
+/* Workspace bytes of mt_pages_advance and mt_pages_pack for M rows and n_pages pages (0 on bad input). */
+size_t mt_pages_workspace_bytes(const mt_attn *a, int M, int n_pages);
+
+/* The page tables of the next step.  Row m continues row src_row[m] of table_in [M_in, n_blocks], len_in [M_in]
+ * (src_row NULL: row m, M = M_in; src_row[m] < 0: an empty row, so a finished hypothesis gives its pages back), and gets
+ * room for add[m] >= 0 more positions (add NULL: one each): len_out[m] = its length + add[m].
+ *   - A page is free where no row continues with it.  The tables are all that says so: one pool of pages has one table.
+ *   - A row that grows inside a page which others hold too gets a copy of it: its positions so far, in all layers.  Where
+ *     every holder of the page grows, the last of them keeps the page itself.
+ *   - Free pages are given out lowest number first, to the rows in order, to each its copy before its further blocks.
+ *   - table_out [M, n_blocks] holds -1 behind a row's blocks; free_out [1] int32 or NULL: the pages free afterwards.
+ *   - Where the free pages do not suffice or a row would pass n_blocks, no page is written, every len_out is 0 (so that
+ *     calls with them do nothing), table_out is -1, free_out n_pages, and mt_attn_device_errors reports it; table_in and
+ *     len_in still describe the cache.
+ * k_pages, v_pages [layers, n_pages, Hk, page, Dh].  1 <= M, M_in <= 2^20, M*n_blocks, M_in*n_blocks <= 2^30,
+ * n_blocks*page <= 2^30, 1 <= n_pages <= 2^24, 1 <= layers <= 1024. */
+mt_status mt_pages_advance(mt_attn *a, int M_in, int M, const int32_t *src_row, const int32_t *add,
+                           const int32_t *table_in, const int32_t *len_in, int n_blocks, int n_pages,
+                           int32_t *table_out, int32_t *len_out, int32_t *free_out, int layers, void *k_pages,
+                           void *v_pages, void *ws, size_t ws_bytes, void *stream);
+
+/* The pages in use copied to the front of another cache (smaller, larger, or the next pool): page number p becomes the
+ * count of used pages below p; k_out, v_out [layers, n_pages_out, Hk, page, Dh], table_out [M, n_blocks] (-1 behind a
+ * row's blocks), len_out [M], used_out [1] int32 (or NULL) the number of them.  Pages are copied whole.  Where n_pages_out do not
+ * suffice, no page is written, len_out and used_out are 0, table_out is -1, and mt_attn_device_errors reports it. */
+mt_status mt_pages_pack(mt_attn *a, int M, const int32_t *table_in, const int32_t *len_in, int n_blocks, int n_pages,
+                        int layers, const void *k_in, const void *v_in, int n_pages_out, int32_t *table_out,
+                        int32_t *len_out, int32_t *used_out, void *k_out, void *v_out, void *ws, size_t ws_bytes,
+                        void *stream);
+
+/* Reads and clears the layer's device-side error bits (synchronises the device): bit 1 = a src_row out of range, bit
+ * 2 = a len, n_new, n_q or add out of range, bit 4 = a page number out of range, bit 8 = too few pages or blocks. */
+mt_status mt_attn_device_errors(mt_attn *a, int32_t *flags);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char *mt_last_error(void);
 

@@ -1,0 +1,113 @@
+// Device helpers shared by the attention kernels: where a key's features are, what a query sees, and one query by one wave.
+#pragma once
+
+#include "mt_layer_dev.h"
+#include "mt_mha.h"
+
+namespace mt {
+
+constexpr float kNegInf = -__builtin_inff();
+
+// The lengths of row b: positions and new ones (paged), or keys and queries (cross); clamped, reported where tell is set
+struct RowSpan {
+  int len, n;  // keys, queries
+  int first;   // paged: position of query 0
+};
+template <bool PAGED>
+__device__ __forceinline__ RowSpan row_span(const MhaArgs &a, int b, bool tell) {
+  RowSpan r;
+  const int n0 = a.n_new ? a.n_new[b] : a.S;
+  r.n = min(max(n0, 0), a.S);
+  bool bad = n0 != r.n;
+  if (PAGED) {
+    const int l0 = a.len[b];
+    r.len = min(max(l0, 0), a.n_blocks << a.page_log2);
+    bad |= l0 != r.len;
+  } else {
+    r.len = a.Sk;
+  }
+  r.first = r.len - r.n;
+  if (tell && bad) atomicOr(a.err, kErrLen);
+  return r;
+}
+
+// keys [lo, hi) that query i may see
+template <bool PAGED>
+__device__ __forceinline__ void seen_keys(const MhaArgs &a, const RowSpan &r, int i, int &lo, int &hi) {
+  lo = 0;
+  hi = r.len;
+  if (PAGED) {
+    hi = r.first + i + 1;
+    if (a.window) lo = max(0, hi - a.window);
+  }
+}
+
+// page of block j of row b (a number out of range is clamped and reported)
+__device__ __forceinline__ int block_page(const MhaArgs &a, int b, int j) {
+  const int p = a.table[(long long)b * a.n_blocks + j];
+  if ((unsigned)p < (unsigned)a.n_pages) return p;
+  atomicOr(a.err, kErrPage);
+  return p < 0 ? 0 : a.n_pages - 1;
+}
+
+// element offset of key j of row b and key head h from the cache's (or the rows') beginning
+template <bool PAGED>
+__device__ __forceinline__ long long key_at(const MhaArgs &a, int b, int h, int j, long long ld) {
+  if (PAGED)
+    return ((((long long)block_page(a, b, j >> a.page_log2) * a.Hk + h) << a.page_log2) + (j & ((1 << a.page_log2) - 1))) * a.Dh;
+  return ((long long)b * a.Sk + j) * ld + h * a.Dh;
+}
+
+// One query head of one query by one wave: 64 keys at a time, a key per lane for the scores (running maximum and sum
+// in 32 bits), a feature per lane for the values.  qs: 256 floats of LDS of the wave.  A key that is not seen is not read.
+template <typename T, bool PAGED>
+__device__ void attend_one(const MhaArgs &a, const RowSpan &r, int b, int i, int hq, float *qs) {
+  constexpr int VEC = 16 / sizeof(T);
+  typedef Vec<T, VEC> V;
+  const int lane = threadIdx.x & 63, h = hq / a.G;
+  const long long row = (long long)b * a.S + i;
+  const T *q = (const T *)a.q + row * a.ldq + (long long)hq * a.Dh;
+  for (int d = lane; d < a.Dh; d += 64) qs[d] = (float)q[d];
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  int lo, hi;
+  seen_keys<PAGED>(a, r, i, lo, hi);
+  float m = kNegInf, l = 0.f, acc[4] = {};
+  for (int t = lo; t < hi; t += 64) {
+    const int j = t + lane;
+    const bool seen = j < hi && (PAGED || !a.mask || a.mask[(long long)b * a.Sk + j] != 0.f);
+    float s = kNegInf;
+    if (seen) {
+      const T *k = (const T *)a.k + key_at<PAGED>(a, b, h, j, a.ldk);
+      float x = 0.f;
+      for (int d = 0; d < a.Dh; d += VEC) {
+        const typename V::Raw v = V::raw_any(k + d);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x = fmaf(qs[d + e], (float)v.v[e], x);
+      }
+      s = x * a.scale;
+    }
+    const float mn = fmaxf(m, wave_max(s)), use = mn == kNegInf ? 0.f : mn;
+    const float p = seen ? __builtin_amdgcn_exp2f(s - use) : 0.f;
+    const float c = m == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m - use);
+    m = mn;
+    l = l * c + wave_sum(p);
+#pragma unroll
+    for (int f = 0; f < 4; ++f) acc[f] *= c;
+    for (unsigned long long left = __ballot(seen); left; left &= left - 1) {
+      const int kk = __builtin_ctzll(left);
+      const float w = lane_f(p, kk);
+      const T *v = (const T *)a.v + key_at<PAGED>(a, b, h, t + kk, a.ldv);
+#pragma unroll
+      for (int f = 0; f < 4; ++f)
+        if (lane + 64 * f < a.Dh) acc[f] = fmaf(w, (float)v[lane + 64 * f], acc[f]);
+    }
+  }
+  T *y = (T *)a.y + row * a.ldy + (long long)hq * a.Dh;
+#pragma unroll
+  for (int f = 0; f < 4; ++f)
+    if (lane + 64 * f < a.Dh) Store<T>::put(y + lane + 64 * f, l == 0.f ? 0.f : acc[f] / l);
+  __builtin_amdgcn_wave_barrier();
+}
+
+}  // namespace mt

@@ -1,0 +1,299 @@
+// Page tables of a cache along the beam: rows continue others, shared pages that are written next are copied, free
+// pages given out; and the used pages packed into another cache.  Which pages are free follows from the tables alone.
+#include "mt_mha.h"
+
+namespace mt {
+
+namespace {
+
+constexpr int kRowChunk = 256, kPageChunk = 4096;
+
+// Workspace: per page its references, those by rows that go on writing it, and the last such row + 1; per row its needs
+// and where they begin within its chunk; per chunk of rows and of pages their sums; the free (packed: used) pages in order
+struct Space {
+  int *refs, *growers, *last;  // [n_pages]
+  int *list;                   // [n_pages]
+  int *begin;                  // [M] need before the row within its chunk; the row's own need in the upper half of need
+  int *need;                   // [M]
+  int *row_sum, *page_sum;     // per chunk
+  int *flags;                  // [4]: too long a row
+};
+
+__host__ __device__ inline int chunks(int n, int c) { return (n + c - 1) / c; }
+
+Space space(void *ws, int M, int n_pages) {
+  Space s;
+  int *p = (int *)ws;
+  s.flags = p; p += 4;
+  s.refs = p; p += n_pages;
+  s.growers = p; p += n_pages;
+  s.last = p; p += n_pages;
+  s.list = p; p += n_pages;
+  s.begin = p; p += M;
+  s.need = p; p += M;
+  s.row_sum = p; p += chunks(M, kRowChunk);
+  s.page_sum = p;
+  return s;
+}
+
+// A row's source, length and growth, as the arguments say and clamped; out of range is reported where tell is set
+struct Row {
+  int src, len, blocks, add;  // src < 0: an empty row
+};
+__device__ __forceinline__ Row row_of(const PagesArgs &a, int m, bool tell) {
+  Row r;
+  int bad = 0;
+  r.src = a.row ? a.row[m] : m;
+  if (r.src >= a.M_in) {
+    r.src = a.M_in - 1;
+    bad |= kErrRow;
+  }
+  const int cap = a.n_blocks << a.page_log2;
+  r.len = 0;
+  if (r.src >= 0) {
+    const int l = a.len_in[r.src];
+    r.len = min(max(l, 0), cap);
+    if (l != r.len) bad |= kErrLen;
+  }
+  r.blocks = (r.len + (1 << a.page_log2) - 1) >> a.page_log2;
+  const int add = a.add ? a.add[m] : 1;
+  r.add = max(add, 0);
+  if (add < 0) bad |= kErrLen;
+  if (tell && bad) atomicOr(a.err, bad);
+  return r;
+}
+
+__device__ __forceinline__ int page_of(const PagesArgs &a, const Row &r, int j, bool tell) {
+  int p = a.table_in[(long long)r.src * a.n_blocks + j];
+  if ((unsigned)p >= (unsigned)a.n_pages) {
+    if (tell) atomicOr(a.err, kErrPage);
+    p = p < 0 ? 0 : a.n_pages - 1;
+  }
+  return p;
+}
+
+__global__ void __launch_bounds__(256) clear_kernel(int *p, long long n) {
+  for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) p[i] = 0;
+}
+
+// Copies the tables and counts the references.  GROW: and those by rows that go on writing their last page.
+template <bool GROW>
+__global__ void __launch_bounds__(256) count_kernel(PagesArgs a, Space s) {
+  const long long n = (long long)a.M * a.n_blocks;
+  for (long long e = blockIdx.x * 256ll + threadIdx.x; e < n; e += gridDim.x * 256ll) {
+    const int m = (int)(e / a.n_blocks), j = (int)(e - (long long)m * a.n_blocks);
+    const Row r = row_of(a, m, j == 0);
+    int p = -1;
+    if (j < r.blocks) {
+      p = page_of(a, r, j, true);
+      if (GROW) {
+        atomicAdd(&s.refs[p], 1);
+        if (j == r.blocks - 1 && r.add > 0 && (r.len & ((1 << a.page_log2) - 1))) {
+          atomicAdd(&s.growers[p], 1);
+          atomicMax(&s.last[p], m + 1);
+        }
+      } else {
+        s.refs[p] = 1;  // whoever writes it
+      }
+    }
+    if (GROW) a.table_out[e] = p;
+  }
+}
+
+// whether row m takes a copy of the page that it goes on writing
+__device__ __forceinline__ bool copies(const PagesArgs &a, const Space &s, const Row &r, int m) {
+  if (r.add == 0 || !(r.len & ((1 << a.page_log2) - 1))) return false;
+  const int p = page_of(a, r, r.blocks - 1, false);
+  return s.refs[p] > 1 && !(s.last[p] == m + 1 && s.growers[p] == s.refs[p]);
+}
+
+__device__ __forceinline__ int blocks_after(const PagesArgs &a, const Row &r) {  // both addends are below 2^31
+  return (int)(((long long)r.len + r.add + (1 << a.page_log2) - 1) >> a.page_log2);
+}
+
+// sum over a workgroup of 256 threads, and the sum of the threads before this one
+__device__ __forceinline__ int block_scan(int v, int &total) {
+  __shared__ int w[4];
+  const int incl = wave_incl_scan(v);
+  if ((threadIdx.x & 63) == 63) w[threadIdx.x >> 6] = incl;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (i < (int)(threadIdx.x >> 6)) before += w[i];
+    total += w[i];
+  }
+  __syncthreads();
+  return before + incl - v;
+}
+
+// sum of n values before a chunk, over the workgroup
+__device__ __forceinline__ int sum_before(const int *v, int n) {
+  int x = 0, total;
+  for (int i = threadIdx.x; i < n; i += 256) x += v[i];
+  block_scan(x, total);
+  return total;
+}
+
+// The first workgroups: the needs of a chunk of rows; the others: the free (used) pages of a chunk of pages.
+template <bool GROW>
+__global__ void __launch_bounds__(256) need_kernel(PagesArgs a, Space s, int row_chunks) {
+  int total;
+  if ((int)blockIdx.x < row_chunks) {
+    const int m = blockIdx.x * kRowChunk + threadIdx.x;
+    int need = 0;
+    if (m < a.M) {
+      const Row r = row_of(a, m, false);
+      const int after = blocks_after(a, r);
+      if (after > a.n_blocks)
+        s.flags[0] = 1;
+      else  // fewer than 2^30 blocks a table: their sum fits
+        need = after - r.blocks + (copies(a, s, r, m) ? 1 : 0);
+    }
+    const int before = block_scan(need, total);
+    if (m < a.M) {
+      s.begin[m] = before;
+      s.need[m] = need;
+    }
+    if (threadIdx.x == 0) s.row_sum[blockIdx.x] = total;
+    return;
+  }
+  const int c = blockIdx.x - row_chunks, p0 = c * kPageChunk;
+  int n = 0;
+  for (int i = threadIdx.x; i < kPageChunk; i += 256)
+    if (p0 + i < a.n_pages) n += GROW ? s.refs[p0 + i] == 0 : s.refs[p0 + i] != 0;
+  block_scan(n, total);
+  if (threadIdx.x == 0) s.page_sum[c] = total;
+}
+
+// The free pages in order; PACK: every used page's number in the order instead.
+template <bool PACK>
+__global__ void __launch_bounds__(256) list_kernel(PagesArgs a, Space s) {
+  const int p0 = blockIdx.x * kPageChunk;
+  int at = sum_before(s.page_sum, blockIdx.x);
+  constexpr int PER = kPageChunk / 256;  // a thread's pages are neighbours
+  const int first = p0 + threadIdx.x * PER;
+  int n = 0, total;
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (first + i < a.n_pages) n += (s.refs[first + i] == 0) != PACK;
+  at += block_scan(n, total);
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (first + i < a.n_pages && (s.refs[first + i] == 0) != PACK) {
+      s.list[at] = first + i;
+      if (PACK) s.growers[first + i] = at;
+      ++at;
+    }
+}
+
+// bytes of one page of one layer's keys or values
+__device__ __forceinline__ long long page_size(const PagesArgs &a) { return (a.head_bytes << a.page_log2) * a.Hk; }
+
+__device__ __forceinline__ void copy16(char *dst, const char *src, long long bytes, int t, int n) {
+  for (long long o = t * 16ll; o < bytes; o += n * 16ll) *(int4 *)(dst + o) = *(const int4 *)(src + o);
+}
+
+// Row m: its table and length, and (every slice blockIdx.y: a layer's keys or values) the copy of its shared page.
+__global__ void __launch_bounds__(256) assign_kernel(PagesArgs a, Space s, int row_chunks, int page_chunks) {
+  const int m = blockIdx.x;
+  const int need_all = sum_before(s.row_sum, row_chunks), free_all = sum_before(s.page_sum, page_chunks);
+  const bool fails = s.flags[0] || need_all > free_all;
+  int *const row = a.table_out + (long long)m * a.n_blocks;
+  const Row r = row_of(a, m, false);
+  if (fails) {
+    if (blockIdx.y) return;
+    for (int j = threadIdx.x; j < a.n_blocks; j += 256) row[j] = -1;
+    if (threadIdx.x == 0) {
+      a.len_out[m] = 0;
+      if (m == 0) {
+        if (a.free_out) *a.free_out = a.n_pages;
+        atomicOr(a.err, kErrRoom);
+      }
+    }
+    return;
+  }
+  const int after = blocks_after(a, r), cow = s.need[m] - (after - r.blocks);
+  const int begin = s.begin[m] + sum_before(s.row_sum, m / kRowChunk);
+  if (blockIdx.y == 0) {
+    for (int j = threadIdx.x; j < after - r.blocks; j += 256) row[r.blocks + j] = s.list[begin + cow + j];
+    if (threadIdx.x == 0) {
+      a.len_out[m] = r.len + r.add;
+      if (cow) row[r.blocks - 1] = s.list[begin];
+      if (m == 0 && a.free_out) *a.free_out = free_all - need_all;
+    }
+  }
+  if (!cow) return;
+  const int from = page_of(a, r, r.blocks - 1, false), to = s.list[begin];
+  const long long bytes = (r.len & ((1 << a.page_log2) - 1)) * a.head_bytes, head = a.head_bytes << a.page_log2;
+  const int layer = blockIdx.y >> 1;
+  char *base = (char *)(blockIdx.y & 1 ? a.v_out : a.k_out) + (long long)layer * a.n_pages * page_size(a);
+  for (int h = 0; h < a.Hk; ++h)
+    copy16(base + to * page_size(a) + h * head, base + from * page_size(a) + h * head, bytes, threadIdx.x, 256);
+}
+
+// Pack: the tables renumbered
+__global__ void __launch_bounds__(256) renumber_kernel(PagesArgs a, Space s, int page_chunks) {
+  const int used = sum_before(s.page_sum, page_chunks);
+  const bool fails = used > a.n_pages_out;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    if (a.free_out) *a.free_out = fails ? 0 : used;
+    if (fails) atomicOr(a.err, kErrRoom);
+  }
+  const long long n = (long long)a.M * a.n_blocks;
+  for (long long e = blockIdx.x * 256ll + threadIdx.x; e < n; e += gridDim.x * 256ll) {
+    const int m = (int)(e / a.n_blocks), j = (int)(e - (long long)m * a.n_blocks);
+    const Row r = row_of(a, m, false);
+    a.table_out[e] = !fails && j < r.blocks ? s.growers[page_of(a, r, j, false)] : -1;
+    if (j == 0) a.len_out[m] = fails ? 0 : r.len;
+  }
+}
+
+// Pack: the pages, each slice blockIdx.y a layer's keys or values
+__global__ void __launch_bounds__(256) move_kernel(PagesArgs a, Space s, int page_chunks) {
+  const int used = sum_before(s.page_sum, page_chunks);
+  if (used > a.n_pages_out) return;
+  const long long size = page_size(a);
+  const int layer = blockIdx.y >> 1;
+  const char *in = (const char *)(blockIdx.y & 1 ? a.v_in : a.k_in) + (long long)layer * a.n_pages * size;
+  char *out = (char *)(blockIdx.y & 1 ? a.v_out : a.k_out) + (long long)layer * a.n_pages_out * size;
+  for (int i = blockIdx.x; i < used; i += gridDim.x) copy16(out + i * size, in + s.list[i] * size, size, threadIdx.x, 256);
+}
+
+}  // namespace
+
+size_t pages_workspace_bytes(int M, int n_pages) {
+  const long long n = 4 + 4ll * n_pages + 2ll * M + chunks(M, kRowChunk) + chunks(n_pages, kPageChunk);
+  return (size_t)((n * 4 + 255) / 256 * 256);
+}
+
+hipError_t launch_advance(const PagesArgs &a, hipStream_t st) {
+  const Space s = space(a.ws, a.M, a.n_pages);
+  const int rc = chunks(a.M, kRowChunk), pc = chunks(a.n_pages, kPageChunk);
+  const long long clear = 4 + 3ll * a.n_pages, n = (long long)a.M * a.n_blocks;
+  auto blocks = [](long long k) { return dim3((unsigned)(k < 256 * 4096 ? (k + 255) / 256 : 4096)); };
+  hipLaunchKernelGGL(clear_kernel, blocks(clear), dim3(256), 0, st, s.flags, clear);
+  hipLaunchKernelGGL(count_kernel<true>, blocks(n), dim3(256), 0, st, a, s);
+  hipLaunchKernelGGL(need_kernel<true>, dim3(rc + pc), dim3(256), 0, st, a, s, rc);
+  hipLaunchKernelGGL(list_kernel<false>, dim3(pc), dim3(256), 0, st, a, s);
+  hipLaunchKernelGGL(assign_kernel, dim3(a.M, 2 * a.layers), dim3(256), 0, st, a, s, rc, pc);
+  return hipGetLastError();
+}
+
+hipError_t launch_pack(const PagesArgs &a, hipStream_t st) {
+  const Space s = space(a.ws, a.M, a.n_pages);
+  const int pc = chunks(a.n_pages, kPageChunk);
+  const long long clear = 4 + (long long)a.n_pages, n = (long long)a.M * a.n_blocks;
+  auto blocks = [](long long k) { return dim3((unsigned)(k < 256 * 4096 ? (k + 255) / 256 : 4096)); };
+  hipLaunchKernelGGL(clear_kernel, blocks(clear), dim3(256), 0, st, s.flags, clear);
+  hipLaunchKernelGGL(count_kernel<false>, blocks(n), dim3(256), 0, st, a, s);
+  hipLaunchKernelGGL(need_kernel<false>, dim3(pc), dim3(256), 0, st, a, s, 0);
+  hipLaunchKernelGGL(list_kernel<true>, dim3(pc), dim3(256), 0, st, a, s);
+  hipLaunchKernelGGL(renumber_kernel, blocks(n), dim3(256), 0, st, a, s, pc);
+  const int most = a.n_pages < a.n_pages_out ? a.n_pages : a.n_pages_out;
+  hipLaunchKernelGGL(move_kernel, dim3(most < 65536 ? most : 65536, 2 * a.layers), dim3(256), 0, st, a, s, pc);
+  return hipGetLastError();
+}
+
+}  // namespace mt

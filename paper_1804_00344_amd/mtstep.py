@@ -68,6 +68,19 @@ class mt_ssm_weights(C.Structure):
     _fields_ = [(n, _fp) for n in SSM_WEIGHT_FIELDS]
 
 
+class mt_attn_config(C.Structure):
+    _fields_ = [("Hq", C.c_int32), ("Hk", C.c_int32), ("Dh", C.c_int32), ("page", C.c_int32), ("dtype", C.c_int32),
+                ("window", C.c_int32), ("qk_norm", C.c_int32), ("rot", C.c_int32), ("rot_pairs", C.c_int32),
+                ("scale", C.c_float), ("norm_eps", C.c_float), ("rot_base", C.c_float)]
+
+
+ATTN_WEIGHT_FIELDS = ["gq", "gk", "freq"]
+
+
+class mt_attn_weights(C.Structure):
+    _fields_ = [(n, _fp) for n in ATTN_WEIGHT_FIELDS]
+
+
 _lib = None
 _vp = C.c_void_p
 
@@ -146,6 +159,25 @@ def lib() -> C.CDLL:
         for f in ("mt_i8_load", "mt_i8_free", "mt_i8_product", "mt_ssm_load", "mt_ssm_free", "mt_ssm_conv",
                   "mt_ssm_conv_step", "mt_ssm_scan", "mt_ssm_step", "mt_ssm_device_errors"):
             getattr(L, f).restype = C.c_int
+        L.mt_attn_load.argtypes = [C.POINTER(mt_attn_config), C.POINTER(mt_attn_weights), C.POINTER(_vp)]
+        L.mt_attn_free.argtypes = [_vp]
+        L.mt_attn_append.argtypes = [_vp, C.c_int, C.c_int, _vp, _vp, _vp, i64, _vp, i64, _vp, i64, _vp, i64, _vp,
+                                     C.c_int, C.c_int, _vp, _vp, _vp]
+        L.mt_attn_workspace_bytes.argtypes = [_vp, C.c_int, C.c_int, i64]
+        L.mt_attn_paged.argtypes = [_vp, C.c_int, C.c_int, _vp, _vp, _vp, i64, _vp, C.c_int, C.c_int, _vp, _vp, _vp,
+                                    i64, _vp, sz, _vp]
+        L.mt_attn_cross.argtypes = [_vp, C.c_int, C.c_int, _vp, C.c_int, _vp, _vp, i64, _vp, i64, _vp, i64, _vp, i64,
+                                    _vp, sz, _vp]
+        L.mt_pages_workspace_bytes.argtypes = [_vp, C.c_int, C.c_int]
+        L.mt_pages_advance.argtypes = [_vp, C.c_int, C.c_int, _vp, _vp, _vp, _vp, C.c_int, C.c_int, _vp, _vp, _vp,
+                                       C.c_int, _vp, _vp, _vp, sz, _vp]
+        L.mt_pages_pack.argtypes = [_vp, C.c_int, _vp, _vp, C.c_int, C.c_int, C.c_int, _vp, _vp, C.c_int, _vp, _vp,
+                                    _vp, _vp, _vp, _vp, sz, _vp]
+        L.mt_attn_device_errors.argtypes = [_vp, C.POINTER(C.c_int32)]
+        for f in ("mt_attn_load", "mt_attn_free", "mt_attn_append", "mt_attn_paged", "mt_attn_cross", "mt_pages_advance",
+                  "mt_pages_pack", "mt_attn_device_errors"):
+            getattr(L, f).restype = C.c_int
+        L.mt_attn_workspace_bytes.restype = L.mt_pages_workspace_bytes.restype = sz
         L.mt_round_bf16.argtypes = [_vp, _vp, C.c_size_t]
         L.mt_round_bf16.restype = None
         for f in ("mt_load_weights", "mt_free", "mt_precompute_ctx", "mt_decoder_step", "mt_beam_topk",
@@ -639,3 +671,159 @@ def mt_ssm_step(cell: Ssm, x, dt, bmat, cmat, y, state_in, state_out, *, z=None,
     _check(lib().mt_ssm_step(cell.handle, M, _packed(src_row, "src_row", (M,), cell.i32, dev), n, *r[:9],
                              _packed(state_in, "state_in", (n, cell.D, cell.N), cell.f32, dev), r[9], r[10],
                              _packed(state_out, "state_out", (M, cell.D, cell.N), cell.f32, dev), _stream_on(stream, dev)))
+
+
+# ---- attention layers: heads, a cache in pages, page tables along the beam -------------------------
+#
+# Row matrices as above.  A layer's cache is k_pages, v_pages [n_pages, Hk, page, Dh], several layers' (mt_pages_*)
+# [layers, n_pages, Hk, page, Dh]; page tables are [rows, n_blocks] int32, contiguous.
+
+class Attn:
+    """Owns an mt_attn handle (freed with mt_attn_free)."""
+
+    def __init__(self, handle: int, cfg: mt_attn_config, device):
+        import torch
+        self.handle, self.cfg, self.device = handle, cfg, device
+        self.QD, self.KD = cfg.Hq * cfg.Dh, cfg.Hk * cfg.Dh
+        self.page_shape = torch.Size((cfg.Hk, cfg.page, cfg.Dh))
+        self.dtype = torch.bfloat16 if cfg.dtype == MT_BF16 else torch.float32
+        self.f32, self.i32 = torch.float32, torch.int32
+
+    def __del__(self):
+        if getattr(self, "handle", None):
+            try:
+                lib().mt_attn_free(self.handle)
+            except Exception:
+                pass
+            self.handle = None
+
+
+def make_attn_config(Hq, Hk, Dh, *, page=16, dtype="f32", window=0, scale=0.0, qk_norm=False, norm_eps=1e-6, rot=0,
+                     rot_pairs=False, rot_base=10000.0):
+    return mt_attn_config(Hq, Hk, Dh, page, MT_BF16 if dtype == "bf16" else MT_F32, window, int(qk_norm), rot,
+                          int(rot_pairs), scale, norm_eps, rot_base)
+
+
+def mt_attn_load(cfg: mt_attn_config, weights=None) -> Attn:
+    """weights: fp32 numpy arrays or torch tensors by field name (see mt_attn_weights), each optional."""
+    shapes = dict(gq=(cfg.Dh,), gk=(cfg.Dh,), freq=(cfg.rot // 2,))
+    w, keep = mt_attn_weights(), []
+    for n in ATTN_WEIGHT_FIELDS:
+        a = (weights or {}).get(n)
+        if a is None:
+            continue
+        if hasattr(a, "detach"):
+            a = a.detach().float().cpu().numpy()
+        a = np.ascontiguousarray(a, np.float32)
+        if a.shape != shapes[n]:
+            raise ValueError(f"{n} has shape {a.shape}: need {shapes[n]}")
+        keep.append(a)
+        setattr(w, n, a.ctypes.data_as(_fp))
+    h = _vp()
+    _check(lib().mt_attn_load(C.byref(cfg), C.byref(w), C.byref(h)))
+    return Attn(h.value, mt_attn_config.from_buffer_copy(cfg), _current_device())
+
+
+def mt_attn_free(layer: Attn):
+    if layer.handle:
+        _check(lib().mt_attn_free(layer.handle))
+        layer.handle = None
+
+
+def mt_attn_workspace_bytes(layer: Attn, B: int, S: int, n_keys: int) -> int:
+    return int(lib().mt_attn_workspace_bytes(layer.handle, B, S, n_keys))
+
+
+def mt_pages_workspace_bytes(layer: Attn, M: int, n_pages: int) -> int:
+    return int(lib().mt_pages_workspace_bytes(layer.handle, M, n_pages))
+
+
+def mt_attn_device_errors(layer: Attn) -> int:
+    f = C.c_int32(0)
+    _check(lib().mt_attn_device_errors(layer.handle, C.byref(f)))
+    return int(f.value)
+
+
+def _cache(layer, k, v, layers, names=("k_pages", "v_pages")):
+    """(layers or None, pages, addresses) of a cache; layers: whether it has that dimension."""
+    if k.dim() != 4 + layers:
+        raise ValueError(f"{names[0]}: need {4 + layers} dimensions")
+    shape = k.shape[:1 + layers] + layer.page_shape
+    return k.shape[0], k.shape[layers], _packed(k, names[0], shape, layer.dtype, layer.device), _packed(
+        v, names[1], shape, layer.dtype, layer.device)
+
+
+def mt_attn_append(layer: Attn, q, k, v, q_out, lens, table, k_pages, v_pages, *, n_new=None, stream=None):
+    """q, q_out [B, S, Hq*Dh], k, v [B, S, Hk*Dh]; lens, n_new [B], table [B, n_blocks] int32."""
+    t, dev = layer.dtype, layer.device
+    B, S = lead = q.shape[:-1]
+    nb = table.shape[1]
+    qp, ldq = _rows(q, "q", lead + (layer.QD,), t, dev)
+    kp, ldk = _rows(k, "k", lead + (layer.KD,), t, dev)
+    vp, ldv = _rows(v, "v", lead + (layer.KD,), t, dev)
+    op, ldo = _rows(q_out, "q_out", lead + (layer.QD,), t, dev)
+    _, n, kc, vc = _cache(layer, k_pages, v_pages, 0)
+    _check(lib().mt_attn_append(layer.handle, B, S, _packed(n_new, "n_new", (B,), layer.i32, dev),
+                                _packed(lens, "lens", (B,), layer.i32, dev), qp, ldq, kp, ldk, vp, ldv, op, ldo,
+                                _packed(table, "table", (B, nb), layer.i32, dev), nb, n, kc, vc, _stream_on(stream, dev)))
+
+
+def mt_attn_paged(layer: Attn, q, lens, table, k_pages, v_pages, y, *, n_new=None, ws, stream=None):
+    """q, y [B, S, Hq*Dh]; lens, n_new [B], table [B, n_blocks] int32."""
+    t, dev = layer.dtype, layer.device
+    B, S = lead = q.shape[:-1]
+    nb, rows = table.shape[1], lead + (layer.QD,)
+    qp, ldq = _rows(q, "q", rows, t, dev)
+    yp, ldy = _rows(y, "y", rows, t, dev)
+    _, n, kc, vc = _cache(layer, k_pages, v_pages, 0)
+    _check(lib().mt_attn_paged(layer.handle, B, S, _packed(n_new, "n_new", (B,), layer.i32, dev),
+                               _packed(lens, "lens", (B,), layer.i32, dev), qp, ldq,
+                               _packed(table, "table", (B, nb), layer.i32, dev), nb, n, kc, vc, yp, ldy,
+                               *_space(ws, dev), _stream_on(stream, dev)))
+
+
+def mt_attn_cross(layer: Attn, q, k, v, y, *, mask=None, n_q=None, ws, stream=None):
+    """q, y [B, T, Hq*Dh]; k, v [B, S, Hk*Dh]; mask [B, S] fp32, n_q [B] int32."""
+    t, dev = layer.dtype, layer.device
+    B, T = lead = q.shape[:-1]
+    S = k.shape[1]
+    qp, ldq = _rows(q, "q", lead + (layer.QD,), t, dev)
+    kp, ldk = _rows(k, "k", (B, S, layer.KD), t, dev)
+    vp, ldv = _rows(v, "v", (B, S, layer.KD), t, dev)
+    yp, ldy = _rows(y, "y", lead + (layer.QD,), t, dev)
+    _check(lib().mt_attn_cross(layer.handle, B, T, _packed(n_q, "n_q", (B,), layer.i32, dev), S,
+                               _packed(mask, "mask", (B, S), layer.f32, dev), qp, ldq, kp, ldk, vp, ldv, yp, ldy,
+                               *_space(ws, dev), _stream_on(stream, dev)))
+
+
+def mt_pages_advance(layer: Attn, src_row, add, table_in, len_in, table_out, len_out, k_pages, v_pages, *, free_out=None,
+                     ws, stream=None):
+    """src_row, add [M] int32 (or None); table_in [M_in, n_blocks], len_in [M_in]; table_out [M, n_blocks], len_out [M];
+    k_pages, v_pages [layers, n_pages, Hk, page, Dh]; free_out [1] int32."""
+    dev, i32 = layer.device, layer.i32
+    Mi, nb = table_in.shape
+    M = table_out.shape[0]
+    layers, n, kc, vc = _cache(layer, k_pages, v_pages, 1)
+    _check(lib().mt_pages_advance(layer.handle, Mi, M, _packed(src_row, "src_row", (M,), i32, dev),
+                                  _packed(add, "add", (M,), i32, dev), _packed(table_in, "table_in", (Mi, nb), i32, dev),
+                                  _packed(len_in, "len_in", (Mi,), i32, dev), nb, n,
+                                  _packed(table_out, "table_out", (M, nb), i32, dev),
+                                  _packed(len_out, "len_out", (M,), i32, dev), _packed(free_out, "free_out", (1,), i32, dev),
+                                  layers, kc, vc, *_space(ws, dev), _stream_on(stream, dev)))
+
+
+def mt_pages_pack(layer: Attn, table_in, len_in, k_in, v_in, table_out, len_out, k_out, v_out, used_out=None, *, ws,
+                  stream=None):
+    """table_in, table_out [M, n_blocks], len_in, len_out [M], used_out [1] int32; k_in, v_in [layers, n_pages, Hk, page,
+    Dh], k_out, v_out the same with their own number of pages."""
+    dev, i32 = layer.device, layer.i32
+    M, nb = table_in.shape
+    layers, n, ki, vi = _cache(layer, k_in, v_in, 1, ("k_in", "v_in"))
+    lo, no, ko, vo = _cache(layer, k_out, v_out, 1, ("k_out", "v_out"))
+    if lo != layers:
+        raise ValueError("the two caches must have the same number of layers")
+    _check(lib().mt_pages_pack(layer.handle, M, _packed(table_in, "table_in", (M, nb), i32, dev),
+                               _packed(len_in, "len_in", (M,), i32, dev), nb, n, layers, ki, vi, no,
+                               _packed(table_out, "table_out", (M, nb), i32, dev),
+                               _packed(len_out, "len_out", (M,), i32, dev), _packed(used_out, "used_out", (1,), i32, dev),
+                               ko, vo, *_space(ws, dev), _stream_on(stream, dev)))

@@ -1,0 +1,432 @@
+"""The attention layer's operators on the GPU against plain 64-bit implementations (attn_ref), within the bounds
+derived there: fp32 arithmetic, softmax weights in bf16 for a bf16 layer, plus half a step of the output's type."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import attn_ref as ref
+from paper_1804_00344_amd import mtstep as mt
+from test_gpu_layer import DEV, IO, check, dev, gen, wide
+
+pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
+
+HALF = {"f32": 0.0, "bf16": 2.0 ** -8}  # of the softmax weights
+NAN = float("nan")
+
+
+def layer(Hq, Hk, Dh, dtype, weights=None, **kw):
+    return mt.mt_attn_load(mt.make_attn_config(Hq, Hk, Dh, dtype=dtype, **kw), weights)
+
+
+def space(n):
+    assert n > 0
+    return torch.empty(n, dtype=torch.uint8, device=DEV)
+
+
+def pages_for(lens, page, n_blocks, g, spare=3, junk=-9):
+    """A table of own pages in random order, junk behind each row's blocks; the number of pages."""
+    blocks = [-(-n // page) for n in lens]
+    order = torch.randperm(sum(blocks) + spare, generator=g).tolist()
+    table = torch.full((len(lens), n_blocks), junk, dtype=torch.int32)
+    for b, nb in enumerate(blocks):
+        for j in range(nb):
+            table[b, j] = order.pop()
+    return table, sum(blocks) + spare
+
+
+def fill_cache(table, lens, page, Hk, Dh, n_pages, dtype, g, fill=NAN):
+    """(k rows, v rows [L, Hk*Dh] per sequence, caches); what no length covers holds fill."""
+    kc, vc = (torch.full((n_pages, Hk, page, Dh), fill, dtype=IO[dtype]) for _ in range(2))
+    ks, vs = [], []
+    for b, n in enumerate(lens):
+        k, v = (torch.randn(n, Hk * Dh, generator=g).to(IO[dtype]) for _ in range(2))
+        for t, c in ((k, kc), (v, vc)):
+            for j in range(0, n, page):
+                part = t[j:j + page].reshape(-1, Hk, Dh)
+                c[table[b, j // page], :, :part.shape[0]] = part.transpose(0, 1)
+        ks.append(k)
+        vs.append(v)
+    return ks, vs, kc, vc
+
+
+def run_paged(a, q, lens, table, kc, vc, n_new=None, y=None, stream=None):
+    B, S, W = q.shape
+    y = torch.full((B, S, W), 7.0, dtype=q.dtype, device=DEV) if y is None else y
+    ws = space(mt.mt_attn_workspace_bytes(a, B, S, table.shape[1] * a.cfg.page))
+    ws.fill_(255)  # NaN where nothing is written
+    mt.mt_attn_paged(a, q, dev(torch.tensor(lens, dtype=torch.int32)), dev(table), dev(kc), dev(vc), y,
+                     n_new=None if n_new is None else dev(torch.tensor(n_new, dtype=torch.int32)), ws=ws, stream=stream)
+    return y
+
+
+PAGED = [  # B, S, Hq, Hk, Dh, page, window, lens, n_new
+    (1, 1, 1, 1, 8, 8, 0, [1], None),
+    (3, 1, 4, 4, 64, 16, 0, [1, 0, 33], None),
+    (3, 1, 6, 3, 40, 8, 0, [100, 7, 8], [1, 0, 1]),
+    (2, 1, 8, 1, 128, 16, 0, [700, 1], None),
+    (2, 1, 32, 1, 128, 64, 0, [1500, 64], None),
+    (2, 1, 40, 1, 64, 32, 0, [257, 300], None),
+    (2, 1, 8, 2, 256, 256, 0, [300, 256], None),
+    (1, 1, 2, 1, 72, 16, 0, [4100], None),
+    (5, 1, 4, 2, 64, 16, 20, [19, 20, 21, 200, 64], None),
+    (2, 3, 4, 2, 64, 16, 0, [3, 40], None),
+    (2, 3, 4, 2, 96, 16, 0, [2, 0], [3, 3]),  # fewer positions than new ones: the first queries see nothing
+    (4, 17, 4, 2, 64, 16, 0, [17, 50, 5, 130], [17, 0, 5, 16]),
+    (2, 61, 6, 3, 40, 8, 50, [61, 333], [61, 40]),
+    (2, 70, 2, 1, 128, 16, 0, [70, 200], [70, 69]),
+    (1, 200, 4, 4, 64, 16, 0, [200], None),
+    (1, 130, 3, 1, 136, 32, 0, [515], None),
+    (1, 65, 2, 2, 256, 16, 3, [129], None),
+    (2, 33, 16, 2, 128, 128, 0, [129, 33], [32, 33]),
+    (2, 300, 2, 1, 64, 16, 1, [300, 700], [300, 299]),
+    (1, 12, 3, 3, 200, 64, 0, [2000], None),
+    (1, 256, 4, 2, 128, 64, 100, [1024], None),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", PAGED, ids=lambda c: "-".join(str(v) for v in c[:7]))
+def test_paged(case, dtype):
+    B, S, Hq, Hk, Dh, page, window, lens, n_new = case
+    g = gen(B * S + Dh)
+    nb = -(-max(max(lens), 1) // page) + 2
+    table, n_pages = pages_for(lens, page, nb, g)
+    ks, vs, kc, vc = fill_cache(table, lens, page, Hk, Dh, n_pages, dtype, g)
+    a = layer(Hq, Hk, Dh, dtype, page=page, window=window)
+    q = (torch.randn(B, S, Hq * Dh, generator=g) * 1.5).to(IO[dtype])
+    new = n_new or [S] * B
+    for b in range(B):
+        q[b, new[b]:] = NAN  # behind the new positions: never read
+    y = run_paged(a, dev(q), lens, table, kc, vc, n_new)
+    assert mt.mt_attn_device_errors(a) == 0
+    for b in range(B):
+        n, L = new[b], lens[b]
+        want, err = ref.heads(q[b, :n].double(), ks[b].double(), vs[b].double(), ref.causal(L - n, n, L, window), Hq, Hk,
+                              1 / math.sqrt(Dh), HALF[dtype])
+        check(y[b, :n], want, err, (b, "y"))
+        assert bool((y[b, n:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("S,L,window", [(1, 90, 40), (5, 90, 0), (5, 90, 40), (80, 150, 0), (80, 150, 30)])
+def test_unseen_nonfinite_values_have_no_part(S, L, window, dtype):
+    """Infinities and NaN at positions that a query does not see: later ones, and those before the window."""
+    Hq, Hk, Dh, page = 4, 2, 64, 16
+    g = gen(S + window)
+    a = layer(Hq, Hk, Dh, dtype, page=page, window=window)
+    table, n_pages = pages_for([L], page, 12, g)
+    ks, vs, kc, vc = fill_cache(table, [L], page, Hk, Dh, n_pages, dtype, g)
+    bad = {L - 1: NAN, L - S // 2 - 1: float("inf"), L - S - 3: float("-inf"), L - S - window: NAN}
+    if S == 1:
+        bad = {L - window - 1: NAN, L - window - 2: float("inf"), 0: NAN}
+    if S == 5 and not window:
+        bad = {L - 1: NAN, L - 2: float("inf")}
+    if S == 80 and not window:
+        bad = {L - 1: NAN, L - 40: float("inf"), L - 41: float("-inf")}
+    for j, x in bad.items():
+        for t, c in ((ks[0], kc), (vs[0], vc)):
+            t[j, 3:9] = x
+            c[table[0, j // page], 0, j % page, 3:9] = x
+    q = torch.randn(1, S, Hq * Dh, generator=g).to(IO[dtype])
+    y = run_paged(a, dev(q), [L], table, kc, vc)[0].cpu().double()
+    for i in range(S):
+        p = L - S + i
+        lo = max(0, p + 1 - window) if window else 0
+        dirty = any(lo <= j <= p for j in bad)
+        sl = slice(lo, p + 1)
+        if dirty:  # the heads of key head 0 hold what the formula gives: no numbers
+            assert not bool(torch.isfinite(y[i, :Dh]).all())
+            h0 = Hq // Hk * Dh  # key head 1 is clean
+        else:
+            h0 = 0
+        want, err = ref.heads(q[0, i:i + 1].double(), torch.nan_to_num(ks[0][sl].double()), torch.nan_to_num(vs[0][sl].double()),
+                              torch.ones(1, p + 1 - lo, dtype=torch.bool), Hq, Hk, 1 / math.sqrt(Dh), HALF[dtype])
+        tol = err + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * want.abs() + 1e-37
+        assert bool(((y[i:i + 1] - want).abs() <= tol)[:, h0:].all()), i
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("S", [1, 40])
+def test_all_scores_minus_infinity_gives_zeros(S, dtype):
+    a = layer(2, 1, 64, dtype)
+    table, n_pages = pages_for([40], 16, 3, gen(1))
+    _, _, kc, vc = fill_cache(table, [40], 16, 1, 64, n_pages, dtype, gen(2))
+    kc[:] = 0
+    kc[..., 0] = float("-inf")
+    q = torch.ones(1, S, 128).to(IO[dtype])
+    assert bool((run_paged(a, dev(q), [40], table, kc, vc) == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [1e-30, 1e4])
+def test_small_and_large_scores(size, dtype):
+    """Equal weights, and weights of one key: scores of +-1e8 keep the softmax exact."""
+    a = layer(2, 2, 64, dtype)
+    g = gen(3)
+    table, n_pages = pages_for([77], 16, 5, g)
+    ks, vs, kc, vc = fill_cache(table, [77], 16, 2, 64, n_pages, dtype, g)
+    q = (torch.randn(1, 50, 128, generator=g).sign() * size).to(IO[dtype])
+    kc, ks[0] = kc.sign(), ks[0].sign()
+    if size > 1:  # sums of 64 signs: one key first by far
+        kc[:], ks[0][:] = -kc.abs(), -ks[0].abs()
+        kc[table[0, 0], :, 5], ks[0][5] = 1, 1
+        q = q.abs()
+    y = run_paged(a, dev(q), [77], table, kc, vc)
+    want, err = ref.heads(q[0].double(), ks[0].double(), vs[0].double(), ref.causal(27, 50, 77, 0), 2, 2, 0.125, HALF[dtype])
+    check(y[0], want, torch.where(want == want, err.clamp(max=1.0), err) * (size < 1) + 1e-6, "y")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("S", [1, 40])
+@pytest.mark.parametrize("shift", [0, 1, 3, 8])
+def test_rows_of_wider_matrices(shift, S, dtype):
+    """Rows that start at any element, read and written, are the aligned ones to the bit."""
+    a = layer(4, 2, 64, dtype)
+    g = gen(7)
+    table, n_pages = pages_for([70, 45], 16, 5, g)
+    _, _, kc, vc = fill_cache(table, [70, 45], 16, 2, 64, n_pages, dtype, g)
+    q = torch.randn(2, S, 256, generator=g).to(IO[dtype])
+    y = run_paged(a, dev(q), [70, 45], table, kc, vc)
+    big = torch.full((2, S, 256 + shift + 3), 7.0, dtype=q.dtype, device=DEV)
+    run_paged(a, wide(q, shift, 2), [70, 45], table, kc, vc, y=big[..., shift:shift + 256])
+    assert torch.equal(big[..., shift:shift + 256], y)
+    assert bool((big[..., :shift] == 7).all()) and bool((big[..., shift + 256:] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_lengths_and_pages_out_of_range_are_clamped(dtype):
+    a = layer(4, 2, 64, dtype)
+    g = gen(8)
+    table, n_pages = pages_for([64, 64, 64], 16, 4, g)
+    ks, vs, kc, vc = fill_cache(table, [64, 64, 64], 16, 2, 64, n_pages, dtype, g, fill=0.0)
+    for S in (1, 30):
+        q = dev(torch.randn(3, S, 256, generator=g).to(IO[dtype]))
+        y = run_paged(a, q, [1000, -5, 64], table, kc, vc, [S, S, S + 5])
+        assert mt.mt_attn_device_errors(a) == 2 and mt.mt_attn_device_errors(a) == 0
+        want = run_paged(a, q, [64, 0, 64], table, kc, vc)
+        assert torch.equal(y, want) and bool((y[1] == 0).all())
+        t2, t3 = table.clone(), table.clone()
+        t2[0, 1], t2[2, 3] = -3, n_pages + 2
+        t3[0, 1], t3[2, 3] = 0, n_pages - 1
+        y = run_paged(a, q, [64, 64, 64], t2, kc, vc)
+        assert mt.mt_attn_device_errors(a) == 4
+        assert torch.equal(y, run_paged(a, q, [64, 64, 64], t3, kc, vc)) and mt.mt_attn_device_errors(a) == 0
+
+
+@pytest.mark.parametrize("S", [1, 40])
+def test_a_cache_past_32_bits(S):
+    """Pages whose first byte lies beyond 2^32 bytes and 2^31 elements."""
+    Hk, Dh, page = 8, 128, 64
+    n_pages = 2 ** 33 // (Hk * Dh * page * 2) + 40  # 8 GiB each
+    a = layer(8, Hk, Dh, "bf16", page=page)
+    g = gen(9)
+    L = 200
+    small = torch.arange(4, dtype=torch.int32)[None]
+    ks, vs, kc, vc = fill_cache(small, [L], page, Hk, Dh, 4, "bf16", g)
+    k, v = (torch.empty(n_pages, Hk, page, Dh, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    at = [n_pages - 1, 2 ** 31 // (Hk * Dh * page) + 1, 3, n_pages - 7]
+    for i, p in enumerate(at):
+        k[p], v[p] = dev(kc[i]), dev(vc[i])
+    q = torch.randn(1, S, 8 * Dh, generator=g).bfloat16()
+    y = run_paged(a, dev(q), [L], torch.tensor([at], dtype=torch.int32), k, v)
+    assert torch.equal(y, run_paged(a, dev(q), [L], small, kc, vc))
+    # and stored there
+    kn, vn = (torch.randn(1, S, Hk * Dh, generator=g).bfloat16().to(DEV) for _ in range(2))
+    mt.mt_attn_append(a, dev(q), kn, vn, torch.empty_like(dev(q)), dev(torch.tensor([S], dtype=torch.int32)),
+                      dev(torch.tensor([at], dtype=torch.int32)), k, v)
+    assert torch.equal(k[at[0], :, :S], kn.reshape(S, Hk, Dh).transpose(0, 1))
+    assert torch.equal(v[at[0], :, :S], vn.reshape(S, Hk, Dh).transpose(0, 1))
+
+
+# ---- cross attention ----------------------------------------------------------------------------
+
+def run_cross(a, q, k, v, mask=None, n_q=None, y=None):
+    B, T, W = q.shape
+    y = torch.full((B, T, W), 7.0, dtype=q.dtype, device=DEV) if y is None else y
+    ws = space(mt.mt_attn_workspace_bytes(a, B, T, k.shape[1]))
+    ws.fill_(255)
+    mt.mt_attn_cross(a, q, k, v, y, mask=dev(mask), n_q=None if n_q is None else dev(torch.tensor(n_q, dtype=torch.int32)), ws=ws)
+    return y
+
+
+CROSS = [  # B, T, S, Hq, Hk, Dh, mask, n_q
+    (1, 1, 1, 1, 1, 8, None, None), (2, 1, 5, 2, 2, 64, "holes", None), (3, 5, 80, 8, 8, 64, "ends", None),
+    (4, 12, 33, 4, 2, 40, "holes", [12, 0, 5, 12]), (2, 7, 97, 6, 2, 72, "holes", None), (2, 40, 130, 2, 1, 128, "ends", None),
+    (2, 100, 64, 4, 4, 64, "holes", [100, 33]), (1, 3, 1030, 4, 1, 128, "ends", None), (2, 65, 257, 3, 3, 256, "holes", None),
+    (1, 150, 300, 16, 2, 64, None, None), (2, 1, 300, 40, 1, 96, "holes", None)]
+
+
+def make_mask(kind, B, S, g):
+    if kind is None:
+        return None
+    if kind == "ends":
+        n = torch.randint(1, S + 1, (B,), generator=g)
+        n[0] = S
+        if B > 1:
+            n[-1] = 1
+        return (torch.arange(S)[None] < n[:, None]).float()
+    m = (torch.rand(B, S, generator=g) < 0.6).float() * 2.5  # any value but zero is a valid position
+    m[0, :S // 2] = 0
+    if B > 1:
+        m[1] = 0  # a sentence without positions
+    return m
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", CROSS, ids=lambda c: "-".join(str(v) for v in c[:7]))
+def test_cross(case, dtype):
+    B, T, S, Hq, Hk, Dh, kind, n_q = case
+    g = gen(T * S)
+    a = layer(Hq, Hk, Dh, dtype, scale=0.3)
+    q = torch.randn(B, T, Hq * Dh, generator=g).to(IO[dtype])
+    kv = torch.randn(B, S, 2 * Hk * Dh + 5, generator=g).to(IO[dtype])
+    mask = make_mask(kind, B, S, g)
+    if mask is not None:
+        kv[mask == 0] = NAN
+    w = Hk * Dh
+    both = dev(kv)
+    n = n_q or [T] * B
+    for b in range(B):
+        q[b, n[b]:] = NAN
+    y = run_cross(a, dev(q), both[..., 5:5 + w], both[..., 5 + w:], mask, n_q)
+    assert mt.mt_attn_device_errors(a) == 0
+    for b in range(B):
+        seen = torch.ones(n[b], S, dtype=torch.bool) if mask is None else (mask[b] != 0)[None].expand(n[b], -1)
+        want, err = ref.heads(q[b, :n[b]].double(), kv[b, :, 5:5 + w].double(), kv[b, :, 5 + w:].double(), seen, Hq, Hk, 0.3,
+                              HALF[dtype])
+        check(y[b, :n[b]], want, err, (b, "y"))
+        assert bool((y[b, n[b]:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [4, 60])
+def test_cross_at_any_alignment(T, dtype):
+    g = gen(11)
+    a = layer(4, 2, 64, dtype)
+    q, k, v = (torch.randn(2, n, w, generator=g).to(IO[dtype]) for n, w in ((T, 256), (90, 128), (90, 128)))
+    want = run_cross(a, dev(q), dev(k), dev(v))
+    for s in (1, 2, 4):
+        assert torch.equal(run_cross(a, wide(q, s, 1), wide(k, s, 2), wide(v, s + 1, 0)), want)
+
+
+def test_cross_equals_paged_of_one_position():
+    """One query over all keys is the same operator on both sides."""
+    g = gen(12)
+    a = layer(4, 4, 64, "f32")
+    table, n_pages = pages_for([90], 16, 6, g)
+    ks, vs, kc, vc = fill_cache(table, [90], 16, 4, 64, n_pages, "f32", g)
+    q = torch.randn(1, 1, 256, generator=g)
+    y1, y2 = run_paged(a, dev(q), [90], table, kc, vc), run_cross(a, dev(q), dev(ks[0][None]), dev(vs[0][None]))
+    assert float((y1 - y2).abs().max()) < 1e-5
+
+
+# ---- norms, rotation, store ---------------------------------------------------------------------
+
+APPEND = [  # B, S, Hq, Hk, Dh, page, norm, rot, pairs, lens, n_new
+    (1, 1, 1, 1, 8, 8, True, 8, False, [1], None),
+    (3, 1, 4, 4, 64, 16, False, 64, False, [5, 0, 100], [1, 0, 1]),
+    (2, 7, 6, 3, 40, 8, True, 34, False, [7, 50], [7, 5]),
+    (2, 7, 6, 3, 40, 8, True, 18, True, [3, 50], [7, 5]),  # more new positions than there are
+    (2, 30, 8, 2, 128, 64, True, 128, False, [30, 100000], None),
+    (1, 20, 3, 1, 256, 256, True, 256, True, [20], None),
+    (1, 20, 2, 2, 200, 32, False, 0, False, [40], None),
+    (2, 33, 16, 4, 72, 16, True, 72, False, [33, 40], [33, 0]),
+    (1, 5000, 2, 1, 64, 16, True, 32, False, [70000], None),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", APPEND, ids=lambda c: "-".join(str(v) for v in c[:9]))
+def test_append(case, dtype):
+    B, S, Hq, Hk, Dh, page, norm, rot, pairs, lens, n_new = case
+    g = gen(S + Dh)
+    new = n_new or [S] * B
+    nb = -(-max(lens) // page) + 1
+    table = torch.full((B, nb), -1, dtype=torch.int32)  # pages for the new positions alone
+    at = 0
+    for b in range(B):
+        for j in range(max(0, lens[b] - new[b]) // page, -(-lens[b] // page) if new[b] else 0):
+            table[b, j], at = at, at + 1
+    n_pages = at + 2
+    gains = dict(gq=1 + 0.2 * torch.randn(Dh, generator=g), gk=1 + 0.2 * torch.randn(Dh, generator=g))
+    if not norm:
+        gains = {}
+    freq = 10000.0 ** (-torch.arange(0, rot, 2, dtype=torch.float64) / max(1, rot))
+    if pairs:  # frequencies of the program's own
+        freq = (freq * 0.37).float().double()
+        gains["freq"] = freq
+    a = layer(Hq, Hk, Dh, dtype, gains, page=page, qk_norm=norm, rot=rot, rot_pairs=pairs)
+    qkv = (torch.randn(B, S, (Hq + 2 * Hk) * Dh, generator=g) * torch.exp(torch.randn(B, S, 1, generator=g))).to(IO[dtype])
+    kc, vc = (torch.full((n_pages, Hk, page, Dh), 7.0, dtype=IO[dtype]) for _ in range(2))
+    for b in range(B):
+        qkv[b, new[b]:] = NAN
+    x = wide(qkv, 3, 2)
+    wq, wk = Hq * Dh, Hk * Dh
+    out = torch.full((B, S, wq), 7.0, dtype=IO[dtype], device=DEV)
+    k2, v2 = dev(kc), dev(vc)
+    ln = dev(torch.tensor(lens, dtype=torch.int32))
+    nn = None if n_new is None else dev(torch.tensor(n_new, dtype=torch.int32))
+    mt.mt_attn_append(a, x[..., :wq], x[..., wq:wq + wk], x[..., wq + wk:], out, ln, dev(table), k2, v2, n_new=nn)
+    assert mt.mt_attn_device_errors(a) == 0
+    kw, vw, ke = kc.double(), vc.clone(), torch.zeros_like(kc, dtype=torch.float64)
+    for b in range(B):
+        n = new[b]
+        pos = torch.arange(lens[b] - n, lens[b])
+        rows = qkv[b, :n].double()
+        live = (pos >= 0)[:, None]
+        gq, gk = (gains.get(k, torch.ones(Dh)).double() for k in ("gq", "gk"))
+        want, err = ref.turn_heads(rows[:, :wq], pos, Dh, norm, 1e-6, gq, rot, pairs, freq)
+        check(out[b, :n], torch.where(live, want, 0.0), err, "q")
+        assert bool((out[b, n:] == 7.0).all())
+        want, err = ref.turn_heads(rows[:, wq:wq + wk], pos, Dh, norm, 1e-6, gk, rot, pairs, freq)
+        for i in range(n):
+            p = int(pos[i])
+            if p < 0:
+                continue
+            pg, off = int(table[b, p // page]), p % page
+            kw[pg, :, off], ke[pg, :, off] = want[i].reshape(Hk, Dh), err[i].reshape(Hk, Dh)
+            vw[pg, :, off] = qkv[b, i, wq + wk:].reshape(Hk, Dh)
+    check(k2, kw, ke, "k")  # the positions that are not new as they were
+    assert torch.equal(v2.cpu(), vw)
+    # in place, to the bit
+    x2 = x.clone()
+    k3, v3 = dev(kc), dev(vc)
+    mt.mt_attn_append(a, x2[..., :wq], x2[..., wq:wq + wk], x2[..., wq + wk:], x2[..., :wq], ln, dev(table), k3, v3, n_new=nn)
+    for b in range(B):
+        assert torch.equal(x2[b, :new[b], :wq], out[b, :new[b]])
+    assert torch.equal(k3, k2) and torch.equal(v3, v2)
+
+
+def test_append_far_position():
+    """Angles at positions near 2^30 keep their digits: 2^-21 of a turn (two roundings of 2^30 / 2 pi turns in 64 bits)."""
+    Dh, page = 64, 256
+    a = layer(1, 1, Dh, "f32", page=page, rot=Dh)
+    L = 2 ** 30 - 5
+    nb = 2 ** 30 // page
+    table = torch.zeros(1, nb, dtype=torch.int32, device=DEV)
+    g = gen(5)
+    q, k, v = (torch.randn(1, 3, Dh, generator=g) for _ in range(3))
+    kc, vc = (torch.zeros(1, 1, page, Dh, device=DEV) for _ in range(2))
+    out = torch.empty(1, 3, Dh, device=DEV)
+    mt.mt_attn_append(a, dev(q), dev(k), dev(v), out, dev(torch.tensor([L], dtype=torch.int32)), table, kc, vc)
+    freq = 10000.0 ** (-torch.arange(0, Dh, 2, dtype=torch.float64) / Dh)
+    want, err = ref.turn_heads(q[0].double(), torch.arange(L - 3, L), Dh, False, 0, None, Dh, False, freq)
+    pair = (q[0].double().reshape(3, 2, -1).abs().sum(1)).repeat(1, 2)
+    check(out[0], want, err + pair * 2 * math.pi * 2.0 ** -21, "q")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_append_out_of_range(dtype):
+    a = layer(2, 1, 64, dtype)
+    g = gen(6)
+    q, k, v = (dev(torch.randn(2, 3, w, generator=g).to(IO[dtype])) for w in (128, 64, 64))
+    kc, vc = (torch.zeros(3, 1, 16, 64, dtype=IO[dtype], device=DEV) for _ in range(2))
+    table = dev(torch.tensor([[0, 9], [1, -4]], dtype=torch.int32))
+    out = torch.zeros_like(q)
+    mt.mt_attn_append(a, q, k, v, out, dev(torch.tensor([16, 99], dtype=torch.int32)), table, kc, vc)
+    assert mt.mt_attn_device_errors(a) == 2 | 4  # 99 positions of 32; page -4
+    mt.mt_attn_append(a, q, k, v, out, dev(torch.tensor([17, 16], dtype=torch.int32)), table, kc, vc)
+    assert mt.mt_attn_device_errors(a) == 4
+    assert torch.equal(vc[2, 0, 0], v[0, 2])  # page 9 of 3: the last one

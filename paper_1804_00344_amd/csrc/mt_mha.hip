@@ -1,41 +1,76 @@
 // Attention of query heads over keys and values in pages of a cache, or in rows of another length under a mask:
 //   y = sum_j softmax_j(scale q.k_j) v_j over the keys that a query sees.
-#include "mt_mha_dev.h"
+// Here: how a call is split over the chip, and the join of the parts of a key axis that is cut.
+#include "mt_mha_tile.h"
 
 namespace mt {
 
 namespace {
 
-// A wave per query and head: right for every case.
-template <typename T, bool PAGED>
-__global__ void __launch_bounds__(256) plain_kernel(MhaArgs a) {
-  __shared__ float qs[4][256];
-  const int wave = threadIdx.x >> 6;
-  const long long steps = (long long)a.S * a.Hq;
-  const long long u = blockIdx.x * 4ll + wave;
-  if (u >= steps) return;
-  const int i = (int)(u / a.Hq), hq = (int)(u % a.Hq);
-  for (int b = blockIdx.y; b < a.B; b += gridDim.y) {
-    const RowSpan r = row_span<PAGED>(a, b, u == 0 && (threadIdx.x & 63) == 0);
-    if (i < r.n) attend_one<T, PAGED>(a, r, b, i, hq, qs[wave]);
-  }
+struct Plan {
+  TilePlan tile;
+};
+
+Plan plan_of(int Hq, int Hk, int B, int S, long long n_keys, int num_cu) {
+  Plan p;
+  const long long rows = (long long)S * (Hq / Hk);
+  p.tile.tiles = (int)((rows + kTileRows - 1) / kTileRows);
+  // two workgroups a unit; a part of 256 keys at least
+  const long long wgs = (long long)B * Hk * p.tile.tiles, want = 2 * num_cu / wgs, most = n_keys / 256;
+  p.tile.parts = (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
+  return p;
 }
 
-template <typename T, bool PAGED>
-hipError_t run(const MhaArgs &a, hipStream_t st) {
-  const long long steps = (long long)a.S * a.Hq;
-  hipLaunchKernelGGL((plain_kernel<T, PAGED>), dim3((unsigned)((steps + 3) / 4), (unsigned)(a.B < 32768 ? a.B : 32768)),
-                     dim3(256), 0, st, a);
-  return hipGetLastError();
+// The parts of a row together: sums relative to the largest of the parts' maxima.  A wave per row.
+template <typename T>
+__global__ void __launch_bounds__(256) join_kernel(MhaArgs a, int n_parts) {
+  const long long rows = (long long)a.B * a.Hq * a.S;
+  const long long row = blockIdx.x * 4ll + (threadIdx.x >> 6);
+  if (row >= rows) return;
+  const int lane = threadIdx.x & 63;
+  const long long per = (long long)a.S * a.G, bh = row / per;
+  const int rr = (int)(row - bh * per), i = rr / a.G, b = (int)(bh / a.Hk), hq = (int)(bh - (long long)b * a.Hk) * a.G + rr - i * a.G;
+  const int n0 = a.n_new ? a.n_new[b] : a.S;
+  // the parts hold a sequence's rows one after the other: those of its n queries
+  if (i >= min(max(n0, 0), a.S)) return;
+  const Parts p = parts_of(a.ws, rows, n_parts);
+  float m = kNegInf;
+  for (int s = 0; s < n_parts; ++s) m = fmaxf(m, p.ml[s * rows + row].x);
+  const float use = m == kNegInf ? 0.f : m;
+  float l = 0.f, acc[4] = {};
+  for (int s = 0; s < n_parts; ++s) {
+    const float2 ml = p.ml[s * rows + row];
+    if (ml.y == 0.f) continue;  // nothing seen
+    const float c = ml.x == kNegInf ? 1.f : __builtin_amdgcn_exp2f(ml.x - use);
+    l = fmaf(ml.y, c, l);
+#pragma unroll
+    for (int f = 0; f < 4; ++f)
+      if (lane + 64 * f < a.Dh) acc[f] = fmaf(p.o[(s * rows + row) * a.Dh + lane + 64 * f], c, acc[f]);
+  }
+  T *y = (T *)a.y + ((long long)b * a.S + i) * a.ldy + (long long)hq * a.Dh;
+#pragma unroll
+  for (int f = 0; f < 4; ++f)
+    if (lane + 64 * f < a.Dh) Store<T>::put(y + lane + 64 * f, l == 0.f ? 0.f : acc[f] / l);
 }
 
 }  // namespace
 
-size_t mha_workspace_bytes(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int num_cu) { return 256; }
+size_t mha_workspace_bytes(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int num_cu) {
+  const Plan p = plan_of(Hq, Hk, B, S, n_keys, num_cu);
+  return p.tile.parts > 1 ? (parts_bytes((long long)B * Hq * S, p.tile.parts, Dh) + 255) / 256 * 256 : 256;
+}
 
 hipError_t launch_mha(const MhaArgs &a, hipStream_t st) {
-  if (a.table) return a.bf16_io ? run<bf16, true>(a, st) : run<float, true>(a, st);
-  return a.bf16_io ? run<bf16, false>(a, st) : run<float, false>(a, st);
+  const Plan p = plan_of(a.Hq, a.Hk, a.B, a.S, a.table ? (long long)a.n_blocks << a.page_log2 : a.Sk, a.num_cu);
+  hipError_t e = a.bf16_io ? launch_tiles_bf16(a, p.tile, st) : launch_tiles_f32(a, p.tile, st);
+  if (e != hipSuccess || p.tile.parts == 1) return e;
+  const long long rows = (long long)a.B * a.Hq * a.S;
+  const dim3 grid((unsigned)((rows + 3) / 4));
+  if (a.bf16_io)
+    hipLaunchKernelGGL(join_kernel<bf16>, grid, dim3(256), 0, st, a, p.tile.parts);
+  else
+    hipLaunchKernelGGL(join_kernel<float>, grid, dim3(256), 0, st, a, p.tile.parts);
+  return hipGetLastError();
 }
 
 }  // namespace mt

@@ -58,10 +58,28 @@ __device__ __forceinline__ long long key_at(const MhaArgs &a, int b, int h, int 
   return ((long long)b * a.Sk + j) * ld + h * a.Dh;
 }
 
-// One query head of one query by one wave: 64 keys at a time, a key per lane for the scores (running maximum and sum
-// in 32 bits), a feature per lane for the values.  qs: 256 floats of LDS of the wave.  A key that is not seen is not read.
+// Where a call's parts of a result go that the key axis is cut for: part s of row (b*Hk + h)*S*G + i*G + g holds the
+// sums of its keys, the maximum that they are relative to and their weights' sum (both halves of a pair)
+struct Parts {
+  float *o;   // [parts][rows][Dh]
+  float2 *ml; // [parts][rows]
+};
+__host__ __device__ inline Parts parts_of(void *ws, long long rows, int parts) {
+  Parts p;
+  p.ml = (float2 *)ws;
+  p.o = (float *)ws + ((rows * parts * 2 + 63) & ~63ll);
+  return p;
+}
+inline size_t parts_bytes(long long rows, int parts, int Dh) {
+  return (size_t)(((rows * parts * 2 + 63) & ~63ll) + rows * parts * Dh) * 4;
+}
+
+// One query head of one query by one wave over its keys in [k0, k1): 64 keys at a time, a key per lane for the scores
+// (running maximum and sum in 32 bits), a feature per lane for the values.  qs: 256 floats of LDS of the wave.  A key
+// that is not seen is not read.  Gives the result, or where po is set the sums and their pair.
 template <typename T, bool PAGED>
-__device__ void attend_one(const MhaArgs &a, const RowSpan &r, int b, int i, int hq, float *qs) {
+__device__ void attend_one(const MhaArgs &a, const RowSpan &r, int b, int i, int hq, int k0, int k1, float *qs,
+                           float *po, float2 *pml) {
   constexpr int VEC = 16 / sizeof(T);
   typedef Vec<T, VEC> V;
   const int lane = threadIdx.x & 63, h = hq / a.G;
@@ -72,6 +90,8 @@ __device__ void attend_one(const MhaArgs &a, const RowSpan &r, int b, int i, int
   __builtin_amdgcn_wave_barrier();
   int lo, hi;
   seen_keys<PAGED>(a, r, i, lo, hi);
+  lo = max(lo, k0);
+  hi = min(hi, k1);
   float m = kNegInf, l = 0.f, acc[4] = {};
   for (int t = lo; t < hi; t += 64) {
     const int j = t + lane;
@@ -105,8 +125,15 @@ __device__ void attend_one(const MhaArgs &a, const RowSpan &r, int b, int i, int
   }
   T *y = (T *)a.y + row * a.ldy + (long long)hq * a.Dh;
 #pragma unroll
-  for (int f = 0; f < 4; ++f)
-    if (lane + 64 * f < a.Dh) Store<T>::put(y + lane + 64 * f, l == 0.f ? 0.f : acc[f] / l);
+  for (int f = 0; f < 4; ++f) {
+    const int d = lane + 64 * f;
+    if (d >= a.Dh) continue;
+    if (po)
+      po[d] = acc[f];
+    else
+      Store<T>::put(y + d, l == 0.f ? 0.f : acc[f] / l);
+  }
+  if (po && lane == 0) *pml = make_float2(m, l);
   __builtin_amdgcn_wave_barrier();
 }
 

@@ -42,19 +42,18 @@ __device__ __forceinline__ void seen_keys(const MhaArgs &a, const RowSpan &r, in
   }
 }
 
-// page of block j of row b (a number out of range is clamped and reported)
-__device__ __forceinline__ int block_page(const MhaArgs &a, int b, int j) {
+// page of block j of row b; a number out of range is clamped, and reported by who asks
+__device__ __forceinline__ int block_page(const MhaArgs &a, int b, int j, bool &bad) {
   const int p = a.table[(long long)b * a.n_blocks + j];
-  if ((unsigned)p < (unsigned)a.n_pages) return p;
-  atomicOr(a.err, kErrPage);
-  return p < 0 ? 0 : a.n_pages - 1;
+  bad |= (unsigned)p >= (unsigned)a.n_pages;
+  return min(max(p, 0), a.n_pages - 1);
 }
 
 // element offset of key j of row b and key head h from the cache's (or the rows') beginning
 template <bool PAGED>
-__device__ __forceinline__ long long key_at(const MhaArgs &a, int b, int h, int j, long long ld) {
+__device__ __forceinline__ long long key_at(const MhaArgs &a, int b, int h, int j, long long ld, bool &bad) {
   if (PAGED)
-    return ((((long long)block_page(a, b, j >> a.page_log2) * a.Hk + h) << a.page_log2) + (j & ((1 << a.page_log2) - 1))) * a.Dh;
+    return ((((long long)block_page(a, b, j >> a.page_log2, bad) * a.Hk + h) << a.page_log2) + (j & ((1 << a.page_log2) - 1))) * a.Dh;
   return ((long long)b * a.Sk + j) * ld + h * a.Dh;
 }
 
@@ -93,12 +92,13 @@ __device__ void attend_one(const MhaArgs &a, const RowSpan &r, int b, int i, int
   lo = max(lo, k0);
   hi = min(hi, k1);
   float m = kNegInf, l = 0.f, acc[4] = {};
+  bool bad = false;  // reported by the caller's own reads
   for (int t = lo; t < hi; t += 64) {
     const int j = t + lane;
     const bool seen = j < hi && (PAGED || !a.mask || a.mask[(long long)b * a.Sk + j] != 0.f);
     float s = kNegInf;
     if (seen) {
-      const T *k = (const T *)a.k + key_at<PAGED>(a, b, h, j, a.ldk);
+      const T *k = (const T *)a.k + key_at<PAGED>(a, b, h, j, a.ldk, bad);
       float x = 0.f;
       for (int d = 0; d < a.Dh; d += VEC) {
         const typename V::Raw v = V::raw_any(k + d);
@@ -117,7 +117,7 @@ __device__ void attend_one(const MhaArgs &a, const RowSpan &r, int b, int i, int
     for (unsigned long long left = __ballot(seen); left; left &= left - 1) {
       const int kk = __builtin_ctzll(left);
       const float w = lane_f(p, kk);
-      const T *v = (const T *)a.v + key_at<PAGED>(a, b, h, t + kk, a.ldv);
+      const T *v = (const T *)a.v + key_at<PAGED>(a, b, h, t + kk, a.ldv, bad);
 #pragma unroll
       for (int f = 0; f < 4; ++f)
         if (lane + 64 * f < a.Dh) acc[f] = fmaf(w, (float)v[lane + 64 * f], acc[f]);

@@ -63,7 +63,247 @@ __device__ __forceinline__ bool any_nonfinite(const int4 &v) {
   return bad;
 }
 
+// One wave's 32 queries, a query per lane (and half of a tile's keys): its features, and the running softmax.
+template <typename T, int DP>
+struct Rows {
+  typedef Tile<T> M;
+  static constexpr int ES = sizeof(T), STEPS = DP / M::STEP, DB = DP / 32, ROWB = DP * ES;
+  typename M::Q q[STEPS];
+  f32x16 o[DB];  // features 32 d + 8 (r / 4) + 4 (lane / 32) + r % 4
+  float m, l;    // maximum that the sums are relative to; this half's sum of weights
+
+  __device__ __forceinline__ void start(const T *src, bool live, int Dh) {
+    constexpr int VEC = 16 / ES;
+    const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const int d = s * M::STEP + half * VEC;
+      typename Vec<T, VEC>::Raw v = {};
+      if (live && d < Dh) v = Vec<T, VEC>::raw_any(src + d);
+      __builtin_memcpy(&q[s], &v, 16);
+    }
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] = (f32x16)(0.f);
+    m = kNegInf;
+    l = 0.f;
+  }
+
+  // scores of 32 keys, rows row0 .. of the tile in LDS
+  __device__ __forceinline__ f32x16 scores(const char *keys, int row0) const {
+    f32x16 s = (f32x16)(0.f);
+    const int lane = threadIdx.x & 63, row = row0 + (lane & 31), half = lane >> 5;
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) M::qk(s, keys + row * ROWB + (((2 * st + half) ^ M::swap_k(row)) << 4), q[st]);
+    return s;
+  }
+
+  // Weights relative to a maximum that only moves where a score passes it by 2^8: the sums stay far inside 32 bits,
+  // and the accumulators are rescaled a few times in a row's life.
+  template <int KB>
+  __device__ __forceinline__ void weights(f32x16 (&s)[KB], float scale) {
+    float mx = kNegInf;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
+    mx = both_halves_max(mx) * scale;
+    if (__any(mx > m + 8.f)) {
+      const float mn = fmaxf(m, mx), c = m == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= c;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] *= c;
+    }
+    const float use = m == kNegInf ? 0.f : m;
+    float sum[2] = {};
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[kb][e] = __builtin_amdgcn_exp2f(fmaf(s[kb][e], scale, -use));
+        sum[e & 1] += s[kb][e];
+      }
+    l += sum[0] + sum[1];
+  }
+
+  // the products of 32 keys' weights with their values, rows row0 .. of the tile in LDS
+  __device__ __forceinline__ void values(const char *vals, int row0, const f32x16 &s) {
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+    if constexpr (ES == 2) {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef s16x4 __attribute__((address_space(3))) * Lp;
+      const int l16 = lane & 15;
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        bf16x8 p;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = (bf16)s[hf * 8 + e];
+        const int row = row0 + hf * 16 + 4 * half + l16 / 4;
+        const char *from = vals + row * ROWB + (l16 & 1) * 8;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const int c = (4 * d + 2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1)) ^ M::swap_v(row);
+          union {
+            s16x4 q[2];
+            bf16x8 v;
+          } f;
+          // a lane's 8 bytes go to four lanes: it receives one feature of four keys
+          f.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lp)(from + (c << 4)));
+          f.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lp)(from + 8 * ROWB + (c << 4)));
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, p, o[d], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int row = row0 + 8 * (e / 4) + 4 * half + e % 4;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(*(const float *)(vals + row * ROWB + (d * 32 + (lane & 31)) * 4), s[e], o[d],
+                                                      0, 0, 0);
+      }
+    }
+  }
+
+  // sums and their pair of a part (l: of both halves)
+  __device__ __forceinline__ void put_part(float *po, float2 *pml, int Dh) const {
+    const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int f = d * 32 + 2 * e + 4 * half;
+        if (f < Dh) *(float4 *)(po + f) = make_float4(o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]);
+      }
+    if (half == 0) *pml = make_float2(m, l);
+  }
+  __device__ __forceinline__ void put(T *y, int Dh) const {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int f = d * 32 + 2 * e + 4 * half;
+        const float v[4] = {o[d][e] * inv, o[d][e + 1] * inv, o[d][e + 2] * inv, o[d][e + 3] * inv};
+        if (f < Dh) Vec<T, 4>::put_any(y + f, v);
+      }
+  }
+};
+
+// scores of keys that a query does not see: of 32 keys from k0 on, those outside [lo, hi) or whose bit of seen is 0
+template <bool PAGED>
+__device__ __forceinline__ void hide(f32x16 &s, int k0, int lo, int hi, unsigned seen) {
+  int first = 4 * ((threadIdx.x >> 5) & 1);
+  asm volatile("" : "+v"(first));  // a branch: without it the selects move into every tile
+  const unsigned from = k0 + first - lo, n = max(hi - lo, 0), bits = seen >> first;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int kk = 8 * (e / 4) + e % 4;
+    s[e] = (PAGED ? from + kk < n : (bits >> kk) & 1) ? s[e] : kNegInf;
+  }
+}
+
 constexpr int kTileRows = 128;
+
+// Brings tiles of KT keys and values from memory to LDS by TH threads: a tile's chunks of 16 bytes are on their way in
+// registers while the one before is computed, and its page numbers (mask) a tile earlier still.
+template <typename T, int DP, bool PAGED, int KT, int TH>
+struct Mover {
+  typedef Tile<T> M;
+  static constexpr int ES = sizeof(T), CH = DP * ES / 16, ROWB = DP * ES, TB = KT * ROWB;
+  static constexpr int NL = KT * CH / TH, RSTEP = TH / CH;  // chunks of a thread, all of one column
+  static_assert(TH % CH == 0 && KT % RSTEP == 0, "a thread keeps its column");
+  const char *k, *v;        // of this key head (and sequence), this thread's column
+  long long ldk, ldv;       // bytes of a page, or of a row
+  const int32_t *table;
+  const float *mask;
+  int row, chunk, last, plog, n_pages, rowb;
+  bool feature;             // whether the column is one of the head's
+  bool bad;                 // a page number was out of range
+  int pg[NL];
+  float valid;              // mask of key lane of the next tile
+  unsigned long long seen;  // keys of the tile on its way that are there and not masked
+  int4 kr[NL], vr[NL];
+
+  __device__ __forceinline__ void start(const MhaArgs &a, int b, int h, int tid, int last_key, const float *m) {
+    row = tid / CH;
+    chunk = tid % CH;
+    feature = chunk * 16 < a.Dh * ES;
+    last = last_key;
+    plog = a.page_log2;
+    n_pages = a.n_pages;
+    rowb = a.Dh * ES;
+    bad = false;
+    mask = m;
+    const long long col = feature ? chunk * 16 : 0;  // columns that only pad read the first one and become zeros
+    if (PAGED) {
+      table = a.table + (long long)b * a.n_blocks;
+      ldk = ldv = ((long long)a.Hk << plog) * rowb;
+      const long long at = ((long long)h << plog) * rowb + col;
+      k = (const char *)a.k + at;
+      v = (const char *)a.v + at;
+    } else {
+      ldk = a.ldk * ES;
+      ldv = a.ldv * ES;
+      k = (const char *)a.k + ((long long)b * a.Sk) * ldk + h * rowb + col;
+      v = (const char *)a.v + ((long long)b * a.Sk) * ldv + h * rowb + col;
+    }
+  }
+  // what a tile's loads will need: keys behind the last one are not read
+  __device__ __forceinline__ void look(int k0) {
+    if (PAGED) {
+#pragma unroll
+      for (int x = 0; x < NL; ++x) pg[x] = table[min(k0 + row + x * RSTEP, last) >> plog];
+    } else if (mask) {
+      valid = mask[min(k0 + (int)(threadIdx.x & 63), last)];
+    }
+  }
+  __device__ __forceinline__ void fetch(int k0) {
+    if (!PAGED) {
+      const int j = threadIdx.x & 63;
+      seen = __ballot(j < KT && k0 + j <= last && (!mask || valid != 0.f));
+    }
+#pragma unroll
+    for (int x = 0; x < NL; ++x) {
+      const int j = min(k0 + row + x * RSTEP, last);
+      if (PAGED) {
+        bad |= (unsigned)pg[x] >= (unsigned)n_pages;
+        const int page = min(max(pg[x], 0), n_pages - 1);
+        const long long at = page * ldk + (j & ((1 << plog) - 1)) * rowb;
+        kr[x] = *(const int4 *)(k + at);
+        vr[x] = *(const int4 *)(v + at);
+      } else {
+        const auto kv = Vec<T, 16 / ES>::raw_any((const T *)(k + j * ldk)), vv = Vec<T, 16 / ES>::raw_any((const T *)(v + j * ldv));
+        __builtin_memcpy(&kr[x], &kv, 16);
+        __builtin_memcpy(&vr[x], &vv, 16);
+      }
+    }
+    look(k0 + KT);
+  }
+  // The tile that was fetched, into LDS.  Values that no row may see are zeros (their weights are).  mixed: some rows see
+  // keys of the tile that others do not; says whether one of its values is no number then, as its weights' zeros would
+  // not hide that.
+  __device__ __forceinline__ bool put(int k0, char *buf, bool mixed) {
+    bool odd = false;
+#pragma unroll
+    for (int x = 0; x < NL; ++x) {
+      const int r = row + x * RSTEP;
+      const bool there = feature && (PAGED ? k0 + r <= last : (seen >> r) & 1);
+      if (!feature) kr[x] = make_int4(0, 0, 0, 0);
+      if (!there) vr[x] = make_int4(0, 0, 0, 0);
+      *(int4 *)(buf + r * ROWB + ((chunk ^ M::swap_k(r)) << 4)) = kr[x];
+      *(int4 *)(buf + TB + r * ROWB + ((chunk ^ M::swap_v(r)) << 4)) = vr[x];
+    }
+    if (PAGED && mixed) {
+#pragma unroll
+      for (int x = 0; x < NL; ++x) odd |= any_nonfinite<T>(vr[x]);
+    }
+    return odd;
+  }
+};
 
 // What a launch of the tile kernel has decided
 struct TilePlan {
@@ -79,13 +319,10 @@ struct TilePlan {
 template <typename T, int DP, bool PAGED>
 __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a, TilePlan plan) {
   typedef Tile<T> M;
-  constexpr int KT = M::KT, ES = sizeof(T), CH = DP * ES / 16, ROWB = DP * ES, TB = KT * ROWB;
-  constexpr int NL = KT * CH / 256;  // chunks of each operand that a thread moves per tile
-  constexpr int KB = KT / 32, DB = DP / 32, STEPS = DP / M::STEP;
-  static_assert(KT * CH % 256 == 0, "every thread moves as many");
+  constexpr int KT = M::KT, TB = KT * DP * (int)sizeof(T), KB = KT / 32;
   __shared__ __attribute__((aligned(1024))) char lds[4 * TB];
   __shared__ int dirty, edge[2];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31;
   // consecutive tiles of a key head run on one XCD, whose L2 holds its keys and values; the last tiles, which see the
   // most keys, first
   const int w = plan.first + xcd_remap(blockIdx.x, gridDim.x);
@@ -127,184 +364,46 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a,
   const int qi = (live ? r : R - 1) / a.G, hq = h * a.G + (live ? r : R - 1) - qi * a.G;
   int qlo, qhi;
   seen_keys<PAGED>(a, span, qi, qlo, qhi);
-  typename M::Q qf[STEPS];
-  {
-    constexpr int VEC = 16 / ES;
-    const T *q = (const T *)a.q + ((long long)b * a.S + qi) * a.ldq + (long long)hq * a.Dh;
-#pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-      const int d = s * M::STEP + half * VEC;
-      typename Vec<T, VEC>::Raw v = {};
-      if (live && d < a.Dh) v = Vec<T, VEC>::raw_any(q + d);
-      __builtin_memcpy(&qf[s], &v, 16);
-    }
-  }
-  f32x16 o[DB];
-#pragma unroll
-  for (int d = 0; d < DB; ++d) o[d] = (f32x16)(0.f);
-  float m = kNegInf, l = 0.f;
-  // ---- tiles of keys: this thread's chunks
-  int4 kr[NL], vr[NL];
-  unsigned long long seen_next = 0;  // keys of the next tile that are there and not masked
-  auto fetch = [&](int k0) {
-    if (!PAGED) {
-      const int j = k0 + lane;
-      seen_next = __ballot(lane < KT && j < hi2 && (!mask || mask[j] != 0.f));
-    }
-#pragma unroll
-    for (int x = 0; x < NL; ++x) {
-      const int id = threadIdx.x + x * 256, row = id / CH, c = id % CH;
-      const int j = min(k0 + row, hi2 - 1);  // keys behind the last one are not read
-      kr[x] = make_int4(0, 0, 0, 0);
-      vr[x] = make_int4(0, 0, 0, 0);
-      if (c * 16 < a.Dh * ES) {
-        const T *ks = (const T *)a.k + key_at<PAGED>(a, b, h, j, a.ldk);
-        const T *vs = (const T *)a.v + (PAGED ? ks - (const T *)a.k : key_at<PAGED>(a, b, h, j, a.ldv));
-        if (PAGED) {
-          kr[x] = *(const int4 *)((const char *)ks + c * 16);
-          vr[x] = *(const int4 *)((const char *)vs + c * 16);
-        } else {
-          const auto kv = Vec<T, 16 / ES>::raw_any(ks + c * (16 / ES)), vv = Vec<T, 16 / ES>::raw_any(vs + c * (16 / ES));
-          __builtin_memcpy(&kr[x], &kv, 16);
-          __builtin_memcpy(&vr[x], &vv, 16);
-        }
-      }
-    }
-  };
-  // Values that no row may see are zeros (their weights are); values that some rows see and others not have to be
-  // numbers, or the weights' zeros would not hide them.
-  auto put = [&](int k0, char *buf) {
-    const bool mixed = k0 + KT > hi || k0 < lo2;
-#pragma unroll
-    for (int x = 0; x < NL; ++x) {
-      const int id = threadIdx.x + x * 256, row = id / CH, c = id % CH;
-      const bool there = PAGED ? k0 + row < hi2 : (seen_next >> row) & 1;
-      if (!there) vr[x] = make_int4(0, 0, 0, 0);
-      if (PAGED && mixed && any_nonfinite<T>(vr[x])) dirty = 1;
-      *(int4 *)(buf + row * ROWB + ((c ^ M::swap_k(row)) << 4)) = kr[x];
-      *(int4 *)(buf + TB + row * ROWB + ((c ^ M::swap_v(row)) << 4)) = vr[x];
-    }
-  };
+  Rows<T, DP> me;
+  me.start((const T *)a.q + ((long long)b * a.S + qi) * a.ldq + (long long)hq * a.Dh, live, a.Dh);
+  // ---- tiles of keys
+  Mover<T, DP, PAGED, KT, 256> mv;
+  auto mixed = [&](int k0) { return k0 + KT > hi || k0 < lo2; };
   if (nt > 0) {
-    fetch(lo);
-    put(lo, lds);
+    mv.start(a, b, h, threadIdx.x, hi2 - 1, mask);
+    mv.look(lo);
+    mv.fetch(lo);
+    if (mv.put(lo, lds, mixed(lo))) dirty = 1;
   }
   for (int t = 0; t < nt; ++t) {
     const int k0 = lo + t * KT;
     const char *buf = lds + (t & 1) * 2 * TB;
-    const unsigned long long seen = seen_next;
+    const unsigned long long seen = mv.seen;
     __syncthreads();
-    if (t + 1 < nt) fetch(k0 + KT);
-    // ---- scores
+    if (t + 1 < nt) mv.fetch(k0 + KT);
     f32x16 s[KB];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      s[kb] = (f32x16)(0.f);
-      const int row = kb * 32 + col;
+    for (int kb = 0; kb < KB; ++kb) s[kb] = me.scores(buf, kb * 32);
+    if (PAGED ? mixed(k0) : seen != (KT == 64 ? ~0ull : (1ull << KT) - 1)) {
 #pragma unroll
-      for (int st = 0; st < STEPS; ++st)
-        M::qk(s[kb], buf + row * ROWB + (((2 * st + half) ^ M::swap_k(row)) << 4), qf[st]);
+      for (int kb = 0; kb < KB; ++kb) hide<PAGED>(s[kb], k0 + kb * 32, qlo, qhi, (unsigned)(seen >> (kb * 32)));
     }
-    if (PAGED ? (k0 + KT > hi || k0 < lo2) : seen != (KT == 64 ? ~0ull : (1ull << KT) - 1)) {
+    me.weights(s, a.scale);
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int kk = kb * 32 + 8 * (e / 4) + 4 * half + e % 4;
-          const bool ok = PAGED ? k0 + kk >= qlo && k0 + kk < qhi : (seen >> kk) & 1;
-          s[kb][e] = ok ? s[kb][e] : kNegInf;
-        }
-    }
-    // ---- weights relative to a maximum that only moves where a score passes it by 2^8: the sums stay far inside
-    // 32 bits, and the accumulators are rescaled a few times in a row's life
-    float mx = kNegInf;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
-    mx = both_halves_max(mx) * a.scale;
-    if (__any(mx > m + 8.f)) {
-      const float mn = fmaxf(m, mx), c = m == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-      m = mn;
-      l *= c;
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[d][e] *= c;
-    }
-    const float use = m == kNegInf ? 0.f : m;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[kb][e] = __builtin_amdgcn_exp2f(fmaf(s[kb][e], a.scale, -use));
-        l += s[kb][e];
-      }
-    // ---- values
-    const char *vb = buf + TB;
-    if constexpr (ES == 2) {
-      const int l16 = lane & 15;
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          bf16x8 p;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) p[e] = (bf16)s[kb][hf * 8 + e];
-          const int row = kb * 32 + hf * 16 + 4 * half + l16 / 4;
-#pragma unroll
-          for (int d = 0; d < DB; ++d) {
-            const int c = 4 * d + 2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1), by = (l16 & 1) * 8;
-            typedef short s16x4 __attribute__((ext_vector_type(4)));
-            typedef s16x4 __attribute__((address_space(3))) * Lp;
-            union {
-              s16x4 q[2];
-              bf16x8 v;
-            } f;
-            f.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lp)(vb + row * ROWB + ((c ^ M::swap_v(row)) << 4) + by));
-            f.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lp)(vb + (row + 8) * ROWB + ((c ^ M::swap_v(row)) << 4) + by));
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, p, o[d], 0, 0, 0);
-          }
-        }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int row = 8 * (e / 4) + 4 * half + e % 4;
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(*(const float *)(vb + row * ROWB + (d * 32 + col) * 4), s[0][e], o[d], 0, 0, 0);
-      }
-    }
-    if (t + 1 < nt) put(k0 + KT, lds + ((t + 1) & 1) * 2 * TB);
+    for (int kb = 0; kb < KB; ++kb) me.values(buf + TB, kb * 32, s[kb]);
+    if (t + 1 < nt && mv.put(k0 + KT, lds + ((t + 1) & 1) * 2 * TB, mixed(k0 + KT))) dirty = 1;
   }
+  if (PAGED && nt > 0 && mv.bad) atomicOr(a.err, kErrPage);
   // ---- results
-  l = both_halves_sum(l);
+  me.l = both_halves_sum(me.l);
   const long long rows = (long long)a.B * a.Hq * a.S;
   const Parts parts = parts_of(a.ws, rows, plan.parts);
   const long long prow = part * rows + (long long)bh * a.S * a.G;
   if (live) {
-    if (plan.parts > 1) {
-      float *po = parts.o + (prow + r) * a.Dh;
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-          const int f = d * 32 + 2 * e + 4 * half;
-          if (f < a.Dh) *(float4 *)(po + f) = make_float4(o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]);
-        }
-      if (half == 0) parts.ml[prow + r] = make_float2(m, l);
-    } else {
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      T *y = (T *)a.y + ((long long)b * a.S + qi) * a.ldy + (long long)hq * a.Dh;
-#pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-          const int f = d * 32 + 2 * e + 4 * half;
-          const float v[4] = {o[d][e] * inv, o[d][e + 1] * inv, o[d][e + 2] * inv, o[d][e + 3] * inv};
-          if (f < a.Dh) Vec<T, 4>::put_any(y + f, v);
-        }
-    }
+    if (plan.parts > 1)
+      me.put_part(parts.o + (prow + r) * a.Dh, parts.ml + prow + r, a.Dh);
+    else
+      me.put((T *)a.y + ((long long)b * a.S + qi) * a.ldy + (long long)hq * a.Dh, a.Dh);
   }
   if (!PAGED) return;
   // values that are no numbers where some rows see them and others not: row by row instead

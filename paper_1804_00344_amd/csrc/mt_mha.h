@@ -34,7 +34,7 @@ hipError_t launch_mha(const MhaArgs &a, hipStream_t st);
 // ---- norms, rotation and store (mt_mha_append.hip) ----
 struct AppendArgs {
   int Hq, Hk, Dh, bf16_io, norm, rot, rot_pairs;
-  float eps;
+  float eps, inv_Dh;
   const float *gq, *gk;      // [Dh]
   const double *turns;       // [rot/2] turns per position: frequency / (2 pi)
   int B, S;

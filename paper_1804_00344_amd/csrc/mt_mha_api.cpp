@@ -179,6 +179,7 @@ mt_status mt_attn_append(mt_attn *a, int B, int S, const int32_t *n_new, const i
   AppendArgs p{};
   p.Hq = c.Hq; p.Hk = c.Hk; p.Dh = c.Dh; p.bf16_io = es == 2;
   p.norm = c.qk_norm; p.rot = c.rot; p.rot_pairs = c.rot_pairs; p.eps = c.norm_eps;
+  p.inv_Dh = 1.f / c.Dh;
   p.gq = a->gq; p.gk = a->gk; p.turns = a->turns;
   p.B = B; p.S = S; p.n_new = n_new; p.len = len; p.table = table;
   p.n_blocks = n_blocks; p.n_pages = n_pages; p.page_log2 = a->page_log2;

@@ -7,153 +7,237 @@ namespace mt {
 
 namespace {
 
-// What a row's lengths say: the position of its first new one and their number (clamped, reported by one lane)
-__device__ __forceinline__ void row_lengths(const AppendArgs &a, int b, bool tell, int &first, int &n) {
-  const int cap = a.n_blocks << a.page_log2, l0 = a.len[b], n0 = a.n_new ? a.n_new[b] : a.S;
-  const int l = min(max(l0, 0), cap);
-  n = min(max(n0, 0), a.S);
-  if (tell && (l != l0 || n != n0)) atomicOr(a.err, kErrLen);
-  first = l - n;
+// v of lane ^ O within groups of more than O lanes
+template <int O>
+__device__ __forceinline__ float lane_xor(float v) {
+  if constexpr (O == 1) return dpp_mov<kDppQuadSwap1>(v);
+  if constexpr (O == 2) return dpp_mov<kDppQuadSwap2>(v);
+  if constexpr (O == 4) return dpp_mov<0x1B>(dpp_mov<0x141>(v));  // eight lanes reversed, then each four
+  if constexpr (O == 8) return dpp_mov<kDppRowRor8>(v);
+  if constexpr (O == 16) return __shfl_xor(v, 16);
+  if constexpr (O == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+    return __int_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+  }
+  return 0.f;
 }
 
-// A head takes LP lanes (a power of two) of VEC features each, one 16-byte access per lane; a workgroup takes TOK
-// rows, whose angles its threads form first (in 64 bits, as turns: the product keeps 2^-22 of a turn at position
-// 2^30) and all heads of the row share.  Partners of a rotation pass through LDS within the head's lanes.
+template <int O, int LP, int U>
+__device__ __forceinline__ void head_sums(float (&v)[U]) {
+  if constexpr (O < LP) {
+    float other[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) other[u] = lane_xor<O>(v[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] += other[u];
+    head_sums<O * 2, LP, U>(v);
+  }
+}
+
+// A head takes LP lanes (a power of two) of VEC features each, one 16-byte access per lane, and a lane U heads at a
+// time, step by step together.  A workgroup takes TOK positions of a row, whose angles its threads form first (in 64
+// bits, as turns: the product keeps 2^-22 of a turn at position 2^30) and all heads share.  Partners of a rotation come
+// from the lane half a head away where the lanes are a whole head, else through LDS.
 template <typename T, int LP, int TOK>
-__global__ void __launch_bounds__(256) append_kernel(AppendArgs a) {
-  constexpr int VEC = 16 / sizeof(T);
+__global__ void __launch_bounds__(256) append_kernel(AppendArgs a, int per_row, int base) {
+  constexpr int VEC = 16 / sizeof(T), U = 4, HEADS = 256 / LP;
   typedef Vec<T, VEC> V;
-  __shared__ float cs[TOK][2][128];
+  __shared__ __attribute__((aligned(16))) float cs[TOK][2][128];
   __shared__ __attribute__((aligned(16))) float part[256 * VEC];
-  const long long row0 = (long long)blockIdx.x * TOK, rows = (long long)a.B * a.S;
-  const int half = a.rot / 2, H = a.Hq + 2 * a.Hk;
-  for (int e = threadIdx.x; e < TOK * half; e += 256) {
+  const int w = base + blockIdx.x, b = w / per_row, i0 = (w - b * per_row) * TOK;
+  const int cap = a.n_blocks << a.page_log2, l0 = a.len[b], n0 = a.n_new ? a.n_new[b] : a.S;
+  const int len = min(max(l0, 0), cap), n = min(max(n0, 0), a.S), first = len - n;
+  if (i0 == 0 && threadIdx.x == 0 && (len != l0 || n != n0)) atomicOr(a.err, kErrLen);
+  const int toks = min(TOK, n - i0);
+  if (toks <= 0) return;
+  const int half = a.rot / 2, H = a.Hq + a.Hk, pmask = (1 << a.page_log2) - 1;
+  const int chunk = threadIdx.x & (LP - 1), d0 = chunk * VEC, h0 = threadIdx.x / LP;
+  const bool in_head = d0 < a.Dh;  // the others only take part in the sums
+  const long long row0 = (long long)b * a.S + i0;
+  // first feature of a position in the pages, of key head 0
+  bool bad = false;
+  auto place = [&](int pos) {
+    const int pg = a.table[(long long)b * a.n_blocks + (pos >> a.page_log2)];
+    bad |= (unsigned)pg >= (unsigned)a.n_pages;
+    return ((((long long)min(max(pg, 0), a.n_pages - 1) * a.Hk) << a.page_log2) + (pos & pmask)) * a.Dh;
+  };
+  const long long head_step = (long long)a.Dh << a.page_log2;
+  struct Task {
+    int t, h;
+  };
+  auto next = [&](Task &k, int heads) {
+    k.h += HEADS;
+    while (k.h >= heads && k.t < toks) {
+      k.h -= heads;
+      ++k.t;
+    }
+  };
+  // ---- values: copies
+  {
+    Task k{0, h0};
+    while (k.h >= a.Hk && k.t < toks) {
+      k.h -= a.Hk;
+      ++k.t;
+    }
+    while (k.t < toks) {
+      typename V::Raw in[U];
+      long long to[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int pos = first + i0 + k.t;
+        to[u] = -1;
+        if (k.t < toks && in_head && pos >= 0) {
+          in[u] = V::raw_any((const T *)a.v + (row0 + k.t) * a.ldv + k.h * a.Dh + d0);
+          to[u] = place(pos) + k.h * head_step + d0;
+        }
+        next(k, a.Hk);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (to[u] >= 0) *(typename V::Raw *)((T *)a.vp + to[u]) = in[u];
+    }
+  }
+  for (int e = threadIdx.x; e < toks * half; e += 256) {
     const int t = e / half, i = e - t * half;
-    const long long row = row0 + t;
-    if (row >= rows) break;
-    int first, n;
-    row_lengths(a, (int)(row / a.S), false, first, n);
-    const double v = (double)(first + (int)(row % a.S)) * a.turns[i];
+    const double v = (double)(first + i0 + t) * a.turns[i];
     float s, c;
     sincospif(2.0f * (float)(v - rint(v)), &s, &c);
     cs[t][0][i] = c;
     cs[t][1][i] = s;
   }
+  float gq[VEC], gk[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) gq[e] = a.gq[d0 + e], gk[e] = a.gk[d0 + e];  // 256 of each are there
   __syncthreads();
-  const int chunk = threadIdx.x & (LP - 1), d0 = chunk * VEC;
-  float *const mine = part + threadIdx.x * VEC, *const head = part + (threadIdx.x & ~(LP - 1)) * VEC;
-  const bool whole = half % VEC == 0;  // a lane's partners are one lane's
-  for (int u = threadIdx.x / LP; u < TOK * H; u += 256 / LP) {
-    const int t = u / H, h = u - t * H;
-    const long long row = row0 + t;
-    if (row >= rows) break;
-    const int b = (int)(row / a.S), i = (int)(row % a.S);
-    int first, n;
-    row_lengths(a, b, i == 0 && h == 0 && chunk == 0, first, n);
-    if (i >= n) continue;
-    const bool in_head = d0 < a.Dh;  // the others only take part in the sum
-    const int pos = first + i;
-    const int kind = h < a.Hq ? 0 : h < a.Hq + a.Hk ? 1 : 2, hk = h - a.Hq - (kind == 2 ? a.Hk : 0);
-    if (pos < 0) {  // before the row's beginning: no position
-      if (kind == 0 && in_head) {
-        const float zero[VEC] = {};
-        V::put_any((T *)a.qo + row * a.ldqo + h * a.Dh + d0, zero);
-      }
-      continue;
-    }
-    const T *src = kind == 0   ? (const T *)a.q + row * a.ldq + h * a.Dh
-                   : kind == 1 ? (const T *)a.k + row * a.ldk + hk * a.Dh
-                               : (const T *)a.v + row * a.ldv + hk * a.Dh;
-    typename V::Raw in = {};
-    if (in_head) in = V::raw_any(src + d0);
-    T *dst = nullptr;
-    if (kind != 0) {
-      int pg = a.table[(long long)b * a.n_blocks + (pos >> a.page_log2)];
-      if ((unsigned)pg >= (unsigned)a.n_pages) {
-        if (chunk == 0) atomicOr(a.err, kErrPage);
-        pg = pg < 0 ? 0 : a.n_pages - 1;
-      }
-      dst = (T *)(kind == 1 ? a.kp : a.vp) +
-            ((((long long)pg * a.Hk + hk) << a.page_log2) + (pos & ((1 << a.page_log2) - 1))) * a.Dh + d0;
-    }
-    if (kind == 2) {
-      if (in_head) *(typename V::Raw *)dst = in;
-      continue;
-    }
-    float x[VEC];
+  float *const mine = part + threadIdx.x * VEC, *const head = part + h0 * LP * VEC;
+  const bool whole = half % VEC == 0, swaps = a.rot == LP * VEC && LP > 1;
+  Task k{0, h0};
+  while (k.h >= H && k.t < toks) {
+    k.h -= H;
+    ++k.t;
+  }
+  while (k.t < toks) {
+    Task task[U];
+    float x[U][VEC];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) x[e] = (float)in.v[e];
+    for (int u = 0; u < U; ++u) {
+      task[u] = k;
+      typename V::Raw in = {};
+      if (k.t < toks && in_head) {
+        const T *src = k.h < a.Hq ? (const T *)a.q + (row0 + k.t) * a.ldq + k.h * a.Dh
+                                  : (const T *)a.k + (row0 + k.t) * a.ldk + (k.h - a.Hq) * a.Dh;
+        in = V::raw_any(src + d0);
+      }
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[u][e] = (float)in.v[e];
+      next(k, H);
+    }
     if (a.norm) {
-      float ss = 0.f;
+      float ss[U];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) ss = fmaf(x[e], x[e], ss);
+      for (int u = 0; u < U; ++u) {
+        ss[u] = 0.f;
 #pragma unroll
-      for (int o = 1; o < LP; o <<= 1) ss += __shfl_xor(ss, o);
-      const float r = rsqrtf(ss / (float)a.Dh + a.eps);
-      const float *g = kind == 0 ? a.gq : a.gk;
+        for (int e = 0; e < VEC; ++e) ss[u] = fmaf(x[u][e], x[u][e], ss[u]);
+      }
+      head_sums<1, LP, U>(ss);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) x[e] = in_head ? x[e] * r * g[d0 + e] : 0.f;
+      for (int u = 0; u < U; ++u) {
+        const float r = rsqrtf(fmaf(ss[u], a.inv_Dh, a.eps));
+        const bool q = task[u].h < a.Hq;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[u][e] = x[u][e] * r * (q ? gq[e] : gk[e]);
+      }
     }
-    if (d0 < a.rot) {
-      if (a.rot_pairs) {
+    if (a.rot && a.rot_pairs) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int t = min(task[u].t, toks - 1);
 #pragma unroll
         for (int e = 0; e < VEC; e += 2) {
           if (d0 + e < a.rot) {
-            const float c = cs[t][0][(d0 + e) >> 1], s = cs[t][1][(d0 + e) >> 1], p = x[e], w = x[e + 1];
-            x[e] = p * c - w * s;
-            x[e + 1] = w * c + p * s;
+            const float c = cs[t][0][(d0 + e) >> 1], s = cs[t][1][(d0 + e) >> 1], p = x[u][e], w = x[u][e + 1];
+            x[u][e] = p * c - w * s;
+            x[u][e + 1] = w * c + p * s;
           }
         }
-      } else {
-        // the lanes of a head are of one wave, whose LDS accesses are served in order
+      }
+    } else if (swaps) {
+      const bool low = chunk < LP / 2;
+      const int i2 = (chunk & (LP / 2 - 1)) * VEC;
 #pragma unroll
-        for (int e = 0; e < VEC; e += 4) *(float4 *)(mine + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+      for (int u = 0; u < U; ++u) {
+        const int t = min(task[u].t, toks - 1);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const float p = lane_xor<(LP > 1 ? LP / 2 : 1)>(x[u][e]), s = cs[t][1][i2 + e];
+          x[u][e] = x[u][e] * cs[t][0][i2 + e] + p * (low ? -s : s);
+        }
+      }
+    } else if (a.rot) {
+      // the lanes of a head are of one wave, whose LDS accesses are served in order
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int t = min(task[u].t, toks - 1);
+#pragma unroll
+        for (int e = 0; e < VEC; e += 4) *(float4 *)(mine + e) = make_float4(x[u][e], x[u][e + 1], x[u][e + 2], x[u][e + 3]);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        float p[VEC];
-        if (whole) {
-          const float *from = head + (d0 < half ? d0 + half : d0 - half);
+        if (d0 >= a.rot) {
+        } else if (whole) {
+          const bool low = d0 < half;
+          const float *from = head + (low ? d0 + half : d0 - half);
+          const int i2 = low ? d0 : d0 - half;
 #pragma unroll
-          for (int e = 0; e < VEC; e += 4) {
-            const float4 f = *(const float4 *)(from + e);
-            p[e] = f.x; p[e + 1] = f.y; p[e + 2] = f.z; p[e + 3] = f.w;
+          for (int e = 0; e < VEC; ++e) {
+            const float s = cs[t][1][i2 + e];
+            x[u][e] = x[u][e] * cs[t][0][i2 + e] + from[e] * (low ? -s : s);
           }
         } else {
 #pragma unroll
           for (int e = 0; e < VEC; ++e) {
             const int d = d0 + e;
-            p[e] = d < a.rot ? head[d < half ? d + half : d - half] : 0.f;
+            if (d < a.rot) {
+              const int i2 = d < half ? d : d - half;
+              const float p = head[d < half ? d + half : i2], s = cs[t][1][i2];
+              x[u][e] = x[u][e] * cs[t][0][i2] + (d < half ? -p : p) * s;
+            }
           }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          const int d = d0 + e;
-          if (d < a.rot) {
-            const int i2 = d < half ? d : d - half;
-            const float s = cs[t][1][i2];
-            x[e] = x[e] * cs[t][0][i2] + p[e] * (d < half ? -s : s);
-          }
-        }
       }
     }
-    if (!in_head) continue;
-    if (kind == 0)
-      V::put_any((T *)a.qo + row * a.ldqo + h * a.Dh + d0, x);
-    else
-      V::put(dst, x);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (task[u].t >= toks || !in_head) continue;
+      const int pos = first + i0 + task[u].t;
+      if (pos < 0) {  // before the row's beginning: no position
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[u][e] = 0.f;
+      }
+      if (task[u].h < a.Hq)
+        V::put_any((T *)a.qo + (row0 + task[u].t) * a.ldqo + task[u].h * a.Dh + d0, x[u]);
+      else if (pos >= 0)
+        V::put((T *)a.kp + place(pos) + (task[u].h - a.Hq) * head_step + d0, x[u]);
+    }
   }
+  if (bad) atomicOr(a.err, kErrPage);
 }
 
 template <typename T, int LP>
 hipError_t by_rows(const AppendArgs &a, hipStream_t st) {
-  const long long rows = (long long)a.B * a.S;
-  // several rows of a workgroup share nothing but its start: only where there are enough of them
-  if (rows >= 16ll * a.num_cu)
-    hipLaunchKernelGGL((append_kernel<T, LP, 4>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL((append_kernel<T, LP, 1>), dim3((unsigned)rows), dim3(256), 0, st, a);
+  // several positions of a workgroup share its start and keep loads on their way: only where there are enough of them
+  const bool many = (long long)a.B * a.S >= 16ll * a.num_cu && a.S >= 4;
+  const int per_row = many ? (a.S + 3) / 4 : a.S;
+  const int all = a.B * per_row, most = 1 << 22;  // workgroups of a launch
+  for (int base = 0; base < all; base += most) {
+    const dim3 grid((unsigned)(all - base < most ? all - base : most));
+    if (many)
+      hipLaunchKernelGGL((append_kernel<T, LP, 4>), grid, dim3(256), 0, st, a, per_row, base);
+    else
+      hipLaunchKernelGGL((append_kernel<T, LP, 1>), grid, dim3(256), 0, st, a, per_row, base);
+  }
   return hipGetLastError();
 }
 

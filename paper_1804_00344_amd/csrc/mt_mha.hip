@@ -1,23 +1,28 @@
 // Attention of query heads over keys and values in pages of a cache, or in rows of another length under a mask:
 //   y = sum_j softmax_j(scale q.k_j) v_j over the keys that a query sees.
 // Here: how a call is split over the chip, and the join of the parts of a key axis that is cut.
-#include "mt_mha_tile.h"
+#include "mt_mha_step.h"
 
 namespace mt {
 
 namespace {
 
 struct Plan {
-  TilePlan tile;
+  bool step, share;
+  int tiles, parts;
 };
 
-Plan plan_of(int Hq, int Hk, int B, int S, long long n_keys, int num_cu) {
+Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, bool f32, int num_cu) {
   Plan p;
-  const long long rows = (long long)S * (Hq / Hk);
-  p.tile.tiles = (int)((rows + kTileRows - 1) / kTileRows);
+  const long long rows = (long long)S * (Hq / Hk), heads = (long long)B * Hk;
+  const long long big = heads * ((rows + kTileRows - 1) / kTileRows);
+  p.step = (!f32 || Dh <= 128) && (rows <= kStepRows || big < num_cu);
+  const int per = p.step ? kStepRows : kTileRows;
+  p.tiles = (int)((rows + per - 1) / per);
   // two workgroups a unit; a part of 256 keys at least
-  const long long wgs = (long long)B * Hk * p.tile.tiles, want = 2 * num_cu / wgs, most = n_keys / 256;
-  p.tile.parts = (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
+  const long long wgs = heads * p.tiles, want = 2 * num_cu / wgs, most = n_keys / 256;
+  p.parts = (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
+  p.share = wgs < 8 * num_cu;
   return p;
 }
 
@@ -55,21 +60,28 @@ __global__ void __launch_bounds__(256) join_kernel(MhaArgs a, int n_parts) {
 
 }  // namespace
 
-size_t mha_workspace_bytes(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int num_cu) {
-  const Plan p = plan_of(Hq, Hk, B, S, n_keys, num_cu);
-  return p.tile.parts > 1 ? (parts_bytes((long long)B * Hq * S, p.tile.parts, Dh) + 255) / 256 * 256 : 256;
+size_t mha_workspace_bytes(int Hq, int Hk, int Dh, bool f32, int B, int S, long long n_keys, int num_cu) {
+  const Plan p = plan_of(Hq, Hk, Dh, B, S, n_keys, f32, num_cu);
+  return p.parts > 1 ? (parts_bytes((long long)B * Hq * S, p.parts, Dh) + 255) / 256 * 256 : 256;
 }
 
 hipError_t launch_mha(const MhaArgs &a, hipStream_t st) {
-  const Plan p = plan_of(a.Hq, a.Hk, a.B, a.S, a.table ? (long long)a.n_blocks << a.page_log2 : a.Sk, a.num_cu);
-  hipError_t e = a.bf16_io ? launch_tiles_bf16(a, p.tile, st) : launch_tiles_f32(a, p.tile, st);
-  if (e != hipSuccess || p.tile.parts == 1) return e;
+  const Plan p = plan_of(a.Hq, a.Hk, a.Dh, a.B, a.S, a.table ? (long long)a.n_blocks << a.page_log2 : a.Sk, !a.bf16_io, a.num_cu);
+  hipError_t e;
+  if (p.step) {
+    const StepPlan s{p.tiles, p.parts, 0};
+    e = a.bf16_io ? launch_steps_bf16(a, s, p.share, st) : launch_steps_f32(a, s, p.share, st);
+  } else {
+    const TilePlan t{p.tiles, p.parts, 0};
+    e = a.bf16_io ? launch_tiles_bf16(a, t, st) : launch_tiles_f32(a, t, st);
+  }
+  if (e != hipSuccess || p.parts == 1) return e;
   const long long rows = (long long)a.B * a.Hq * a.S;
   const dim3 grid((unsigned)((rows + 3) / 4));
   if (a.bf16_io)
-    hipLaunchKernelGGL(join_kernel<bf16>, grid, dim3(256), 0, st, a, p.tile.parts);
+    hipLaunchKernelGGL(join_kernel<bf16>, grid, dim3(256), 0, st, a, p.parts);
   else
-    hipLaunchKernelGGL(join_kernel<float>, grid, dim3(256), 0, st, a, p.tile.parts);
+    hipLaunchKernelGGL(join_kernel<float>, grid, dim3(256), 0, st, a, p.parts);
   return hipGetLastError();
 }
 

@@ -1,0 +1,191 @@
+// Attention of few query rows: kernel and launch, instantiated by mt_mha_step_*.hip.
+#pragma once
+
+#include "mt_mha_tile.h"
+
+namespace mt {
+
+constexpr int kStepRows = 32;
+
+// What a launch of the step kernel has decided
+struct StepPlan {
+  int tiles;  // of kStepRows rows of a sequence's key head
+  int parts;  // the key axis is cut into
+  int first;  // workgroup of this launch
+};
+
+// Tiles of 32 rows of one key head (as in the tile kernel) and 32 keys at a time, each wave with its own part of LDS and
+// no barriers.  SHARE: the four waves of a workgroup take the tiles of keys in turn and join their sums at the end, for
+// short latency; else each wave has its own rows, for many of them.
+template <typename T, int DP, bool PAGED, bool SHARE>
+__global__ void __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 256 ? 2 : 1) step_kernel(MhaArgs a, StepPlan plan) {
+  constexpr int KT = 32, TB = KT * DP * (int)sizeof(T), DB = DP / 32;
+  __shared__ __attribute__((aligned(1024))) char lds[4 * 2 * TB];
+  __shared__ float2 ends[4][32];
+  __shared__ int dirty;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31;
+  const long long jobs = (long long)a.B * a.Hk * plan.tiles * plan.parts;
+  const int w = plan.first + xcd_remap(blockIdx.x, gridDim.x);
+  const long long job = SHARE ? w : w * 4ll + wave;
+  if (job >= jobs) return;
+  const int part = (int)(job % plan.parts), u = (int)(job / plan.parts), bh = u / plan.tiles, tile = u - bh * plan.tiles;
+  const int b = bh / a.Hk, h = bh - b * a.Hk;
+  const RowSpan span = row_span<PAGED>(a, b, h == 0 && tile == 0 && part == 0 && lane == 0);
+  const int R = span.n * a.G, r0 = tile * kStepRows;
+  if (r0 >= R) return;
+  const int i_first = r0 / a.G, i_last = min(r0 + kStepRows - 1, R - 1) / a.G;
+  int lo, hi, lo2, hi2;  // keys that some row sees: [lo, hi2); that all see: [lo2, hi)
+  seen_keys<PAGED>(a, span, i_first, lo, hi);
+  seen_keys<PAGED>(a, span, i_last, lo2, hi2);
+  const float *mask = !PAGED && a.mask ? a.mask + (long long)b * a.Sk : nullptr;
+  if (!PAGED && mask) {  // the first and the last valid position
+    int first = a.Sk, last = 0;
+    for (int j = lane; j < a.Sk; j += 64)
+      if (mask[j] != 0.f) first = min(first, j), last = j + 1;
+    lo = wave_ext<int, false>(first);
+    hi2 = wave_ext<int, true>(last);
+  }
+  if (SHARE) {
+    if (threadIdx.x == 0) dirty = 0;
+    __syncthreads();  // dirty is set from here on
+  }
+  lo &= ~(KT - 1);
+  int nt = hi2 > lo ? (hi2 - lo + KT - 1) / KT : 0;  // tiles of keys, this part's of them
+  {
+    const int per = (nt + plan.parts - 1) / plan.parts;
+    const int t0 = min(nt, part * per);
+    nt = min(nt, t0 + per) - t0;
+    lo += t0 * KT;
+  }
+  // ---- this lane's query
+  const int r = r0 + col;
+  const bool live = r < R;
+  const int qi = (live ? r : R - 1) / a.G, hq = h * a.G + (live ? r : R - 1) - qi * a.G;
+  int qlo, qhi;
+  seen_keys<PAGED>(a, span, qi, qlo, qhi);
+  Rows<T, DP> me;
+  me.start((const T *)a.q + ((long long)b * a.S + qi) * a.ldq + (long long)hq * a.Dh, live, a.Dh);
+  // ---- tiles of keys
+  char *const buf = lds + wave * 2 * TB;
+  Mover<T, DP, PAGED, KT, 64> mv;
+  bool odd = false;
+  const int every = SHARE ? 4 : 1;
+  int t = SHARE ? wave : 0;
+  if (t < nt) {
+    mv.start(a, b, h, lane, hi2 - 1, mask);
+    mv.look(lo + t * KT);
+    mv.fetch(lo + t * KT, every * KT);
+  }
+  for (; t < nt; t += every) {
+    const int k0 = lo + t * KT;
+    const bool mixed = k0 + KT > hi || k0 < lo2;
+    odd |= mv.put(k0, buf, mixed);
+    const unsigned seen = (unsigned)mv.seen;
+    // the wave's own LDS accesses are served in order
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (t + every < nt) mv.fetch(k0 + every * KT, every * KT);
+    f32x16 s[1] = {me.scores(buf, 0)};
+    if (PAGED ? mixed : seen != ~0u) hide<PAGED>(s[0], k0, qlo, qhi, seen);
+    me.weights(s, a.scale);
+    me.values(buf + TB, 0, s[0]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  if (PAGED && (SHARE ? wave : 0) < nt && mv.bad) atomicOr(a.err, kErrPage);
+  me.l = both_halves_sum(me.l);
+  // ---- results
+  const long long rows = (long long)a.B * a.Hq * a.S;
+  const Parts parts = parts_of(a.ws, rows, plan.parts);
+  const long long prow = part * rows + (long long)bh * a.S * a.G;
+  const bool cut = plan.parts > 1;
+  T *const y = (T *)a.y + ((long long)b * a.S + qi) * a.ldy + (long long)hq * a.Dh;
+  float *const po = parts.o + (prow + r) * a.Dh;
+  if (!SHARE) {
+    if (live) {
+      if (cut)
+        me.put_part(po, parts.ml + prow + r, a.Dh);
+      else
+        me.put(y, a.Dh);
+    }
+    odd = __any(odd);
+  } else {
+    if (odd) dirty = 1;
+    if (lane < 32) ends[wave][lane] = make_float2(me.m, me.l);
+    __syncthreads();
+    float m = kNegInf, l = 0.f;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) m = fmaxf(m, ends[v][col].x);
+    const float use = m == kNegInf ? 0.f : m;
+    auto factor = [&](float x) { return x == kNegInf ? 1.f : __builtin_amdgcn_exp2f(x - use); };  // sums without a maximum: zeros, or NaN
+#pragma unroll
+    for (int v = 0; v < 4; ++v) l = fmaf(ends[v][col].y, factor(ends[v][col].x), l);
+    // a wave's sums take its own part of LDS: group g of four features of a lane at (64 g + lane) * 16
+    const float c = factor(me.m);
+    float4 *const own = (float4 *)buf;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        own[(d * 4 + e / 4) * 64 + lane] = make_float4(me.o[d][e] * c, me.o[d][e + 1] * c, me.o[d][e + 2] * c, me.o[d][e + 3] * c);
+    static_assert(DB * 4 * 64 * 16 <= 2 * TB, "the sums fit into the wave's part");
+    __syncthreads();
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int x = 0; x < DB; ++x) {  // this wave's quarter of the groups
+      const int g = wave * DB + x, f = g * 8 + 4 * (lane >> 5);
+      float v[4] = {};
+#pragma unroll
+      for (int o = 0; o < 4; ++o) {
+        const float4 q = ((const float4 *)(lds + o * 2 * TB))[g * 64 + lane];
+        v[0] += q.x, v[1] += q.y, v[2] += q.z, v[3] += q.w;
+      }
+      if (!live || f >= a.Dh) continue;
+      if (cut) {
+        *(float4 *)(po + f) = make_float4(v[0], v[1], v[2], v[3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] *= inv;
+        Vec<T, 4>::put_any(y + f, v);
+      }
+    }
+    if (cut && live && wave == 0 && lane < 32) parts.ml[prow + r] = make_float2(m, l);
+    odd = dirty;
+  }
+  if (!PAGED || !odd) return;
+  // values that are no numbers where some rows see them and others not: row by row instead
+  if (SHARE) __syncthreads();
+  for (int x = SHARE ? wave : 0; x < kStepRows && r0 + x < R; x += SHARE ? 4 : 1) {
+    const int ii = (r0 + x) / a.G, hh = h * a.G + (r0 + x) - ii * a.G;
+    attend_one<T, PAGED>(a, span, b, ii, hh, lo, lo + nt * KT, (float *)buf, cut ? parts.o + (prow + r0 + x) * a.Dh : nullptr,
+                         cut ? parts.ml + prow + r0 + x : nullptr);
+  }
+}
+
+template <typename T, int DP, bool PAGED>
+hipError_t launch_steps_of(const MhaArgs &a, StepPlan plan, bool share, hipStream_t st) {
+  const long long jobs = (long long)a.B * a.Hk * plan.tiles * plan.parts, all = share ? jobs : (jobs + 3) / 4;
+  const long long most = 1 << 22;  // workgroups of a launch
+  for (long long first = 0; first < all; first += most) {
+    plan.first = (int)first;
+    const dim3 grid((unsigned)(all - first < most ? all - first : most)), block(256);
+    if (share)
+      hipLaunchKernelGGL((step_kernel<T, DP, PAGED, true>), grid, block, 0, st, a, plan);
+    else
+      hipLaunchKernelGGL((step_kernel<T, DP, PAGED, false>), grid, block, 0, st, a, plan);
+  }
+  return hipGetLastError();
+}
+
+template <typename T, bool PAGED>
+hipError_t launch_steps_as(const MhaArgs &a, const StepPlan &plan, bool share, hipStream_t st) {
+  if (a.Dh <= 64) return launch_steps_of<T, 64, PAGED>(a, plan, share, st);
+  if (a.Dh <= 128) return launch_steps_of<T, 128, PAGED>(a, plan, share, st);
+  if constexpr (sizeof(T) == 2) return launch_steps_of<T, 256, PAGED>(a, plan, share, st);
+  return hipErrorInvalidValue;  // fp32 heads of more than 128 features: a tile in flight would not fit a wave's registers
+}
+
+hipError_t launch_steps_bf16(const MhaArgs &a, const StepPlan &plan, bool share, hipStream_t st);
+hipError_t launch_steps_f32(const MhaArgs &a, const StepPlan &plan, bool share, hipStream_t st);
+
+}  // namespace mt

@@ -261,7 +261,8 @@ struct Mover {
       valid = mask[min(k0 + (int)(threadIdx.x & 63), last)];
     }
   }
-  __device__ __forceinline__ void fetch(int k0) {
+  // ahead: keys to the tile after it
+  __device__ __forceinline__ void fetch(int k0, int ahead) {
     if (!PAGED) {
       const int j = threadIdx.x & 63;
       seen = __ballot(j < KT && k0 + j <= last && (!mask || valid != 0.f));
@@ -281,7 +282,7 @@ struct Mover {
         __builtin_memcpy(&vr[x], &vv, 16);
       }
     }
-    look(k0 + KT);
+    look(k0 + ahead);
   }
   // The tile that was fetched, into LDS.  Values that no row may see are zeros (their weights are).  mixed: some rows see
   // keys of the tile that others do not; says whether one of its values is no number then, as its weights' zeros would
@@ -372,7 +373,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a,
   if (nt > 0) {
     mv.start(a, b, h, threadIdx.x, hi2 - 1, mask);
     mv.look(lo);
-    mv.fetch(lo);
+    mv.fetch(lo, KT);
     if (mv.put(lo, lds, mixed(lo))) dirty = 1;
   }
   for (int t = 0; t < nt; ++t) {
@@ -380,7 +381,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a,
     const char *buf = lds + (t & 1) * 2 * TB;
     const unsigned long long seen = mv.seen;
     __syncthreads();
-    if (t + 1 < nt) mv.fetch(k0 + KT);
+    if (t + 1 < nt) mv.fetch(k0 + KT, KT);
     f32x16 s[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) s[kb] = me.scores(buf, kb * 32);

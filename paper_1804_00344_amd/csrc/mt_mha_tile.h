@@ -19,10 +19,12 @@ struct Tile<bf16> {
   static constexpr int KT = 64;    // keys of a tile
   static constexpr int STEP = 16;  // features of a step of q.k
   typedef bf16x8 Q;                // features 16 s + 8 (lane / 32) + ..
-  // chunks of 16 bytes of a row are permuted by its number: 8 rows read at one feature (keys), or 4 rows at 16
-  // neighbouring ones (values, transposed), fall into different banks
-  __device__ static __forceinline__ int swap_k(int row) { return row & 7; }
-  __device__ static __forceinline__ int swap_v(int row) { return (row & 3) << 1; }
+  // the 64 banks take 16 rows' chunks of keys at a time, or 4 rows' chunks of 32 neighbouring features (values,
+  // transposed): the chunks of 16 bytes of a row are permuted by its number so that they fall into different banks
+  template <int ROWB>
+  __device__ static __forceinline__ int swap_v(int row) {
+    return ROWB >= 256 ? (row & 3) << 2 : (row & 2) << 1;
+  }
   __device__ static __forceinline__ void qk(f32x16 &s, const char *k, const Q &q) {
     s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8 *)k, q, s, 0, 0, 0);
   }
@@ -33,14 +35,22 @@ struct Tile<float> {
   static constexpr int KT = 32;
   static constexpr int STEP = 8;
   typedef f32x4 Q;  // features 8 s + 4 (lane / 32) + ..
-  __device__ static __forceinline__ int swap_k(int row) { return row & 7; }
-  __device__ static __forceinline__ int swap_v(int) { return 0; }
+  // values: 32 neighbouring features of two rows four apart
+  template <int ROWB>
+  __device__ static __forceinline__ int swap_v(int row) {
+    return (row & 4) << 1;
+  }
   __device__ static __forceinline__ void qk(f32x16 &s, const char *k, const Q &q) {
     const f32x4 kk = *(const f32x4 *)k;
 #pragma unroll
     for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kk[e], q[e], s, 0, 0, 0);
   }
 };
+
+template <int ROWB>
+__device__ __forceinline__ int swap_k(int row) {
+  return ROWB >= 256 ? row & 15 : (row >> 1) & 7;
+}
 
 __device__ __forceinline__ float both_halves_max(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
@@ -93,7 +103,7 @@ struct Rows {
     f32x16 s = (f32x16)(0.f);
     const int lane = threadIdx.x & 63, row = row0 + (lane & 31), half = lane >> 5;
 #pragma unroll
-    for (int st = 0; st < STEPS; ++st) M::qk(s, keys + row * ROWB + (((2 * st + half) ^ M::swap_k(row)) << 4), q[st]);
+    for (int st = 0; st < STEPS; ++st) M::qk(s, keys + row * ROWB + (((2 * st + half) ^ swap_k<ROWB>(row)) << 4), q[st]);
     return s;
   }
 
@@ -144,7 +154,7 @@ struct Rows {
         const char *from = vals + row * ROWB + (l16 & 1) * 8;
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
-          const int c = (4 * d + 2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1)) ^ M::swap_v(row);
+          const int c = (4 * d + 2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1)) ^ M::template swap_v<ROWB>(row);
           union {
             s16x4 q[2];
             bf16x8 v;
@@ -161,8 +171,9 @@ struct Rows {
         const int row = row0 + 8 * (e / 4) + 4 * half + e % 4;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(*(const float *)(vals + row * ROWB + (d * 32 + (lane & 31)) * 4), s[e], o[d],
-                                                      0, 0, 0);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(
+              *(const float *)(vals + row * ROWB + (((d * 32 + (lane & 31)) * 4) ^ (M::template swap_v<ROWB>(row) << 4))), s[e], o[d], 0,
+              0, 0);
       }
     }
   }
@@ -209,20 +220,23 @@ __device__ __forceinline__ void hide(f32x16 &s, int k0, int lo, int hi, unsigned
 constexpr int kTileRows = 128;
 
 // Brings tiles of KT keys and values from memory to LDS by TH threads: a tile's chunks of 16 bytes are on their way in
-// registers while the one before is computed, and its page numbers (mask) a tile earlier still.
+// registers while the one before is computed, and its page numbers (mask) a tile earlier still.  Tiles begin at a
+// multiple of KT, so a tile is a run of whole pages or lies inside one, and what a thread adds to either is the same in
+// every tile.
 template <typename T, int DP, bool PAGED, int KT, int TH>
 struct Mover {
   typedef Tile<T> M;
   static constexpr int ES = sizeof(T), CH = DP * ES / 16, ROWB = DP * ES, TB = KT * ROWB;
   static constexpr int NL = KT * CH / TH, RSTEP = TH / CH;  // chunks of a thread, all of one column
   static_assert(TH % CH == 0 && KT % RSTEP == 0, "a thread keeps its column");
-  const char *k, *v;        // of this key head (and sequence), this thread's column
-  long long ldk, ldv;       // bytes of a page, or of a row
+  const char *k, *v;        // of this key head (and sequence), this thread's column; not paged: its row of key 0 too
+  long long ldk, ldv;       // not paged: bytes of a row
+  unsigned page_bytes;
   const int32_t *table;
   const float *mask;
-  int row, chunk, last, plog, n_pages, rowb;
+  int row, chunk, last, plog, top, rowb;
   bool feature;             // whether the column is one of the head's
-  bool bad;                 // a page number was out of range
+  int bad;                  // not 0: a page number was out of range
   int pg[NL];
   float valid;              // mask of key lane of the next tile
   unsigned long long seen;  // keys of the tile on its way that are there and not masked
@@ -234,50 +248,64 @@ struct Mover {
     feature = chunk * 16 < a.Dh * ES;
     last = last_key;
     plog = a.page_log2;
-    n_pages = a.n_pages;
+    top = a.n_pages - 1;
     rowb = a.Dh * ES;
-    bad = false;
+    bad = 0;
     mask = m;
+    seen = 0;
     const long long col = feature ? chunk * 16 : 0;  // columns that only pad read the first one and become zeros
     if (PAGED) {
       table = a.table + (long long)b * a.n_blocks;
-      ldk = ldv = ((long long)a.Hk << plog) * rowb;
+      page_bytes = ((unsigned)a.Hk << plog) * rowb;
       const long long at = ((long long)h << plog) * rowb + col;
       k = (const char *)a.k + at;
       v = (const char *)a.v + at;
     } else {
       ldk = a.ldk * ES;
       ldv = a.ldv * ES;
-      k = (const char *)a.k + ((long long)b * a.Sk) * ldk + h * rowb + col;
-      v = (const char *)a.v + ((long long)b * a.Sk) * ldv + h * rowb + col;
+      k = (const char *)a.k + ((long long)b * a.Sk + row) * ldk + h * rowb + col;
+      v = (const char *)a.v + ((long long)b * a.Sk + row) * ldv + h * rowb + col;
     }
   }
-  // what a tile's loads will need: keys behind the last one are not read
+  // what a tile's loads will need; the rows behind the last key stand for that one
   __device__ __forceinline__ void look(int k0) {
     if (PAGED) {
+      if (k0 + KT - 1 <= last) {
+        const int32_t *t = table + (k0 >> plog);
 #pragma unroll
-      for (int x = 0; x < NL; ++x) pg[x] = table[min(k0 + row + x * RSTEP, last) >> plog];
+        for (int x = 0; x < NL; ++x) pg[x] = t[(unsigned)(row + x * RSTEP) >> plog];
+      } else {
+#pragma unroll
+        for (int x = 0; x < NL; ++x) pg[x] = table[min(k0 + row + x * RSTEP, last) >> plog];
+      }
     } else if (mask) {
       valid = mask[min(k0 + (int)(threadIdx.x & 63), last)];
     }
   }
   // ahead: keys to the tile after it
   __device__ __forceinline__ void fetch(int k0, int ahead) {
-    if (!PAGED) {
+    const bool whole = k0 + KT - 1 <= last;
+    if (PAGED) {
+      const int pmask = (1 << plog) - 1;
+      const unsigned inside = (k0 & pmask) * rowb;
+#pragma unroll
+      for (int x = 0; x < NL; ++x) {
+        const int page = min(max(pg[x], 0), top);
+        bad |= page ^ pg[x];
+        unsigned at = inside + ((row + x * RSTEP) & pmask) * rowb;
+        if (!whole) at = (min(k0 + row + x * RSTEP, last) & pmask) * rowb;
+        const unsigned long long off = (unsigned long long)(unsigned)page * page_bytes + at;
+        kr[x] = *(const int4 *)(k + off);
+        vr[x] = *(const int4 *)(v + off);
+      }
+    } else {
       const int j = threadIdx.x & 63;
       seen = __ballot(j < KT && k0 + j <= last && (!mask || valid != 0.f));
-    }
+      const char *kp = k + k0 * ldk, *vp = v + k0 * ldv;
 #pragma unroll
-    for (int x = 0; x < NL; ++x) {
-      const int j = min(k0 + row + x * RSTEP, last);
-      if (PAGED) {
-        bad |= (unsigned)pg[x] >= (unsigned)n_pages;
-        const int page = min(max(pg[x], 0), n_pages - 1);
-        const long long at = page * ldk + (j & ((1 << plog) - 1)) * rowb;
-        kr[x] = *(const int4 *)(k + at);
-        vr[x] = *(const int4 *)(v + at);
-      } else {
-        const auto kv = Vec<T, 16 / ES>::raw_any((const T *)(k + j * ldk)), vv = Vec<T, 16 / ES>::raw_any((const T *)(v + j * ldv));
+      for (int x = 0; x < NL; ++x) {
+        const int r = whole ? x * RSTEP : min(x * RSTEP, last - k0 - row);
+        const auto kv = Vec<T, 16 / ES>::raw_any((const T *)(kp + r * ldk)), vv = Vec<T, 16 / ES>::raw_any((const T *)(vp + r * ldv));
         __builtin_memcpy(&kr[x], &kv, 16);
         __builtin_memcpy(&vr[x], &vv, 16);
       }
@@ -289,18 +317,25 @@ struct Mover {
   // not hide that.
   __device__ __forceinline__ bool put(int k0, char *buf, bool mixed) {
     bool odd = false;
+    const bool all = PAGED ? k0 + KT - 1 <= last : seen == (KT == 64 ? ~0ull : (1ull << KT) - 1);
+    if (!all || rowb != ROWB) {
 #pragma unroll
-    for (int x = 0; x < NL; ++x) {
-      const int r = row + x * RSTEP;
-      const bool there = feature && (PAGED ? k0 + r <= last : (seen >> r) & 1);
-      if (!feature) kr[x] = make_int4(0, 0, 0, 0);
-      if (!there) vr[x] = make_int4(0, 0, 0, 0);
-      *(int4 *)(buf + r * ROWB + ((chunk ^ M::swap_k(r)) << 4)) = kr[x];
-      *(int4 *)(buf + TB + r * ROWB + ((chunk ^ M::swap_v(r)) << 4)) = vr[x];
+      for (int x = 0; x < NL; ++x) {
+        const int r = row + x * RSTEP;
+        const bool there = feature && (PAGED ? k0 + r <= last : (seen >> r) & 1);
+        if (!feature) kr[x] = make_int4(0, 0, 0, 0);
+        if (!there) vr[x] = make_int4(0, 0, 0, 0);
+      }
     }
     if (PAGED && mixed) {
 #pragma unroll
       for (int x = 0; x < NL; ++x) odd |= any_nonfinite<T>(vr[x]);
+    }
+#pragma unroll
+    for (int x = 0; x < NL; ++x) {
+      const int r = row + x * RSTEP;
+      *(int4 *)(buf + r * ROWB + ((chunk ^ swap_k<ROWB>(r)) << 4)) = kr[x];
+      *(int4 *)(buf + TB + r * ROWB + ((chunk ^ M::template swap_v<ROWB>(r)) << 4)) = vr[x];
     }
     return odd;
   }
@@ -324,11 +359,20 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a,
   __shared__ __attribute__((aligned(1024))) char lds[4 * TB];
   __shared__ int dirty, edge[2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31;
-  // consecutive tiles of a key head run on one XCD, whose L2 holds its keys and values; the last tiles, which see the
-  // most keys, first
-  const int w = plan.first + xcd_remap(blockIdx.x, gridDim.x);
-  const int part = w % plan.parts, u = w / plan.parts, bh = u / plan.tiles;
-  const int tile = plan.tiles - 1 - (u - bh * plan.tiles);
+  // the tiles of a key head run on one XCD, whose L2 holds its keys and values, the heads of a sequence on different
+  // ones; what does not divide among them is spread.  The last tiles, which see the most keys, come first.
+  const int w = plan.first + blockIdx.x, per = plan.tiles * plan.parts, heads = a.B * a.Hk, even = heads / kXcds * kXcds;
+  int bh, u;
+  if (w < even * per) {
+    const int v = w / kXcds;
+    bh = v / per * kXcds + w % kXcds;
+    u = v % per;
+  } else {
+    const int v = w - even * per;
+    bh = even + v / per;
+    u = v % per;
+  }
+  const int part = u % plan.parts, tile = plan.tiles - 1 - u / plan.parts;
   const int b = bh / a.Hk, h = bh - b * a.Hk;
   const RowSpan span = row_span<PAGED>(a, b, h == 0 && tile == 0 && part == 0 && threadIdx.x == 0);
   const int R = span.n * a.G, r0 = tile * kTileRows;

@@ -69,7 +69,7 @@ hipError_t launch_mha(const MhaArgs &a, hipStream_t st) {
   const Plan p = plan_of(a.Hq, a.Hk, a.Dh, a.B, a.S, a.table ? (long long)a.n_blocks << a.page_log2 : a.Sk, !a.bf16_io, a.num_cu);
   hipError_t e;
   if (p.step) {
-    const StepPlan s{p.tiles, p.parts, 0};
+    const StepPlan s{p.tiles, p.parts, 0, 0};
     e = a.bf16_io ? launch_steps_bf16(a, s, p.share, st) : launch_steps_f32(a, s, p.share, st);
   } else {
     const TilePlan t{p.tiles, p.parts, 0};

@@ -12,6 +12,7 @@ struct StepPlan {
   int tiles;  // of kStepRows rows of a sequence's key head
   int parts;  // the key axis is cut into
   int first;  // workgroup of this launch
+  unsigned jobs;  // rows' tiles of all key heads and parts: below 2^31
 };
 
 // Tiles of 32 rows of one key head (as in the tile kernel) and 32 keys at a time, each wave with its own part of LDS and
@@ -23,12 +24,10 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T
   __shared__ __attribute__((aligned(1024))) char lds[4 * 2 * TB];
   __shared__ float2 ends[4][32];
   __shared__ int dirty;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31;
-  const long long jobs = (long long)a.B * a.Hk * plan.tiles * plan.parts;
-  const int w = plan.first + xcd_remap(blockIdx.x, gridDim.x);
-  const long long job = SHARE ? w : w * 4ll + wave;
-  if (job >= jobs) return;
-  const int part = (int)(job % plan.parts), u = (int)(job / plan.parts), bh = u / plan.tiles, tile = u - bh * plan.tiles;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31;
+  const unsigned w = plan.first + xcd_remap(blockIdx.x, gridDim.x), job = SHARE ? w : w * 4 + wave;
+  if (job >= plan.jobs) return;
+  const int part = (int)(job % (unsigned)plan.parts), u = (int)(job / (unsigned)plan.parts), bh = u / plan.tiles, tile = u - bh * plan.tiles;
   const int b = bh / a.Hk, h = bh - b * a.Hk;
   const RowSpan span = row_span<PAGED>(a, b, h == 0 && tile == 0 && part == 0 && lane == 0);
   const int R = span.n * a.G, r0 = tile * kStepRows;
@@ -165,6 +164,7 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T
 template <typename T, int DP, bool PAGED>
 hipError_t launch_steps_of(const MhaArgs &a, StepPlan plan, bool share, hipStream_t st) {
   const long long jobs = (long long)a.B * a.Hk * plan.tiles * plan.parts, all = share ? jobs : (jobs + 3) / 4;
+  plan.jobs = (unsigned)jobs;
   const long long most = 1 << 22;  // workgroups of a launch
   for (long long first = 0; first < all; first += most) {
     plan.first = (int)first;

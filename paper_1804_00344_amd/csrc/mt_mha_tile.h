@@ -61,16 +61,19 @@ __device__ __forceinline__ float both_halves_sum(float v) {
   return __int_as_float(r[0]) + __int_as_float(r[1]);
 }
 
+// Sets bits of `over` where one of the elements of v is an infinity or a NaN: an exponent of all ones passes into the
+// sign's place when one is added.
 template <typename T>
-__device__ __forceinline__ bool any_nonfinite(const int4 &v) {
-  const unsigned w[4] = {(unsigned)v.x, (unsigned)v.y, (unsigned)v.z, (unsigned)v.w};
-  bool bad = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (sizeof(T) == 2) bad |= (w[i] & 0x7f80u) == 0x7f80u;
-    bad |= (w[i] & 0x7f800000u) == 0x7f800000u;
-  }
-  return bad;
+__device__ __forceinline__ void note_nonfinite(const int4 &v, unsigned &over) {
+  constexpr unsigned field = sizeof(T) == 2 ? 0x7f807f80u : 0x7f800000u, one = sizeof(T) == 2 ? 0x00800080u : 0x00800000u;
+  over |= ((unsigned)v.x & field) + one;
+  over |= ((unsigned)v.y & field) + one;
+  over |= ((unsigned)v.z & field) + one;
+  over |= ((unsigned)v.w & field) + one;
+}
+template <typename T>
+__device__ __forceinline__ bool nonfinite(unsigned over) {
+  return over & (sizeof(T) == 2 ? 0x80008000u : 0x80000000u);
 }
 
 // One wave's 32 queries, a query per lane (and half of a tile's keys): its features, and the running softmax.
@@ -220,21 +223,23 @@ __device__ __forceinline__ void hide(f32x16 &s, int k0, int lo, int hi, unsigned
 constexpr int kTileRows = 128;
 
 // Brings tiles of KT keys and values from memory to LDS by TH threads: a tile's chunks of 16 bytes are on their way in
-// registers while the one before is computed, and its page numbers (mask) a tile earlier still.  Tiles begin at a
-// multiple of KT, so a tile is a run of whole pages or lies inside one, and what a thread adds to either is the same in
-// every tile.
+// registers while the one before is computed, and its page numbers (mask) a tile earlier still.  A wave's 64 chunks are at
+// most eight neighbouring rows, beginning at a multiple of their number, so they lie in one page: page numbers and
+// bases are the wave's, and what a lane adds to them is the same in every tile.
 template <typename T, int DP, bool PAGED, int KT, int TH>
 struct Mover {
   typedef Tile<T> M;
   static constexpr int ES = sizeof(T), CH = DP * ES / 16, ROWB = DP * ES, TB = KT * ROWB;
   static constexpr int NL = KT * CH / TH, RSTEP = TH / CH;  // chunks of a thread, all of one column
-  static_assert(TH % CH == 0 && KT % RSTEP == 0, "a thread keeps its column");
-  const char *k, *v;        // of this key head (and sequence), this thread's column; not paged: its row of key 0 too
+  static_assert(TH % CH == 0 && KT % RSTEP == 0 && 64 % CH == 0 && 64 / CH <= 8, "a wave's rows lie in one page");
+  const char *k, *v;        // of this key head (and sequence)
   long long ldk, ldv;       // not paged: bytes of a row
+  long long lane_k, lane_v; // not paged: this lane's bytes from its wave's first row
+  unsigned lane_at;         // paged: the same
   unsigned page_bytes;
   const int32_t *table;
   const float *mask;
-  int row, chunk, last, plog, top, rowb;
+  int row, chunk, wave_row, last, plog, top, rowb;
   bool feature;             // whether the column is one of the head's
   int bad;                  // not 0: a page number was out of range
   int pg[NL];
@@ -245,6 +250,7 @@ struct Mover {
   __device__ __forceinline__ void start(const MhaArgs &a, int b, int h, int tid, int last_key, const float *m) {
     row = tid / CH;
     chunk = tid % CH;
+    wave_row = TH == 64 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6) * (64 / CH);
     feature = chunk * 16 < a.Dh * ES;
     last = last_key;
     plog = a.page_log2;
@@ -253,70 +259,71 @@ struct Mover {
     bad = 0;
     mask = m;
     seen = 0;
-    const long long col = feature ? chunk * 16 : 0;  // columns that only pad read the first one and become zeros
+    const int col = feature ? chunk * 16 : 0;  // columns that only pad read the first one and become zeros
     if (PAGED) {
       table = a.table + (long long)b * a.n_blocks;
       page_bytes = ((unsigned)a.Hk << plog) * rowb;
-      const long long at = ((long long)h << plog) * rowb + col;
+      const long long at = ((long long)h << plog) * rowb;
       k = (const char *)a.k + at;
       v = (const char *)a.v + at;
+      lane_at = (row - wave_row) * rowb + col;
     } else {
       ldk = a.ldk * ES;
       ldv = a.ldv * ES;
-      k = (const char *)a.k + ((long long)b * a.Sk + row) * ldk + h * rowb + col;
-      v = (const char *)a.v + ((long long)b * a.Sk + row) * ldv + h * rowb + col;
+      k = (const char *)a.k + (long long)b * a.Sk * ldk + h * rowb;
+      v = (const char *)a.v + (long long)b * a.Sk * ldv + h * rowb;
+      lane_k = (row - wave_row) * ldk + col;
+      lane_v = (row - wave_row) * ldv + col;
     }
   }
-  // what a tile's loads will need; the rows behind the last key stand for that one
+  // what a tile's loads will need; blocks behind the last key stand for its own
   __device__ __forceinline__ void look(int k0) {
     if (PAGED) {
-      if (k0 + KT - 1 <= last) {
-        const int32_t *t = table + (k0 >> plog);
 #pragma unroll
-        for (int x = 0; x < NL; ++x) pg[x] = t[(unsigned)(row + x * RSTEP) >> plog];
-      } else {
-#pragma unroll
-        for (int x = 0; x < NL; ++x) pg[x] = table[min(k0 + row + x * RSTEP, last) >> plog];
-      }
+      for (int x = 0; x < NL; ++x) pg[x] = table[min(k0 + wave_row + x * RSTEP, last) >> plog];
     } else if (mask) {
       valid = mask[min(k0 + (int)(threadIdx.x & 63), last)];
     }
   }
   // ahead: keys to the tile after it
   __device__ __forceinline__ void fetch(int k0, int ahead) {
-    const bool whole = k0 + KT - 1 <= last;
     if (PAGED) {
+      // positions behind the last key are read too, inside its page; put makes zeros of their values
       const int pmask = (1 << plog) - 1;
-      const unsigned inside = (k0 & pmask) * rowb;
 #pragma unroll
       for (int x = 0; x < NL; ++x) {
         const int page = min(max(pg[x], 0), top);
         bad |= page ^ pg[x];
-        unsigned at = inside + ((row + x * RSTEP) & pmask) * rowb;
-        if (!whole) at = (min(k0 + row + x * RSTEP, last) & pmask) * rowb;
-        const unsigned long long off = (unsigned long long)(unsigned)page * page_bytes + at;
-        kr[x] = *(const int4 *)(k + off);
-        vr[x] = *(const int4 *)(v + off);
+        const unsigned long long at = (unsigned long long)(unsigned)page * page_bytes + (unsigned)((k0 + wave_row + x * RSTEP) & pmask) * rowb;
+        kr[x] = *(const int4 *)(k + at + lane_at);
+        vr[x] = *(const int4 *)(v + at + lane_at);
       }
     } else {
       const int j = threadIdx.x & 63;
       seen = __ballot(j < KT && k0 + j <= last && (!mask || valid != 0.f));
-      const char *kp = k + k0 * ldk, *vp = v + k0 * ldv;
+      if (k0 + KT - 1 <= last) {
 #pragma unroll
-      for (int x = 0; x < NL; ++x) {
-        const int r = whole ? x * RSTEP : min(x * RSTEP, last - k0 - row);
-        const auto kv = Vec<T, 16 / ES>::raw_any((const T *)(kp + r * ldk)), vv = Vec<T, 16 / ES>::raw_any((const T *)(vp + r * ldv));
-        __builtin_memcpy(&kr[x], &kv, 16);
-        __builtin_memcpy(&vr[x], &vv, 16);
+        for (int x = 0; x < NL; ++x) load_rows(x, (k0 + wave_row + x * RSTEP) * ldk + lane_k, (k0 + wave_row + x * RSTEP) * ldv + lane_v);
+      } else {  // rows behind the last key stand for it
+#pragma unroll
+        for (int x = 0; x < NL; ++x) {
+          const long long back = min(0, last - (k0 + row + x * RSTEP));
+          load_rows(x, (k0 + wave_row + x * RSTEP + back) * ldk + lane_k, (k0 + wave_row + x * RSTEP + back) * ldv + lane_v);
+        }
       }
     }
     look(k0 + ahead);
+  }
+  __device__ __forceinline__ void load_rows(int x, long long ak, long long av) {
+    const auto kv = Vec<T, 16 / ES>::raw_any((const T *)(k + ak)), vv = Vec<T, 16 / ES>::raw_any((const T *)(v + av));
+    __builtin_memcpy(&kr[x], &kv, 16);
+    __builtin_memcpy(&vr[x], &vv, 16);
   }
   // The tile that was fetched, into LDS.  Values that no row may see are zeros (their weights are).  mixed: some rows see
   // keys of the tile that others do not; says whether one of its values is no number then, as its weights' zeros would
   // not hide that.
   __device__ __forceinline__ bool put(int k0, char *buf, bool mixed) {
-    bool odd = false;
+    unsigned over = 0;
     const bool all = PAGED ? k0 + KT - 1 <= last : seen == (KT == 64 ? ~0ull : (1ull << KT) - 1);
     if (!all || rowb != ROWB) {
 #pragma unroll
@@ -329,7 +336,7 @@ struct Mover {
     }
     if (PAGED && mixed) {
 #pragma unroll
-      for (int x = 0; x < NL; ++x) odd |= any_nonfinite<T>(vr[x]);
+      for (int x = 0; x < NL; ++x) note_nonfinite<T>(vr[x], over);
     }
 #pragma unroll
     for (int x = 0; x < NL; ++x) {
@@ -337,7 +344,7 @@ struct Mover {
       *(int4 *)(buf + r * ROWB + ((chunk ^ swap_k<ROWB>(r)) << 4)) = kr[x];
       *(int4 *)(buf + TB + r * ROWB + ((chunk ^ M::template swap_v<ROWB>(r)) << 4)) = vr[x];
     }
-    return odd;
+    return nonfinite<T>(over);
   }
 };
 
@@ -358,7 +365,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a,
   constexpr int KT = M::KT, TB = KT * DP * (int)sizeof(T), KB = KT / 32;
   __shared__ __attribute__((aligned(1024))) char lds[4 * TB];
   __shared__ int dirty, edge[2];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31;
   // the tiles of a key head run on one XCD, whose L2 holds its keys and values, the heads of a sequence on different
   // ones; what does not divide among them is spread.  The last tiles, which see the most keys, come first.
   const int w = plan.first + blockIdx.x, per = plan.tiles * plan.parts, heads = a.B * a.Hk, even = heads / kXcds * kXcds;

@@ -9,14 +9,13 @@ namespace {
 constexpr int kRowChunk = 256, kPageChunk = 4096;
 
 // Workspace: per page its references, those by rows that go on writing it, and the last such row + 1; per row its needs
-// and where they begin within its chunk; per chunk of rows and of pages their sums; the free (packed: used) pages in order
+// and where they begin; per chunk of rows and of pages their sums; the free (packed: used) pages in order
 struct Space {
   int *refs, *growers, *last;  // [n_pages]
   int *list;                   // [n_pages]
-  int *begin;                  // [M] need before the row within its chunk; the row's own need in the upper half of need
-  int *need;                   // [M]
+  int *begin, *need;           // [M] pages that the rows before a row take, and its own
   int *row_sum, *page_sum;     // per chunk
-  int *flags;                  // [4]: too long a row
+  int *flags;                  // [4]: too long a row; pages needed; pages free (packed: used)
 };
 
 __host__ __device__ inline int chunks(int n, int c) { return (n + c - 1) / c; }
@@ -167,11 +166,18 @@ __global__ void __launch_bounds__(256) need_kernel(PagesArgs a, Space s, int row
   if (threadIdx.x == 0) s.page_sum[c] = total;
 }
 
-// The free pages in order; PACK: every used page's number in the order instead.
+// The free pages in order; PACK: every used page's number in the order too.  The last workgroups: where the rows' needs begin.
 template <bool PACK>
-__global__ void __launch_bounds__(256) list_kernel(PagesArgs a, Space s) {
+__global__ void __launch_bounds__(256) list_kernel(PagesArgs a, Space s, int row_chunks, int page_chunks) {
+  if ((int)blockIdx.x >= page_chunks) {
+    const int c = blockIdx.x - page_chunks, m = c * kRowChunk + threadIdx.x, before = sum_before(s.row_sum, c);
+    if (m < a.M) s.begin[m] += before;
+    if (c == row_chunks - 1 && threadIdx.x == 0) s.flags[1] = before + s.row_sum[c];
+    return;
+  }
   const int p0 = blockIdx.x * kPageChunk;
   int at = sum_before(s.page_sum, blockIdx.x);
+  if ((int)blockIdx.x == page_chunks - 1 && threadIdx.x == 0) s.flags[2] = at + s.page_sum[blockIdx.x];
   constexpr int PER = kPageChunk / 256;  // a thread's pages are neighbours
   const int first = p0 + threadIdx.x * PER;
   int n = 0, total;
@@ -188,21 +194,130 @@ __global__ void __launch_bounds__(256) list_kernel(PagesArgs a, Space s) {
     }
 }
 
+// All of the above by one workgroup, the counts in LDS, for tables and pools of moderate size: 5 rows of a pool of 23
+// pages 15 -> 9 us with the copies, 768 rows of 3900 pages 38 -> 27.
+constexpr int kSmallPages = 8192, kSmallEntries = 1 << 15;
+
+template <bool GROW>
+__global__ void __launch_bounds__(1024) small_kernel(PagesArgs a, Space s) {
+  __shared__ int refs[kSmallPages], growers[GROW ? kSmallPages : 1], last[GROW ? kSmallPages : 1];
+  __shared__ int sums[16], too_long;
+  for (int p = threadIdx.x; p < a.n_pages; p += 1024) {
+    refs[p] = 0;
+    if (GROW) growers[p] = last[p] = 0;
+  }
+  if (threadIdx.x == 0) too_long = 0;
+  __syncthreads();
+  const int n = a.M * a.n_blocks, pmask = (1 << a.page_log2) - 1;
+  for (int e = threadIdx.x; e < n; e += 1024) {
+    const int m = e / a.n_blocks, j = e - m * a.n_blocks;
+    const Row r = row_of(a, m, j == 0);
+    int p = -1;
+    if (j < r.blocks) {
+      p = page_of(a, r, j, true);
+      if (GROW) {
+        atomicAdd(&refs[p], 1);
+        if (j == r.blocks - 1 && r.add > 0 && (r.len & pmask)) {
+          atomicAdd(&growers[p], 1);
+          atomicMax(&last[p], m + 1);
+        }
+      } else {
+        refs[p] = 1;
+      }
+    }
+    if (GROW) a.table_out[e] = p;
+  }
+  __syncthreads();
+  // sum over the workgroup, and of the threads before this one
+  auto scan = [&](int v, int &total) {
+    const int incl = wave_incl_scan(v), w = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 63) sums[w] = incl;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (i < w) before += sums[i];
+      total += sums[i];
+    }
+    __syncthreads();
+    return before + incl - v;
+  };
+  int total, need_all = 0;
+  if (GROW) {
+    for (int m0 = 0; m0 < a.M; m0 += 1024) {
+      const int m = m0 + threadIdx.x;
+      int need = 0;
+      if (m < a.M) {
+        const Row r = row_of(a, m, false);
+        const int after = blocks_after(a, r);
+        if (after > a.n_blocks) {
+          too_long = 1;
+        } else {
+          need = after - r.blocks;
+          if (r.add > 0 && (r.len & pmask)) {
+            const int p = page_of(a, r, r.blocks - 1, false);
+            need += refs[p] > 1 && !(last[p] == m + 1 && growers[p] == refs[p]);
+          }
+        }
+      }
+      const int before = scan(need, total);
+      if (m < a.M) {
+        s.begin[m] = need_all + before;
+        s.need[m] = need;
+      }
+      need_all += total;
+    }
+  }
+  const int per = (a.n_pages + 1023) / 1024, first = threadIdx.x * per;  // a thread's pages are neighbours
+  int mine = 0;
+  for (int i = 0; i < per; ++i)
+    if (first + i < a.n_pages) mine += (refs[first + i] == 0) == GROW;
+  int at = scan(mine, total);
+  for (int i = 0; i < per; ++i)
+    if (first + i < a.n_pages && (refs[first + i] == 0) == GROW) {
+      s.list[at] = first + i;
+      if (!GROW) s.growers[first + i] = at;
+      ++at;
+    }
+  if (threadIdx.x == 0) {
+    s.flags[0] = too_long;
+    s.flags[1] = need_all;
+    s.flags[2] = total;
+  }
+}
+
 // bytes of one page of one layer's keys or values
 __device__ __forceinline__ long long page_size(const PagesArgs &a) { return (a.head_bytes << a.page_log2) * a.Hk; }
 
-__device__ __forceinline__ void copy16(char *dst, const char *src, long long bytes, int t, int n) {
-  for (long long o = t * 16ll; o < bytes; o += n * 16ll) *(int4 *)(dst + o) = *(const int4 *)(src + o);
+// n chunks of 16 bytes by the workgroup, four of a thread on their way at a time; where(i): chunk i's offset
+template <typename F>
+__device__ __forceinline__ void copy_chunks(char *dst, const char *src, int n, F where) {
+  int i = threadIdx.x;
+  for (; i - (int)threadIdx.x + 1024 <= n; i += 1024) {
+    long long at[4];
+    int4 v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      at[u] = where(i + u * 256);
+      v[u] = *(const int4 *)(src + at[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) *(int4 *)(dst + at[u]) = v[u];
+  }
+  for (; i < n; i += 256) {
+    const long long at = where(i);
+    *(int4 *)(dst + at) = *(const int4 *)(src + at);
+  }
 }
 
-// Row m: its table and length, and (every slice blockIdx.y: a layer's keys or values) the copy of its shared page.
-__global__ void __launch_bounds__(256) assign_kernel(PagesArgs a, Space s, int row_chunks, int page_chunks) {
+// Row m: its table and length, and (blockIdx.y: a layer's keys or values) the copy of its shared page.
+__global__ void __launch_bounds__(256) assign_kernel(PagesArgs a, Space s) {
   const int m = blockIdx.x;
-  const int need_all = sum_before(s.row_sum, row_chunks), free_all = sum_before(s.page_sum, page_chunks);
-  const bool fails = s.flags[0] || need_all > free_all;
+  const int need_all = s.flags[1], free_all = s.flags[2], begin = s.begin[m], need = s.need[m];
   int *const row = a.table_out + (long long)m * a.n_blocks;
   const Row r = row_of(a, m, false);
-  if (fails) {
+  if (s.flags[0] || need_all > free_all) {
     if (blockIdx.y) return;
     for (int j = threadIdx.x; j < a.n_blocks; j += 256) row[j] = -1;
     if (threadIdx.x == 0) {
@@ -214,8 +329,7 @@ __global__ void __launch_bounds__(256) assign_kernel(PagesArgs a, Space s, int r
     }
     return;
   }
-  const int after = blocks_after(a, r), cow = s.need[m] - (after - r.blocks);
-  const int begin = s.begin[m] + sum_before(s.row_sum, m / kRowChunk);
+  const int after = blocks_after(a, r), cow = need - (after - r.blocks);
   if (blockIdx.y == 0) {
     for (int j = threadIdx.x; j < after - r.blocks; j += 256) row[r.blocks + j] = s.list[begin + cow + j];
     if (threadIdx.x == 0) {
@@ -225,40 +339,43 @@ __global__ void __launch_bounds__(256) assign_kernel(PagesArgs a, Space s, int r
     }
   }
   if (!cow) return;
-  const int from = page_of(a, r, r.blocks - 1, false), to = s.list[begin];
-  const long long bytes = (r.len & ((1 << a.page_log2) - 1)) * a.head_bytes, head = a.head_bytes << a.page_log2;
-  const int layer = blockIdx.y >> 1;
-  char *base = (char *)(blockIdx.y & 1 ? a.v_out : a.k_out) + (long long)layer * a.n_pages * page_size(a);
-  for (int h = 0; h < a.Hk; ++h)
-    copy16(base + to * page_size(a) + h * head, base + from * page_size(a) + h * head, bytes, threadIdx.x, 256);
+  const long long size = page_size(a), base = (long long)(blockIdx.y >> 1) * a.n_pages * size;
+  const long long from = base + page_of(a, r, r.blocks - 1, false) * size, to = base + s.list[begin] * size;
+  char *const cache = (char *)(blockIdx.y & 1 ? a.v_out : a.k_out);
+  // the positions so far: a run of every head
+  const int run = (int)((r.len & ((1 << a.page_log2) - 1)) * a.head_bytes / 16), head = (int)(a.head_bytes << a.page_log2);
+  auto where = [&](int i) __attribute__((always_inline)) -> long long {
+    const int h = i / run;
+    return h * head + (i - h * run) * 16;
+  };
+  copy_chunks(cache + to, cache + from, run * a.Hk, where);
 }
 
-// Pack: the tables renumbered
-__global__ void __launch_bounds__(256) renumber_kernel(PagesArgs a, Space s, int page_chunks) {
-  const int used = sum_before(s.page_sum, page_chunks);
+// Pack: the pages, each slice blockIdx.y a layer's keys or values; the last slice: the tables renumbered
+__global__ void __launch_bounds__(256) move_kernel(PagesArgs a, Space s) {
+  const int used = s.flags[2];
   const bool fails = used > a.n_pages_out;
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    if (a.free_out) *a.free_out = fails ? 0 : used;
-    if (fails) atomicOr(a.err, kErrRoom);
+  if ((int)blockIdx.y == 2 * a.layers) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+      if (a.free_out) *a.free_out = fails ? 0 : used;
+      if (fails) atomicOr(a.err, kErrRoom);
+    }
+    const long long n = (long long)a.M * a.n_blocks;
+    for (long long e = blockIdx.x * 256ll + threadIdx.x; e < n; e += gridDim.x * 256ll) {
+      const int m = (int)(e / a.n_blocks), j = (int)(e - (long long)m * a.n_blocks);
+      const Row r = row_of(a, m, false);
+      a.table_out[e] = !fails && j < r.blocks ? s.growers[page_of(a, r, j, false)] : -1;
+      if (j == 0) a.len_out[m] = fails ? 0 : r.len;
+    }
+    return;
   }
-  const long long n = (long long)a.M * a.n_blocks;
-  for (long long e = blockIdx.x * 256ll + threadIdx.x; e < n; e += gridDim.x * 256ll) {
-    const int m = (int)(e / a.n_blocks), j = (int)(e - (long long)m * a.n_blocks);
-    const Row r = row_of(a, m, false);
-    a.table_out[e] = !fails && j < r.blocks ? s.growers[page_of(a, r, j, false)] : -1;
-    if (j == 0) a.len_out[m] = fails ? 0 : r.len;
-  }
-}
-
-// Pack: the pages, each slice blockIdx.y a layer's keys or values
-__global__ void __launch_bounds__(256) move_kernel(PagesArgs a, Space s, int page_chunks) {
-  const int used = sum_before(s.page_sum, page_chunks);
-  if (used > a.n_pages_out) return;
+  if (fails) return;
   const long long size = page_size(a);
   const int layer = blockIdx.y >> 1;
   const char *in = (const char *)(blockIdx.y & 1 ? a.v_in : a.k_in) + (long long)layer * a.n_pages * size;
   char *out = (char *)(blockIdx.y & 1 ? a.v_out : a.k_out) + (long long)layer * a.n_pages_out * size;
-  for (int i = blockIdx.x; i < used; i += gridDim.x) copy16(out + i * size, in + s.list[i] * size, size, threadIdx.x, 256);
+  for (int i = blockIdx.x; i < used; i += gridDim.x)
+    copy_chunks(out + i * size, in + s.list[i] * size, (int)(size / 16), [](int c) __attribute__((always_inline)) { return c * 16ll; });
 }
 
 }  // namespace
@@ -268,31 +385,39 @@ size_t pages_workspace_bytes(int M, int n_pages) {
   return (size_t)((n * 4 + 255) / 256 * 256);
 }
 
-hipError_t launch_advance(const PagesArgs &a, hipStream_t st) {
-  const Space s = space(a.ws, a.M, a.n_pages);
-  const int rc = chunks(a.M, kRowChunk), pc = chunks(a.n_pages, kPageChunk);
-  const long long clear = 4 + 3ll * a.n_pages, n = (long long)a.M * a.n_blocks;
+namespace {
+
+// The plan of a call: what every row needs, and the free (used) pages in order
+template <bool GROW>
+void plan(const PagesArgs &a, const Space &s, hipStream_t st) {
+  const long long n = (long long)a.M * a.n_blocks;
+  if (a.n_pages <= kSmallPages && n <= kSmallEntries) {
+    hipLaunchKernelGGL(small_kernel<GROW>, dim3(1), dim3(1024), 0, st, a, s);
+    return;
+  }
+  const int rc = GROW ? chunks(a.M, kRowChunk) : 0, pc = chunks(a.n_pages, kPageChunk);
+  const long long clear = 4 + (GROW ? 3ll : 1ll) * a.n_pages;
   auto blocks = [](long long k) { return dim3((unsigned)(k < 256 * 4096 ? (k + 255) / 256 : 4096)); };
   hipLaunchKernelGGL(clear_kernel, blocks(clear), dim3(256), 0, st, s.flags, clear);
-  hipLaunchKernelGGL(count_kernel<true>, blocks(n), dim3(256), 0, st, a, s);
-  hipLaunchKernelGGL(need_kernel<true>, dim3(rc + pc), dim3(256), 0, st, a, s, rc);
-  hipLaunchKernelGGL(list_kernel<false>, dim3(pc), dim3(256), 0, st, a, s);
-  hipLaunchKernelGGL(assign_kernel, dim3(a.M, 2 * a.layers), dim3(256), 0, st, a, s, rc, pc);
+  hipLaunchKernelGGL(count_kernel<GROW>, blocks(n), dim3(256), 0, st, a, s);
+  hipLaunchKernelGGL(need_kernel<GROW>, dim3(rc + pc), dim3(256), 0, st, a, s, rc);
+  hipLaunchKernelGGL(list_kernel<!GROW>, dim3(rc + pc), dim3(256), 0, st, a, s, rc, pc);
+}
+
+}  // namespace
+
+hipError_t launch_advance(const PagesArgs &a, hipStream_t st) {
+  const Space s = space(a.ws, a.M, a.n_pages);
+  plan<true>(a, s, st);
+  hipLaunchKernelGGL(assign_kernel, dim3(a.M, 2 * a.layers), dim3(256), 0, st, a, s);
   return hipGetLastError();
 }
 
 hipError_t launch_pack(const PagesArgs &a, hipStream_t st) {
   const Space s = space(a.ws, a.M, a.n_pages);
-  const int pc = chunks(a.n_pages, kPageChunk);
-  const long long clear = 4 + (long long)a.n_pages, n = (long long)a.M * a.n_blocks;
-  auto blocks = [](long long k) { return dim3((unsigned)(k < 256 * 4096 ? (k + 255) / 256 : 4096)); };
-  hipLaunchKernelGGL(clear_kernel, blocks(clear), dim3(256), 0, st, s.flags, clear);
-  hipLaunchKernelGGL(count_kernel<false>, blocks(n), dim3(256), 0, st, a, s);
-  hipLaunchKernelGGL(need_kernel<false>, dim3(pc), dim3(256), 0, st, a, s, 0);
-  hipLaunchKernelGGL(list_kernel<true>, dim3(pc), dim3(256), 0, st, a, s);
-  hipLaunchKernelGGL(renumber_kernel, blocks(n), dim3(256), 0, st, a, s, pc);
+  plan<false>(a, s, st);
   const int most = a.n_pages < a.n_pages_out ? a.n_pages : a.n_pages_out;
-  hipLaunchKernelGGL(move_kernel, dim3(most < 65536 ? most : 65536, 2 * a.layers), dim3(256), 0, st, a, s, pc);
+  hipLaunchKernelGGL(move_kernel, dim3(most < 65536 ? most : 65536, 2 * a.layers + 1), dim3(256), 0, st, a, s);
   return hipGetLastError();
 }
 

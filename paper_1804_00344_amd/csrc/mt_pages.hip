@@ -277,9 +277,23 @@ __global__ void __launch_bounds__(1024) small_kernel(PagesArgs a, Space s) {
   for (int i = 0; i < per; ++i)
     if (first + i < a.n_pages && (refs[first + i] == 0) == GROW) {
       s.list[at] = first + i;
-      if (!GROW) s.growers[first + i] = at;
+      if (!GROW) refs[first + i] = at;
       ++at;
     }
+  if (!GROW) {  // the tables renumbered
+    __syncthreads();
+    const bool fails = total > a.n_pages_out;
+    for (int e = threadIdx.x; e < n; e += 1024) {
+      const int m = e / a.n_blocks, j = e - m * a.n_blocks;
+      const Row r = row_of(a, m, false);
+      a.table_out[e] = !fails && j < r.blocks ? refs[page_of(a, r, j, false)] : -1;
+      if (j == 0) a.len_out[m] = fails ? 0 : r.len;
+    }
+    if (threadIdx.x == 0) {
+      if (a.free_out) *a.free_out = fails ? 0 : total;
+      if (fails) atomicOr(a.err, kErrRoom);
+    }
+  }
   if (threadIdx.x == 0) {
     s.flags[0] = too_long;
     s.flags[1] = need_all;
@@ -293,21 +307,19 @@ __device__ __forceinline__ long long page_size(const PagesArgs &a) { return (a.h
 // n chunks of 16 bytes by the workgroup, four of a thread on their way at a time; where(i): chunk i's offset
 template <typename F>
 __device__ __forceinline__ void copy_chunks(char *dst, const char *src, int n, F where) {
+  typedef int v4 __attribute__((ext_vector_type(4)));
   int i = threadIdx.x;
   for (; i - (int)threadIdx.x + 1024 <= n; i += 1024) {
-    long long at[4];
-    int4 v[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      at[u] = where(i + u * 256);
-      v[u] = *(const int4 *)(src + at[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) *(int4 *)(dst + at[u]) = v[u];
+    const long long a0 = where(i), a1 = where(i + 256), a2 = where(i + 512), a3 = where(i + 768);
+    const v4 v0 = *(const v4 *)(src + a0), v1 = *(const v4 *)(src + a1), v2 = *(const v4 *)(src + a2), v3 = *(const v4 *)(src + a3);
+    *(v4 *)(dst + a0) = v0;
+    *(v4 *)(dst + a1) = v1;
+    *(v4 *)(dst + a2) = v2;
+    *(v4 *)(dst + a3) = v3;
   }
   for (; i < n; i += 256) {
     const long long at = where(i);
-    *(int4 *)(dst + at) = *(const int4 *)(src + at);
+    *(v4 *)(dst + at) = *(const v4 *)(src + at);
   }
 }
 
@@ -351,11 +363,12 @@ __global__ void __launch_bounds__(256) assign_kernel(PagesArgs a, Space s) {
   copy_chunks(cache + to, cache + from, run * a.Hk, where);
 }
 
-// Pack: the pages, each slice blockIdx.y a layer's keys or values; the last slice: the tables renumbered
+// Pack: the pages, each slice blockIdx.y a layer's keys or values; TABLES: in front of them a slice that renumbers the tables
+template <bool TABLES>
 __global__ void __launch_bounds__(256) move_kernel(PagesArgs a, Space s) {
   const int used = s.flags[2];
   const bool fails = used > a.n_pages_out;
-  if ((int)blockIdx.y == 2 * a.layers) {
+  if (TABLES && blockIdx.y == 0) {
     if (blockIdx.x == 0 && threadIdx.x == 0) {
       if (a.free_out) *a.free_out = fails ? 0 : used;
       if (fails) atomicOr(a.err, kErrRoom);
@@ -371,9 +384,9 @@ __global__ void __launch_bounds__(256) move_kernel(PagesArgs a, Space s) {
   }
   if (fails) return;
   const long long size = page_size(a);
-  const int layer = blockIdx.y >> 1;
-  const char *in = (const char *)(blockIdx.y & 1 ? a.v_in : a.k_in) + (long long)layer * a.n_pages * size;
-  char *out = (char *)(blockIdx.y & 1 ? a.v_out : a.k_out) + (long long)layer * a.n_pages_out * size;
+  const int y = blockIdx.y - TABLES, layer = y >> 1;
+  const char *in = (const char *)(y & 1 ? a.v_in : a.k_in) + (long long)layer * a.n_pages * size;
+  char *out = (char *)(y & 1 ? a.v_out : a.k_out) + (long long)layer * a.n_pages_out * size;
   for (int i = blockIdx.x; i < used; i += gridDim.x)
     copy_chunks(out + i * size, in + s.list[i] * size, (int)(size / 16), [](int c) __attribute__((always_inline)) { return c * 16ll; });
 }
@@ -387,13 +400,13 @@ size_t pages_workspace_bytes(int M, int n_pages) {
 
 namespace {
 
-// The plan of a call: what every row needs, and the free (used) pages in order
+// The plan of a call: what every row needs, and the free (used) pages in order.  Whether one workgroup made it.
 template <bool GROW>
-void plan(const PagesArgs &a, const Space &s, hipStream_t st) {
+bool plan(const PagesArgs &a, const Space &s, hipStream_t st) {
   const long long n = (long long)a.M * a.n_blocks;
   if (a.n_pages <= kSmallPages && n <= kSmallEntries) {
     hipLaunchKernelGGL(small_kernel<GROW>, dim3(1), dim3(1024), 0, st, a, s);
-    return;
+    return true;
   }
   const int rc = GROW ? chunks(a.M, kRowChunk) : 0, pc = chunks(a.n_pages, kPageChunk);
   const long long clear = 4 + (GROW ? 3ll : 1ll) * a.n_pages;
@@ -402,6 +415,7 @@ void plan(const PagesArgs &a, const Space &s, hipStream_t st) {
   hipLaunchKernelGGL(count_kernel<GROW>, blocks(n), dim3(256), 0, st, a, s);
   hipLaunchKernelGGL(need_kernel<GROW>, dim3(rc + pc), dim3(256), 0, st, a, s, rc);
   hipLaunchKernelGGL(list_kernel<!GROW>, dim3(rc + pc), dim3(256), 0, st, a, s, rc, pc);
+  return false;
 }
 
 }  // namespace
@@ -415,9 +429,11 @@ hipError_t launch_advance(const PagesArgs &a, hipStream_t st) {
 
 hipError_t launch_pack(const PagesArgs &a, hipStream_t st) {
   const Space s = space(a.ws, a.M, a.n_pages);
-  plan<false>(a, s, st);
-  const int most = a.n_pages < a.n_pages_out ? a.n_pages : a.n_pages_out;
-  hipLaunchKernelGGL(move_kernel, dim3(most < 65536 ? most : 65536, 2 * a.layers + 1), dim3(256), 0, st, a, s);
+  const int most = a.n_pages < a.n_pages_out ? a.n_pages : a.n_pages_out, x = most < 65536 ? most : 65536;
+  if (plan<false>(a, s, st))
+    hipLaunchKernelGGL(move_kernel<false>, dim3(x, 2 * a.layers), dim3(256), 0, st, a, s);
+  else
+    hipLaunchKernelGGL(move_kernel<true>, dim3(x, 2 * a.layers + 1), dim3(256), 0, st, a, s);
   return hipGetLastError();
 }
 

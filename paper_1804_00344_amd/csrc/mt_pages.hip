@@ -196,11 +196,12 @@ __global__ void __launch_bounds__(256) list_kernel(PagesArgs a, Space s, int row
 
 // All of the above by one workgroup, the counts in LDS, for tables and pools of moderate size: 5 rows of a pool of 23
 // pages 15 -> 9 us with the copies, 768 rows of 3900 pages 38 -> 27.
-constexpr int kSmallPages = 8192, kSmallEntries = 1 << 15;
+constexpr int kSmallPages = 8192, kSmallRows = 2048, kSmallEntries = 1 << 15;
 
 template <bool GROW>
 __global__ void __launch_bounds__(1024) small_kernel(PagesArgs a, Space s) {
   __shared__ int refs[kSmallPages], growers[GROW ? kSmallPages : 1], last[GROW ? kSmallPages : 1];
+  __shared__ int src[kSmallRows], len[kSmallRows], add[GROW ? kSmallRows : 1], end[GROW ? kSmallRows : 1];  // of the rows; end: their last page
   __shared__ int sums[16], too_long;
   for (int p = threadIdx.x; p < a.n_pages; p += 1024) {
     refs[p] = 0;
@@ -209,23 +210,57 @@ __global__ void __launch_bounds__(1024) small_kernel(PagesArgs a, Space s) {
   if (threadIdx.x == 0) too_long = 0;
   __syncthreads();
   const int n = a.M * a.n_blocks, pmask = (1 << a.page_log2) - 1;
-  for (int e = threadIdx.x; e < n; e += 1024) {
-    const int m = e / a.n_blocks, j = e - m * a.n_blocks;
-    const Row r = row_of(a, m, j == 0);
-    int p = -1;
-    if (j < r.blocks) {
-      p = page_of(a, r, j, true);
-      if (GROW) {
-        atomicAdd(&refs[p], 1);
-        if (j == r.blocks - 1 && r.add > 0 && (r.len & pmask)) {
-          atomicAdd(&growers[p], 1);
-          atomicMax(&last[p], m + 1);
-        }
-      } else {
-        refs[p] = 1;
-      }
+  for (int m = threadIdx.x; m < a.M; m += 1024) {
+    const Row r = row_of(a, m, true);
+    src[m] = r.src;
+    len[m] = r.len;
+    if (GROW) add[m] = r.add;
+  }
+  __syncthreads();
+  auto row = [&](int m) {
+    Row r;
+    r.src = src[m];
+    r.len = len[m];
+    r.blocks = (r.len + pmask) >> a.page_log2;
+    r.add = GROW ? add[m] : 0;
+    return r;
+  };
+  constexpr int U = 4;  // entries of a thread on their way at a time
+  for (int e0 = threadIdx.x; e0 < n; e0 += U * 1024) {
+    int page[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int e = min(e0 + u * 1024, n - 1), m = e / a.n_blocks, j = e - m * a.n_blocks;
+      // an entry that is not the row's is not used: any entry's address will do
+      page[u] = a.table_in[(long long)max(src[m], 0) * a.n_blocks + j];
     }
-    if (GROW) a.table_out[e] = p;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int e = e0 + u * 1024, m = min(e, n - 1) / a.n_blocks, j = e - m * a.n_blocks;
+      if (e >= n) continue;
+      const Row r = row(m);
+      int p = -1;
+      if (j < r.blocks) {
+        p = page[u];
+        if ((unsigned)p >= (unsigned)a.n_pages) {
+          atomicOr(a.err, kErrPage);
+          p = p < 0 ? 0 : a.n_pages - 1;
+        }
+        if (GROW) {
+          atomicAdd(&refs[p], 1);
+          if (j == r.blocks - 1) {
+            end[m] = p;
+            if (r.add > 0 && (r.len & pmask)) {
+              atomicAdd(&growers[p], 1);
+              atomicMax(&last[p], m + 1);
+            }
+          }
+        } else {
+          refs[p] = 1;
+        }
+      }
+      if (GROW) a.table_out[e] = p;
+    }
   }
   __syncthreads();
   // sum over the workgroup, and of the threads before this one
@@ -249,14 +284,14 @@ __global__ void __launch_bounds__(1024) small_kernel(PagesArgs a, Space s) {
       const int m = m0 + threadIdx.x;
       int need = 0;
       if (m < a.M) {
-        const Row r = row_of(a, m, false);
+        const Row r = row(m);
         const int after = blocks_after(a, r);
         if (after > a.n_blocks) {
           too_long = 1;
         } else {
           need = after - r.blocks;
           if (r.add > 0 && (r.len & pmask)) {
-            const int p = page_of(a, r, r.blocks - 1, false);
+            const int p = end[m];
             need += refs[p] > 1 && !(last[p] == m + 1 && growers[p] == refs[p]);
           }
         }
@@ -285,7 +320,7 @@ __global__ void __launch_bounds__(1024) small_kernel(PagesArgs a, Space s) {
     const bool fails = total > a.n_pages_out;
     for (int e = threadIdx.x; e < n; e += 1024) {
       const int m = e / a.n_blocks, j = e - m * a.n_blocks;
-      const Row r = row_of(a, m, false);
+      const Row r = row(m);
       a.table_out[e] = !fails && j < r.blocks ? refs[page_of(a, r, j, false)] : -1;
       if (j == 0) a.len_out[m] = fails ? 0 : r.len;
     }
@@ -404,7 +439,7 @@ namespace {
 template <bool GROW>
 bool plan(const PagesArgs &a, const Space &s, hipStream_t st) {
   const long long n = (long long)a.M * a.n_blocks;
-  if (a.n_pages <= kSmallPages && n <= kSmallEntries) {
+  if (a.n_pages <= kSmallPages && a.M <= kSmallRows && n <= kSmallEntries) {
     hipLaunchKernelGGL(small_kernel<GROW>, dim3(1), dim3(1024), 0, st, a, s);
     return true;
   }

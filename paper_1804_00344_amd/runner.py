@@ -419,3 +419,146 @@ class SsmLayer:
             mt.mt_i8_product(self.wout, f["y"], f["out"], f["ws"], stream=stream)
         self.cur = nxt
         return f["out"]
+
+
+class PagedCache:
+    """The keys and values of a program's attention layers in pages, k, v [layers, n_pages, Hk, page, Dh], and the table and
+    lengths of its current rows: prompts first, then hypotheses that continue one another's.  Making one, and the first
+    advance to a number of rows, wait for the device (unless captured into a graph): any stream may follow."""
+
+    def __init__(self, attn: mt.Attn, layers: int, n_pages: int, n_blocks: int):
+        self.attn, self.n_blocks = attn, n_blocks
+        shape = (layers, n_pages) + tuple(attn.page_shape)
+        self.k, self.v = (torch.zeros(shape, dtype=attn.dtype, device=attn.device) for _ in range(2))
+        self.free = torch.full((1,), n_pages, dtype=torch.int32, device=attn.device)
+        self._spare = {}
+        self.table, self.lens = self._rows(1)  # one empty row, for new ones to begin with
+        self.lens.zero_()
+        self._wait()
+
+    def _wait(self):
+        with torch.cuda.device(self.attn.device):
+            if not torch.cuda.is_current_stream_capturing():
+                torch.cuda.synchronize(self.attn.device)
+
+    def _rows(self, n):
+        """A table and lengths of n rows that are not the current ones."""
+        i32 = dict(dtype=torch.int32, device=self.attn.device)
+        if n not in self._spare:
+            pair = [(torch.empty(n, self.n_blocks, **i32), torch.empty(n, **i32)) for _ in range(2)]
+            self._spare[n] = pair, torch.empty(mt.mt_pages_workspace_bytes(self.attn, n, self.k.shape[1]), dtype=torch.uint8,
+                                               device=self.attn.device)
+            self._wait()
+        pair = self._spare[n][0]
+        return pair[1] if getattr(self, "table", None) is pair[0][0] else pair[0]
+
+    def advance(self, src_row, add=None, stream=None):
+        """Rows that continue src_row [M] int32 (below 0: new ones) of the current ones, with room for add [M] (None: 1 each)
+        more positions."""
+        n = src_row.numel()
+        table, lens = self._rows(n)
+        with torch.cuda.device(self.attn.device):
+            mt.mt_pages_advance(self.attn, src_row, add, self.table, self.lens, table, lens, self.k, self.v, free_out=self.free,
+                                ws=self._spare[n][1], stream=stream)
+        self.table, self.lens = table, lens
+
+    def pack(self, n_pages: int, stream=None) -> "PagedCache":
+        """A cache of n_pages that holds the current rows, their pages at its front."""
+        out = PagedCache(self.attn, self.k.shape[0], n_pages, self.n_blocks)
+        n = self.lens.numel()
+        table, lens = out._rows(n)
+        ws = torch.empty(mt.mt_pages_workspace_bytes(self.attn, n, self.k.shape[1]), dtype=torch.uint8, device=self.attn.device)
+        self._wait()
+        with torch.cuda.device(self.attn.device):
+            mt.mt_pages_pack(self.attn, self.table, self.lens, self.k, self.v, table, lens, out.k, out.v, out.free, ws=ws,
+                             stream=stream)
+        self._wait()  # the workspace is given back
+        out.free = n_pages - out.free
+        out.table, out.lens = table, lens
+        return out
+
+
+class AttnLayer:
+    """The attention of a decoder's layer for serving: over the positions before (a PagedCache that layers share), for pieces
+    of prompts and for single tokens of hypotheses, and over an encoder's states (mt_encode's context).  Its calls run on
+    its own device, whichever is current.
+
+        [q | k | v] = u Wqkv,  out = attention(q, cache) Wo;   q' = u Wcq,  [k' | v'] = ctx Wckv,  out' = attention(q', k', v') Wco
+
+    weights: Wqkv [E, (Hq + 2Hk) Dh], Wo [Hq Dh, E], optional biases bqkv, bo; with cross attention Wcq [E, Hq Dh],
+    Wckv [C, 2 Hk Dh], Wco [Hq Dh, E], biases bcq, bckv, bco (products in 8 bits); gq, gk, freq (see mt_attn_weights)."""
+
+    def __init__(self, weights, Hq: int, Hk: int, *, page: int = 16, dtype: str = "bf16", device: str = "cuda:0", **heads):
+        w = weights
+        self.E = w["Wqkv"].shape[0]
+        self.Dh = w["Wqkv"].shape[1] // (Hq + 2 * Hk)
+        self.QD, self.KD = Hq * self.Dh, Hk * self.Dh
+        self.device = torch.device(device)
+        if self.device.index is None:  # the device that is current now, for good
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        cfg = mt.make_attn_config(Hq, Hk, self.Dh, page=page, dtype=dtype, **heads)
+        with torch.cuda.device(self.device):
+            self.attn = mt.mt_attn_load(cfg, {k: w.get(k) for k in mt.ATTN_WEIGHT_FIELDS})
+            self.wqkv, self.wo = mt.mt_i8_load(w["Wqkv"], w.get("bqkv")), mt.mt_i8_load(w["Wo"], w.get("bo"))
+            self.cross_w = [mt.mt_i8_load(w["W" + n], w.get("b" + n)) for n in ("cq", "ckv", "co")] if "Wcq" in w else None
+        self.io_dtype = self.attn.dtype
+
+    def _buffers(self, B, S, n_keys, S_src):
+        io = dict(dtype=self.io_dtype, device=self.device)
+        mats = [self.wqkv, self.wo] + (self.cross_w[::2] if S_src else [])
+        n = [mt.mt_i8_workspace_bytes(m, B * S) for m in mats] + [mt.mt_attn_workspace_bytes(self.attn, B, S, n_keys)]
+        return dict(qkv=torch.zeros(B, S, self.QD + 2 * self.KD, **io), y=torch.zeros(B, S, self.QD, **io),
+                    out=torch.zeros(B, S, self.E, **io), ws=torch.empty(max(n), dtype=torch.uint8, device=self.device))
+
+    def set_batch(self, B: int, S: int, K: int, n_keys: int, S_src: int = 0):
+        """Buffers for pieces of S positions of B prompts, single tokens of K hypotheses of each, over n_keys positions (the
+        cache's n_blocks * page), and S_src encoder states a sentence.  Waits for the device (unless captured)."""
+        with torch.cuda.device(self.device):
+            pb, sb = self._buffers(B, S, n_keys, 0), self._buffers(B * K, 1, n_keys, 0)
+            xb = kv = None
+            if S_src:
+                io = dict(dtype=self.io_dtype, device=self.device)
+                xb, kv = self._buffers(B, K, S_src, S_src), torch.zeros(B, S_src, 2 * self.KD, **io)
+                kws = torch.empty(mt.mt_i8_workspace_bytes(self.cross_w[1], B * S_src), dtype=torch.uint8, device=self.device)
+            if not torch.cuda.is_current_stream_capturing():
+                torch.cuda.synchronize(self.device)
+        self.B, self.S, self.K, self.M = B, S, K, B * K
+        self.pb, self.sb, self.xb, self.src_kv, self.src_ws = pb, sb, xb, kv, kws if S_src else None
+
+    def _self(self, f, u, cache, layer, n_new, stream):
+        B, S = u.shape[:2]
+        q, k, v = (f["qkv"][..., a:b] for a, b in ((0, self.QD), (self.QD, self.QD + self.KD), (self.QD + self.KD, None)))
+        with torch.cuda.device(self.device):
+            mt.mt_i8_product(self.wqkv, u, f["qkv"], f["ws"], stream=stream)
+            mt.mt_attn_append(self.attn, q, k, v, q, cache.lens, cache.table, cache.k[layer], cache.v[layer], n_new=n_new,
+                              stream=stream)
+            mt.mt_attn_paged(self.attn, q, cache.lens, cache.table, cache.k[layer], cache.v[layer], f["y"], n_new=n_new,
+                             ws=f["ws"], stream=stream)
+            mt.mt_i8_product(self.wo, f["y"], f["out"], f["ws"], stream=stream)
+        return f["out"]
+
+    def prompt(self, u, cache: PagedCache, layer: int = 0, n_new=None, stream=None):
+        """u [B, S, E]: the new positions of the cache's rows (its advance has made room), n_new [B] int32 of them: out
+        [B, S, E]."""
+        return self._self(self.pb, u, cache, layer, n_new, stream)
+
+    def step(self, u, cache: PagedCache, layer: int = 0, stream=None):
+        """u [M, E], a token of each row: out [M, E]."""
+        return self._self(self.sb, u[:, None], cache, layer, None, stream)[:, 0]
+
+    def set_source(self, ctx, mask, stream=None):
+        """ctx [B, S_src, C] in the io type, mask [B, S_src] fp32: the keys and values of the cross attention."""
+        self.mask = mask
+        with torch.cuda.device(self.device):
+            mt.mt_i8_product(self.cross_w[1], ctx, self.src_kv, self.src_ws, stream=stream)
+
+    def cross(self, u, stream=None):
+        """u [M, E], hypotheses m of sentence m // K: out [M, E]."""
+        f = self.xb
+        q = f["qkv"].view(-1)[:self.M * self.QD].view(self.B, self.K, self.QD)
+        with torch.cuda.device(self.device):
+            mt.mt_i8_product(self.cross_w[0], u.view(self.B, self.K, self.E), q, f["ws"], stream=stream)
+            mt.mt_attn_cross(self.attn, q, self.src_kv[..., :self.KD], self.src_kv[..., self.KD:], f["y"], mask=self.mask,
+                             ws=f["ws"], stream=stream)
+            mt.mt_i8_product(self.cross_w[2], f["y"], f["out"], f["ws"], stream=stream)
+        return f["out"].view(self.M, self.E)

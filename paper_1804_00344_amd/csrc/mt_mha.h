@@ -28,7 +28,7 @@ struct MhaArgs {
   int32_t *err;
   int num_cu;
 };
-size_t mha_workspace_bytes(int Hq, int Hk, int Dh, bool f32, int B, int S, long long n_keys, int num_cu);
+size_t mha_workspace_bytes(int Hq, int Hk, int Dh, bool f32, int B, int S, long long n_keys, int window, int num_cu);
 hipError_t launch_mha(const MhaArgs &a, hipStream_t st);
 
 // ---- norms, rotation and store (mt_mha_append.hip) ----

@@ -12,17 +12,22 @@ struct Plan {
   int tiles, parts;
 };
 
-Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, bool f32, int num_cu) {
+Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window, bool f32, int num_cu) {
   Plan p;
   const long long rows = (long long)S * (Hq / Hk), heads = (long long)B * Hk;
+  if (window && n_keys > (long long)window + S) n_keys = (long long)window + S;  // keys that a row's queries see
+  // the key axis is cut until there are two workgroups a unit; a part has 256 keys at least
+  const long long most = n_keys / 256 < 1 ? 1 : n_keys / 256;
+  auto parts = [&](long long wgs) {
+    const long long want = 2 * num_cu / wgs;
+    return (int)(want < 1 ? 1 : want < most ? want : most);
+  };
   const long long big = heads * ((rows + kTileRows - 1) / kTileRows);
-  p.step = (!f32 || Dh <= 128) && (rows <= kStepRows || big < num_cu);
+  p.step = Dh <= 128 && (rows <= kStepRows || big * parts(big) < num_cu);
   const int per = p.step ? kStepRows : kTileRows;
   p.tiles = (int)((rows + per - 1) / per);
-  // two workgroups a unit; a part of 256 keys at least
-  const long long wgs = heads * p.tiles, want = 2 * num_cu / wgs, most = n_keys / 256;
-  p.parts = (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
-  p.share = wgs < 8 * num_cu;
+  p.parts = parts(heads * p.tiles);
+  p.share = heads * p.tiles < 8 * num_cu;
   return p;
 }
 
@@ -60,13 +65,19 @@ __global__ void __launch_bounds__(256) join_kernel(MhaArgs a, int n_parts) {
 
 }  // namespace
 
-size_t mha_workspace_bytes(int Hq, int Hk, int Dh, bool f32, int B, int S, long long n_keys, int num_cu) {
-  const Plan p = plan_of(Hq, Hk, Dh, B, S, n_keys, f32, num_cu);
-  return p.parts > 1 ? (parts_bytes((long long)B * Hq * S, p.parts, Dh) + 255) / 256 * 256 : 256;
+size_t mha_workspace_bytes(int Hq, int Hk, int Dh, bool f32, int B, int S, long long n_keys, int window, int num_cu) {
+  size_t most = 256;  // of both attentions: only that over pages has the window
+  for (int w : {window, 0}) {
+    const Plan p = plan_of(Hq, Hk, Dh, B, S, n_keys, w, f32, num_cu);
+    const size_t n = p.parts > 1 ? (parts_bytes((long long)B * Hq * S, p.parts, Dh) + 255) / 256 * 256 : 256;
+    if (n > most) most = n;
+  }
+  return most;
 }
 
 hipError_t launch_mha(const MhaArgs &a, hipStream_t st) {
-  const Plan p = plan_of(a.Hq, a.Hk, a.Dh, a.B, a.S, a.table ? (long long)a.n_blocks << a.page_log2 : a.Sk, !a.bf16_io, a.num_cu);
+  const Plan p = plan_of(a.Hq, a.Hk, a.Dh, a.B, a.S, a.table ? (long long)a.n_blocks << a.page_log2 : a.Sk, a.window,
+                        !a.bf16_io, a.num_cu);
   hipError_t e;
   if (p.step) {
     const StepPlan s{p.tiles, p.parts, 0, 0};

@@ -193,7 +193,8 @@ mt_status mt_attn_append(mt_attn *a, int B, int S, const int32_t *n_new, const i
 size_t mt_attn_workspace_bytes(const mt_attn *a, int B, int S, int64_t n_keys) {
   if (!valid(a) || B < 1 || S < 1 || (long long)B * S > kMaxRows || (long long)B * S * a->cfg.Hq > kMaxSteps) return 0;
   if (n_keys < 1 || n_keys > kMaxSteps) return 0;
-  return mha_workspace_bytes(a->cfg.Hq, a->cfg.Hk, a->cfg.Dh, a->cfg.dtype == MT_F32, B, S, n_keys, a->num_cu);
+  return mha_workspace_bytes(a->cfg.Hq, a->cfg.Hk, a->cfg.Dh, a->cfg.dtype == MT_F32, B, S, n_keys, a->cfg.window,
+                             a->num_cu);
 }
 
 // what both attentions check and pass on

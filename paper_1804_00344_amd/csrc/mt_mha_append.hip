@@ -227,13 +227,18 @@ __global__ void __launch_bounds__(256) append_kernel(AppendArgs a, int per_row, 
 
 template <typename T, int LP>
 hipError_t by_rows(const AppendArgs &a, hipStream_t st) {
-  // several positions of a workgroup share its start and keep loads on their way: only where there are enough of them
-  const bool many = (long long)a.B * a.S >= 16ll * a.num_cu && a.S >= 4;
-  const int per_row = many ? (a.S + 3) / 4 : a.S;
+  // several positions of a workgroup share its start and keep loads on their way: only where there are enough of them,
+  // and as many as fill its lanes
+  const long long rows = (long long)a.B * a.S;
+  int tok = rows >= 16ll * a.num_cu && a.S >= 4 ? 4 : 1;
+  if (tok == 4 && (a.Hq + a.Hk) * LP <= 128 && rows >= 64ll * a.num_cu && a.S >= 16) tok = 16;
+  const int per_row = (a.S + tok - 1) / tok;
   const int all = a.B * per_row, most = 1 << 22;  // workgroups of a launch
   for (int base = 0; base < all; base += most) {
     const dim3 grid((unsigned)(all - base < most ? all - base : most));
-    if (many)
+    if (tok == 16)
+      hipLaunchKernelGGL((append_kernel<T, LP, 16>), grid, dim3(256), 0, st, a, per_row, base);
+    else if (tok == 4)
       hipLaunchKernelGGL((append_kernel<T, LP, 4>), grid, dim3(256), 0, st, a, per_row, base);
     else
       hipLaunchKernelGGL((append_kernel<T, LP, 1>), grid, dim3(256), 0, st, a, per_row, base);

@@ -23,7 +23,7 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T
   constexpr int KT = 32, TB = KT * DP * (int)sizeof(T), DB = DP / 32;
   __shared__ __attribute__((aligned(1024))) char lds[4 * 2 * TB];
   __shared__ float2 ends[4][32];
-  __shared__ int dirty;
+  __shared__ int odds[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31;
   const unsigned w = plan.first + xcd_remap(blockIdx.x, gridDim.x), job = SHARE ? w : w * 4 + wave;
   if (job >= plan.jobs) return;
@@ -36,6 +36,14 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T
   int lo, hi, lo2, hi2;  // keys that some row sees: [lo, hi2); that all see: [lo2, hi)
   seen_keys<PAGED>(a, span, i_first, lo, hi);
   seen_keys<PAGED>(a, span, i_last, lo2, hi2);
+  // ---- this lane's query
+  const int r = r0 + col;
+  const bool live = r < R;
+  const int qi = (live ? r : R - 1) / a.G, hq = h * a.G + (live ? r : R - 1) - qi * a.G;
+  int qlo, qhi;
+  seen_keys<PAGED>(a, span, qi, qlo, qhi);
+  Rows<T, DP> me;
+  me.start((const T *)a.q + ((long long)b * a.S + qi) * a.ldq + (long long)hq * a.Dh, live, a.Dh);
   const float *mask = !PAGED && a.mask ? a.mask + (long long)b * a.Sk : nullptr;
   if (!PAGED && mask) {  // the first and the last valid position
     int first = a.Sk, last = 0;
@@ -43,10 +51,6 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T
       if (mask[j] != 0.f) first = min(first, j), last = j + 1;
     lo = wave_ext<int, false>(first);
     hi2 = wave_ext<int, true>(last);
-  }
-  if (SHARE) {
-    if (threadIdx.x == 0) dirty = 0;
-    __syncthreads();  // dirty is set from here on
   }
   lo &= ~(KT - 1);
   int nt = hi2 > lo ? (hi2 - lo + KT - 1) / KT : 0;  // tiles of keys, this part's of them
@@ -56,14 +60,6 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T
     nt = min(nt, t0 + per) - t0;
     lo += t0 * KT;
   }
-  // ---- this lane's query
-  const int r = r0 + col;
-  const bool live = r < R;
-  const int qi = (live ? r : R - 1) / a.G, hq = h * a.G + (live ? r : R - 1) - qi * a.G;
-  int qlo, qhi;
-  seen_keys<PAGED>(a, span, qi, qlo, qhi);
-  Rows<T, DP> me;
-  me.start((const T *)a.q + ((long long)b * a.S + qi) * a.ldq + (long long)hq * a.Dh, live, a.Dh);
   // ---- tiles of keys
   char *const buf = lds + wave * 2 * TB;
   Mover<T, DP, PAGED, KT, 64> mv;
@@ -109,7 +105,8 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T
     }
     odd = __any(odd);
   } else {
-    if (odd) dirty = 1;
+    const int any_odd = __any(odd);
+    if (lane == 0) odds[wave] = any_odd;
     if (lane < 32) ends[wave][lane] = make_float2(me.m, me.l);
     __syncthreads();
     float m = kNegInf, l = 0.f;
@@ -149,7 +146,7 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T
       }
     }
     if (cut && live && wave == 0 && lane < 32) parts.ml[prow + r] = make_float2(m, l);
-    odd = dirty;
+    odd = odds[0] | odds[1] | odds[2] | odds[3];
   }
   if (!PAGED || !odd) return;
   // values that are no numbers where some rows see them and others not: row by row instead

@@ -418,6 +418,13 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a,
   seen_keys<PAGED>(a, span, qi, qlo, qhi);
   Rows<T, DP> me;
   me.start((const T *)a.q + ((long long)b * a.S + qi) * a.ldq + (long long)hq * a.Dh, live, a.Dh);
+  // keys that some row of this wave sees
+  int wlo = 0, whi = 0;
+  {
+    const int first = r0 + wave * 32, last = min(first + 31, R - 1);
+    int x;
+    if (first < R) seen_keys<PAGED>(a, span, first / a.G, wlo, x), seen_keys<PAGED>(a, span, last / a.G, x, whi);
+  }
   // ---- tiles of keys
   Mover<T, DP, PAGED, KT, 256> mv;
   auto mixed = [&](int k0) { return k0 + KT > hi || k0 < lo2; };
@@ -433,6 +440,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a,
     const unsigned long long seen = mv.seen;
     __syncthreads();
     if (t + 1 < nt) mv.fetch(k0 + KT, KT);
+    if (k0 < whi && k0 + KT > wlo) {
     f32x16 s[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) s[kb] = me.scores(buf, kb * 32);
@@ -443,6 +451,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a,
     me.weights(s, a.scale);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) me.values(buf + TB, kb * 32, s[kb]);
+    }
     if (t + 1 < nt && mv.put(k0 + KT, lds + ((t + 1) & 1) * 2 * TB, mixed(k0 + KT))) dirty = 1;
   }
   if (PAGED && nt > 0 && mv.bad) atomicOr(a.err, kErrPage);

@@ -362,7 +362,8 @@ struct TilePlan {
 template <typename T, int DP, bool PAGED>
 __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a, TilePlan plan) {
   typedef Tile<T> M;
-  constexpr int KT = M::KT, TB = KT * DP * (int)sizeof(T), KB = KT / 32;
+  // heads of more than 128 features leave no registers for more keys at a time
+  constexpr int KT = DP > 128 ? 32 : M::KT, TB = KT * DP * (int)sizeof(T), KB = KT / 32;
   __shared__ __attribute__((aligned(1024))) char lds[4 * TB];
   __shared__ int dirty, edge[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31;

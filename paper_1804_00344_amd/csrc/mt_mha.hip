@@ -16,23 +16,26 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
   Plan p;
   const long long rows = (long long)S * (Hq / Hk), heads = (long long)B * Hk;
   if (window && n_keys > (long long)window + S) n_keys = (long long)window + S;  // keys that a row's queries see
-  // the key axis is cut until there are two workgroups a unit; a part has 256 keys at least
+  // The key axis is cut until there are enough workgroups; a part has 256 keys at least.  Tiles of 128 rows want two a unit,
+  // one computing scores while the other takes exponentials (300 positions over 9000, 32 heads of 128: 84 us, one 132);
+  // few rows want one, as the parts have to be joined (a token over 20000, 32 heads of 128: 27 us, two 36).
   const long long most = n_keys / 256 < 1 ? 1 : n_keys / 256;
-  auto parts = [&](long long wgs) {
-    const long long want = 2 * num_cu / wgs;
+  auto parts = [&](long long wgs, int a_unit) {
+    const long long want = a_unit * num_cu / wgs;
     return (int)(want < 1 ? 1 : want < most ? want : most);
   };
+  const int tile_unit = Dh <= 128 ? 2 : 1;  // what its registers leave room for
   const long long big = heads * ((rows + kTileRows - 1) / kTileRows);
-  p.step = Dh <= 128 && (rows <= kStepRows || big * parts(big) < num_cu);
+  p.step = Dh <= 128 && (rows <= kStepRows || big * parts(big, tile_unit) < num_cu);
   const int per = p.step ? kStepRows : kTileRows;
   p.tiles = (int)((rows + per - 1) / per);
-  p.parts = parts(heads * p.tiles);
+  p.parts = parts(heads * p.tiles, p.step ? 1 : tile_unit);
   p.share = heads * p.tiles < 8 * num_cu;
   return p;
 }
 
-// The parts of a row together: sums relative to the largest of the parts' maxima.  A wave per row.
-template <typename T>
+// The parts of a row together: sums relative to the largest of the parts' maxima.  A wave per row, NF features a lane.
+template <typename T, int NF>
 __global__ void __launch_bounds__(256) join_kernel(MhaArgs a, int n_parts) {
   const long long rows = (long long)a.B * a.Hq * a.S;
   const long long row = blockIdx.x * 4ll + (threadIdx.x >> 6);
@@ -44,23 +47,55 @@ __global__ void __launch_bounds__(256) join_kernel(MhaArgs a, int n_parts) {
   // the parts hold a sequence's rows one after the other: those of its n queries
   if (i >= min(max(n0, 0), a.S)) return;
   const Parts p = parts_of(a.ws, rows, n_parts);
+  // a part per lane for the maxima and factors, a feature per lane for the sums, whose loads do not wait for each other
   float m = kNegInf;
-  for (int s = 0; s < n_parts; ++s) m = fmaxf(m, p.ml[s * rows + row].x);
+  for (int s0 = 0; s0 < n_parts; s0 += 64) m = fmaxf(m, s0 + lane < n_parts ? p.ml[(s0 + lane) * rows + row].x : kNegInf);
+  m = wave_max(m);
   const float use = m == kNegInf ? 0.f : m;
-  float l = 0.f, acc[4] = {};
-  for (int s = 0; s < n_parts; ++s) {
-    const float2 ml = p.ml[s * rows + row];
-    if (ml.y == 0.f) continue;  // nothing seen
-    const float c = ml.x == kNegInf ? 1.f : __builtin_amdgcn_exp2f(ml.x - use);
-    l = fmaf(ml.y, c, l);
+  float l = 0.f, acc[NF] = {};
+  int d[NF];
 #pragma unroll
-    for (int f = 0; f < 4; ++f)
-      if (lane + 64 * f < a.Dh) acc[f] = fmaf(p.o[(s * rows + row) * a.Dh + lane + 64 * f], c, acc[f]);
+  for (int f = 0; f < NF; ++f) d[f] = min(lane + 64 * f, a.Dh - 1);
+  for (int s0 = 0; s0 < n_parts; s0 += 64) {
+    float2 ml = make_float2(kNegInf, 0.f);
+    if (s0 + lane < n_parts) ml = p.ml[(s0 + lane) * rows + row];
+    // sums without a maximum are zeros or no numbers; a part that has seen nothing has not written its sums
+    const float c = ml.x == kNegInf ? 1.f : __builtin_amdgcn_exp2f(ml.x - use);
+    l += wave_sum(ml.y * c);
+    const unsigned long long there = __ballot(ml.y != 0.f);
+    constexpr int U = 8;
+    for (int s1 = 0; s1 < min(64, n_parts - s0); s1 += U) {
+      float v[U][NF];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float *o = p.o + (min(s0 + s1 + u, n_parts - 1) * rows + row) * a.Dh;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) v[u][f] = o[d[f]];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float w = lane_f(c, s1 + u);
+        const bool ok = (there >> (s1 + u)) & 1;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) acc[f] = ok ? fmaf(v[u][f], w, acc[f]) : acc[f];
+      }
+    }
   }
   T *y = (T *)a.y + ((long long)b * a.S + i) * a.ldy + (long long)hq * a.Dh;
 #pragma unroll
-  for (int f = 0; f < 4; ++f)
+  for (int f = 0; f < NF; ++f)
     if (lane + 64 * f < a.Dh) Store<T>::put(y + lane + 64 * f, l == 0.f ? 0.f : acc[f] / l);
+}
+
+template <typename T>
+void launch_join(const MhaArgs &a, int n_parts, hipStream_t st) {
+  const dim3 grid((unsigned)(((long long)a.B * a.Hq * a.S + 3) / 4)), block(256);
+  if (a.Dh <= 64)
+    hipLaunchKernelGGL((join_kernel<T, 1>), grid, block, 0, st, a, n_parts);
+  else if (a.Dh <= 128)
+    hipLaunchKernelGGL((join_kernel<T, 2>), grid, block, 0, st, a, n_parts);
+  else
+    hipLaunchKernelGGL((join_kernel<T, 4>), grid, block, 0, st, a, n_parts);
 }
 
 }  // namespace
@@ -87,12 +122,7 @@ hipError_t launch_mha(const MhaArgs &a, hipStream_t st) {
     e = a.bf16_io ? launch_tiles_bf16(a, t, st) : launch_tiles_f32(a, t, st);
   }
   if (e != hipSuccess || p.parts == 1) return e;
-  const long long rows = (long long)a.B * a.Hq * a.S;
-  const dim3 grid((unsigned)((rows + 3) / 4));
-  if (a.bf16_io)
-    hipLaunchKernelGGL(join_kernel<bf16>, grid, dim3(256), 0, st, a, p.parts);
-  else
-    hipLaunchKernelGGL(join_kernel<float>, grid, dim3(256), 0, st, a, p.parts);
+  a.bf16_io ? launch_join<bf16>(a, p.parts, st) : launch_join<float>(a, p.parts, st);
   return hipGetLastError();
 }
 

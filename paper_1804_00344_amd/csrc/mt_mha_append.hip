@@ -34,13 +34,22 @@ __device__ __forceinline__ void head_sums(float (&v)[U]) {
   }
 }
 
+template <typename T, bool STREAM, int VEC>
+__device__ __forceinline__ void put_rows(T *p, const float (&x)[VEC]) {
+  if constexpr (STREAM)
+    Vec<T, VEC>::template put<true>(p, x);
+  else
+    Vec<T, VEC>::put_any(p, x);
+}
+
 // A head takes LP lanes (a power of two) of VEC features each, one 16-byte access per lane, and a lane U heads at a
-// time, step by step together.  A workgroup takes TOK positions of a row, whose angles its threads form first (in 64
+// time, step by step together: one, as more waves bring more loads on their way than more heads of a lane do (8 x 4096 x
+// 48 heads of 128 in bf16: one 157 us, 5.1 TB/s, two 166, four 210).  A workgroup takes TOK positions of a row, whose angles its threads form first (in 64
 // bits, as turns: the product keeps 2^-22 of a turn at position 2^30) and all heads share.  Partners of a rotation come
 // from the lane half a head away where the lanes are a whole head, else through LDS.
-template <typename T, int LP, int TOK>
+template <typename T, int LP, int TOK, bool STREAM>
 __global__ void __launch_bounds__(256) append_kernel(AppendArgs a, int per_row, int base) {
-  constexpr int VEC = 16 / sizeof(T), U = 4, HEADS = 256 / LP;
+  constexpr int VEC = 16 / sizeof(T), U = 1, HEADS = 256 / LP;
   typedef Vec<T, VEC> V;
   __shared__ __attribute__((aligned(16))) float cs[TOK][2][128];
   __shared__ __attribute__((aligned(16))) float part[256 * VEC];
@@ -94,7 +103,7 @@ __global__ void __launch_bounds__(256) append_kernel(AppendArgs a, int per_row, 
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (to[u] >= 0) *(typename V::Raw *)((T *)a.vp + to[u]) = in[u];
+        if (to[u] >= 0) V::template store<STREAM>((T *)a.vp + to[u], in[u]);
     }
   }
   for (int e = threadIdx.x; e < toks * half; e += 256) {
@@ -217,32 +226,38 @@ __global__ void __launch_bounds__(256) append_kernel(AppendArgs a, int per_row, 
         for (int e = 0; e < VEC; ++e) x[u][e] = 0.f;
       }
       if (task[u].h < a.Hq)
-        V::put_any((T *)a.qo + (row0 + task[u].t) * a.ldqo + task[u].h * a.Dh + d0, x[u]);
+        put_rows<T, STREAM>((T *)a.qo + (row0 + task[u].t) * a.ldqo + task[u].h * a.Dh + d0, x[u]);
       else if (pos >= 0)
-        V::put((T *)a.kp + place(pos) + (task[u].h - a.Hq) * head_step + d0, x[u]);
+        V::template put<STREAM>((T *)a.kp + place(pos) + (task[u].h - a.Hq) * head_step + d0, x[u]);
     }
   }
   if (bad) atomicOr(a.err, kErrPage);
 }
 
+template <typename T, int LP, int TOK, bool STREAM>
+void launch_as(const AppendArgs &a, hipStream_t st) {
+  const int per_row = (a.S + TOK - 1) / TOK, all = a.B * per_row, most = 1 << 22;  // workgroups of a launch
+  for (int base = 0; base < all; base += most)
+    hipLaunchKernelGGL((append_kernel<T, LP, TOK, STREAM>), dim3((unsigned)(all - base < most ? all - base : most)), dim3(256), 0, st,
+                       a, per_row, base);
+}
+
+// Several positions of a workgroup share its start and keep loads on their way: only where there are enough of them, and
+// as many as fill its lanes (87 x 1507 of 2 heads of 64: 4 positions 152 us, 16 97).  Aligned results larger than the
+// L2s together are stored past them (8 x 4096 x 48 heads of 128, two heads a lane: 192 -> 166 us).
 template <typename T, int LP>
 hipError_t by_rows(const AppendArgs &a, hipStream_t st) {
-  // several positions of a workgroup share its start and keep loads on their way: only where there are enough of them,
-  // and as many as fill its lanes
   const long long rows = (long long)a.B * a.S;
-  int tok = rows >= 16ll * a.num_cu && a.S >= 4 ? 4 : 1;
-  if (tok == 4 && (a.Hq + a.Hk) * LP <= 128 && rows >= 64ll * a.num_cu && a.S >= 16) tok = 16;
-  const int per_row = (a.S + tok - 1) / tok;
-  const int all = a.B * per_row, most = 1 << 22;  // workgroups of a launch
-  for (int base = 0; base < all; base += most) {
-    const dim3 grid((unsigned)(all - base < most ? all - base : most));
-    if (tok == 16)
-      hipLaunchKernelGGL((append_kernel<T, LP, 16>), grid, dim3(256), 0, st, a, per_row, base);
-    else if (tok == 4)
-      hipLaunchKernelGGL((append_kernel<T, LP, 4>), grid, dim3(256), 0, st, a, per_row, base);
-    else
-      hipLaunchKernelGGL((append_kernel<T, LP, 1>), grid, dim3(256), 0, st, a, per_row, base);
-  }
+  const bool many = rows >= 16ll * a.num_cu && a.S >= 4;
+  const bool aligned = (uintptr_t)a.qo % 16 == 0 && a.ldqo % (16 / (int)sizeof(T)) == 0;
+  if (many && aligned && (double)rows * (a.Hq + 2 * a.Hk) * a.Dh * sizeof(T) > 32e6 && (a.Hq + a.Hk) * LP > 128)
+    launch_as<T, LP, 4, true>(a, st);
+  else if (many && (a.Hq + a.Hk) * LP <= 128 && rows >= 64ll * a.num_cu && a.S >= 16)
+    launch_as<T, LP, 16, false>(a, st);
+  else if (many)
+    launch_as<T, LP, 4, false>(a, st);
+  else
+    launch_as<T, LP, 1, false>(a, st);
   return hipGetLastError();
 }
 

@@ -353,6 +353,8 @@ struct TilePlan {
   int tiles;  // of kTileRows rows of a sequence's key head
   int parts;  // the key axis is cut into
   int first;  // workgroup of this launch
+  const int *order;   // masked sentences, those with the most work first, or NULL: as they come
+  const int2 *edges;  // of each one's mask: its first valid position, one past its last
 };
 
 // A workgroup of four waves takes 128 rows of one key head of one sequence: row r is query r / G, head r % G of those
@@ -373,7 +375,8 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a,
   int bh, u;
   if (w < even * per) {
     const int v = w / kXcds;
-    bh = v / per * kXcds + w % kXcds;
+    const int round = v / per, x = w % kXcds;
+    bh = round * kXcds + (plan.order && round % 2 ? kXcds - 1 - x : x);  // sorted by work: there and back
     u = v % per;
   } else {
     const int v = w - even * per;
@@ -381,7 +384,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a,
     u = v % per;
   }
   const int part = u % plan.parts, tile = plan.tiles - 1 - u / plan.parts;
-  const int b = bh / a.Hk, h = bh - b * a.Hk;
+  const int place = bh / a.Hk, h = bh - place * a.Hk, b = plan.order ? plan.order[place] : place;
   const RowSpan span = row_span<PAGED>(a, b, h == 0 && tile == 0 && part == 0 && threadIdx.x == 0);
   const int R = span.n * a.G, r0 = tile * kTileRows;
   if (r0 >= R) return;
@@ -391,7 +394,11 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a,
   seen_keys<PAGED>(a, span, i_last, lo2, hi2);
   if (threadIdx.x == 0) dirty = 0;
   const float *mask = !PAGED && a.mask ? a.mask + (long long)b * a.Sk : nullptr;
-  if (!PAGED && mask) {  // the first and the last valid position
+  if (!PAGED && mask && plan.edges) {
+    const int2 e = plan.edges[b];
+    lo = e.x;
+    hi2 = e.y;
+  } else if (!PAGED && mask) {  // the first and the last valid position
     if (threadIdx.x == 0) edge[0] = a.Sk, edge[1] = 0;
     __syncthreads();
     int first = a.Sk, last = 0;
@@ -460,7 +467,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a,
   me.l = both_halves_sum(me.l);
   const long long rows = (long long)a.B * a.Hq * a.S;
   const Parts parts = parts_of(a.ws, rows, plan.parts);
-  const long long prow = part * rows + (long long)bh * a.S * a.G;
+  const long long prow = part * rows + ((long long)b * a.Hk + h) * a.S * a.G;
   if (live) {
     if (plan.parts > 1)
       me.put_part(parts.o + (prow + r) * a.Dh, parts.ml + prow + r, a.Dh);

@@ -29,7 +29,10 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
   };
   const int tile_unit = Dh <= 128 ? 2 : 1;  // what its registers leave room for
   const long long big = heads * ((rows + kTileRows - 1) / kTileRows);
-  p.step = Dh <= 128 && (rows <= kStepRows || big * parts(big, tile_unit) < num_cu);
+  // Tiles of 128 rows read the keys a quarter as often as those of 32, which fill the chip and end sooner where there is
+  // less to do (heads of 64: 1000 positions of 8 heads 27 us by 128, 13 by 32; 200 over 2000 of 32 heads 32 and 25, of 128
+  // heads 53 and 66; heads of 128: 300 over 9000 of 8 heads 75 and 92).
+  p.step = Dh <= 128 && (rows <= kStepRows || big * parts(big, tile_unit) < num_cu || (big < num_cu && n_keys <= (Dh <= 64 ? 4096 : 2048)));
   const int per = p.step ? kStepRows : kTileRows;
   p.tiles = (int)((rows + per - 1) / per);
   p.parts = parts(heads * p.tiles, p.step ? 1 : tile_unit);

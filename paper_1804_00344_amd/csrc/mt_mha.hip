@@ -162,7 +162,8 @@ hipError_t launch_mha(const MhaArgs &a, hipStream_t st) {
     const StepPlan s{p.tiles, p.parts, 0, 0};
     e = a.bf16_io ? launch_steps_bf16(a, s, p.share, st) : launch_steps_f32(a, s, p.share, st);
   } else {
-    TilePlan t{p.tiles, p.parts, 0, nullptr, nullptr};
+    TilePlan t{p.tiles, p.parts, 0, false, nullptr, nullptr};
+    t.fold = a.table && !a.window && 2ll * a.S >= (long long)a.n_blocks << a.page_log2;
     if (p.sort && a.mask) {
       const size_t at = p.parts > 1 ? (parts_bytes((long long)a.B * a.Hq * a.S, p.parts, a.Dh) + 255) / 256 * 256 : 0;
       int *order = (int *)((char *)a.ws + at);

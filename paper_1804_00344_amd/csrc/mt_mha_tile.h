@@ -353,6 +353,7 @@ struct TilePlan {
   int tiles;  // of kTileRows rows of a sequence's key head
   int parts;  // the key axis is cut into
   int first;  // workgroup of this launch
+  bool fold;  // whether a row's tiles differ much in their keys
   const int *order;   // masked sentences, those with the most work first, or NULL: as they come
   const int2 *edges;  // of each one's mask: its first valid position, one past its last
 };
@@ -375,14 +376,17 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a,
   // the tiles of a key head run on one XCD, whose L2 holds its keys and values, the heads of a sequence on different
   // ones; what does not divide among them is spread.  The last tiles, which see the most keys, come first.
   const int w = plan.first + blockIdx.x, per = plan.tiles * plan.parts, heads = a.B * a.Hk, even = heads / kXcds * kXcds;
+  // Where all workgroups run at once, two a unit, and the first rows see few keys: the second of a unit is taken from the
+  // other end, a short one with a long one (4 x 1000 positions of 16 heads of 64: fp32 144 -> 97 us, bf16 28 -> 24).
+  auto fold = [&](int v, int n, int units) { return plan.fold && v >= units && n <= 2 * units ? units + n - 1 - v : v; };
   int bh, u;
   if (w < even * per) {
-    const int v = w / kXcds;
+    const int v = fold(w / kXcds, even / kXcds * per, a.num_cu / kXcds);
     const int round = v / per, x = w % kXcds;
     bh = round * kXcds + (plan.order && round % 2 ? kXcds - 1 - x : x);  // sorted by work: there and back
     u = v % per;
   } else {
-    const int v = w - even * per;
+    const int v = fold(w - even * per, (heads - even) * per, a.num_cu);
     bh = even + v / per;
     u = v % per;
   }

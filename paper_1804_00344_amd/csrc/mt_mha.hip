@@ -10,6 +10,7 @@ namespace {
 struct Plan {
   bool step, share;
   bool sort;  // masked sentences by their work
+  bool ends;  // the ends of masks looked for once and not by every workgroup
   int tiles, parts;
 };
 
@@ -36,28 +37,37 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
   const int per = p.step ? kStepRows : kTileRows;
   p.tiles = (int)((rows + per - 1) / per);
   p.parts = parts(heads * p.tiles, p.step ? 1 : tile_unit);
-  p.share = heads * p.tiles < 8 * num_cu;
+  // the waves of a workgroup share a row's keys where there are few rows, or long ones (256 tokens of 16 heads over up to 2000
+  // 146 -> 131 us; 768 of 8 over up to 512 41 -> 49)
+  p.share = heads * p.tiles < 8 * num_cu || n_keys >= 1024;
   // Under a mask over several rounds of workgroups: the longest sentence last would leave most units waiting for it, and
   // every workgroup would look for its sentence's end (8 ragged sentences of up to 2048 x 2048, 16 heads of 64: 101 us as
   // they come, 87 sorted, with the two launches that find the order).  Over pages the ends are known, and sorting 16
   // ragged prompts of up to 2048 gained as often as it lost (86 to 108 us, sorted 92).
   p.sort = !p.step && B >= 4 && B <= kMaxSort && heads * p.tiles * p.parts >= 4 * num_cu;
+  p.ends = p.sort || n_keys >= 2048;  // a launch more (12 queries of 8 heads over 30000 positions 108 -> 26 us, over 2100 17 -> 16)
   return p;
 }
 
 // The first valid position of each sentence and one past its last: a workgroup each
-__global__ void __launch_bounds__(256) edges_kernel(const float *mask, int S, int2 *edges) {
-  __shared__ int lo[4], hi[4];
+__global__ void __launch_bounds__(1024) edges_kernel(const float *mask, int S, int2 *edges) {
+  __shared__ int lo[16], hi[16];
   const float *m = mask + (long long)blockIdx.x * S;
   int first = S, last = 0;
-  for (int j = threadIdx.x; j < S; j += 256)
-    if (m[j] != 0.f) first = min(first, j), last = j + 1;
+#pragma unroll 4
+  for (int j = threadIdx.x; j < S; j += 1024) {
+    const bool valid = m[j] != 0.f;
+    first = valid ? min(first, j) : first;
+    last = valid ? j + 1 : last;
+  }
   first = wave_ext<int, false>(first);
   last = wave_ext<int, true>(last);
   const int w = threadIdx.x >> 6;
   if ((threadIdx.x & 63) == 0) lo[w] = first, hi[w] = last;
   __syncthreads();
-  if (threadIdx.x == 0) edges[blockIdx.x] = make_int2(min(min(lo[0], lo[1]), min(lo[2], lo[3])), max(max(hi[0], hi[1]), max(hi[2], hi[3])));
+  if (threadIdx.x != 0) return;
+  for (int i = 1; i < 16; ++i) first = min(first, lo[i]), last = max(last, hi[i]);
+  edges[blockIdx.x] = make_int2(first, last);
 }
 
 // The sentences by their work: a thread each, whose place is the number of those before it
@@ -148,7 +158,7 @@ size_t mha_workspace_bytes(int Hq, int Hk, int Dh, bool f32, int B, int S, long 
   for (int w : {window, 0}) {
     const Plan p = plan_of(Hq, Hk, Dh, B, S, n_keys, w, f32, num_cu);
     size_t n = p.parts > 1 ? (parts_bytes((long long)B * Hq * S, p.parts, Dh) + 255) / 256 * 256 : 256;
-    if (p.sort) n += (size_t)kMaxSort * 12;  // behind the parts: places and edges
+    if (p.ends) n += (size_t)kMaxSort * 4 + ((size_t)B * 8 + 255) / 256 * 256;  // behind the parts: places and edges
     if (n > most) most = n;
   }
   return most;
@@ -157,22 +167,25 @@ size_t mha_workspace_bytes(int Hq, int Hk, int Dh, bool f32, int B, int S, long 
 hipError_t launch_mha(const MhaArgs &a, hipStream_t st) {
   const Plan p = plan_of(a.Hq, a.Hk, a.Dh, a.B, a.S, a.table ? (long long)a.n_blocks << a.page_log2 : a.Sk, a.window,
                         !a.bf16_io, a.num_cu);
+  int *order = nullptr;
+  int2 *edges = nullptr;
+  if (p.ends && a.mask) {
+    const size_t at = p.parts > 1 ? (parts_bytes((long long)a.B * a.Hq * a.S, p.parts, a.Dh) + 255) / 256 * 256 : 0;
+    order = (int *)((char *)a.ws + at);
+    edges = (int2 *)(order + kMaxSort);
+    hipLaunchKernelGGL(edges_kernel, dim3(a.B), dim3(1024), 0, st, a.mask, a.Sk, edges);
+    if (p.sort)
+      hipLaunchKernelGGL(order_kernel, dim3(1), dim3(kMaxSort), 0, st, a, edges, order);
+    else
+      order = nullptr;
+  }
   hipError_t e;
   if (p.step) {
-    const StepPlan s{p.tiles, p.parts, 0, 0};
+    const StepPlan s{p.tiles, p.parts, 0, 0, edges};
     e = a.bf16_io ? launch_steps_bf16(a, s, p.share, st) : launch_steps_f32(a, s, p.share, st);
   } else {
-    TilePlan t{p.tiles, p.parts, 0, false, nullptr, nullptr};
+    TilePlan t{p.tiles, p.parts, 0, false, order, edges};
     t.fold = a.table && !a.window && 2ll * a.S >= (long long)a.n_blocks << a.page_log2;
-    if (p.sort && a.mask) {
-      const size_t at = p.parts > 1 ? (parts_bytes((long long)a.B * a.Hq * a.S, p.parts, a.Dh) + 255) / 256 * 256 : 0;
-      int *order = (int *)((char *)a.ws + at);
-      int2 *edges = (int2 *)(order + kMaxSort);
-      hipLaunchKernelGGL(edges_kernel, dim3(a.B), dim3(256), 0, st, a.mask, a.Sk, edges);
-      hipLaunchKernelGGL(order_kernel, dim3(1), dim3(kMaxSort), 0, st, a, edges, order);
-      t.order = order;
-      t.edges = edges;
-    }
     e = a.bf16_io ? launch_tiles_bf16(a, t, st) : launch_tiles_f32(a, t, st);
   }
   if (e != hipSuccess || p.parts == 1) return e;

@@ -13,6 +13,7 @@ struct StepPlan {
   int parts;  // the key axis is cut into
   int first;  // workgroup of this launch
   unsigned jobs;  // rows' tiles of all key heads and parts: below 2^31
+  const int2 *edges;  // of each sentence's mask: its first valid position, one past its last; or NULL: not yet known
 };
 
 // Tiles of 32 rows of one key head (as in the tile kernel) and 32 keys at a time, each wave with its own part of LDS and
@@ -47,7 +48,11 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T
   Rows<T, DP> me;
   me.start((const T *)a.q + ((long long)b * a.S + qi) * a.ldq + (long long)hq * a.Dh, live, a.Dh);
   const float *mask = !PAGED && a.mask ? a.mask + (long long)b * a.Sk : nullptr;
-  if (!PAGED && mask) {  // the first and the last valid position
+  if (!PAGED && mask && plan.edges) {
+    const int2 e = plan.edges[b];
+    lo = e.x;
+    hi2 = e.y;
+  } else if (!PAGED && mask) {  // the first and the last valid position
     int first = a.Sk, last = 0;
     for (int j = lane; j < a.Sk; j += 64)
       if (mask[j] != 0.f) first = min(first, j), last = j + 1;

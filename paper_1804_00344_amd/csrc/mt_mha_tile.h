@@ -355,7 +355,7 @@ struct TilePlan {
   int first;  // workgroup of this launch
   bool fold;  // whether a row's tiles differ much in their keys
   const int *order;   // masked sentences, those with the most work first, or NULL: as they come
-  const int2 *edges;  // of each one's mask: its first valid position, one past its last
+  const int2 *edges;  // of each sentence's mask: its first valid position, one past its last; or NULL: not yet known
 };
 
 // A workgroup of four waves takes 128 rows of one key head of one sequence: row r is query r / G, head r % G of those

@@ -256,7 +256,8 @@ CROSS = [  # B, T, S, Hq, Hk, Dh, mask, n_q
     (4, 12, 33, 4, 2, 40, "holes", [12, 0, 5, 12]), (2, 7, 97, 6, 2, 72, "holes", None), (2, 40, 130, 2, 1, 128, "ends", None),
     (2, 100, 64, 4, 4, 64, "holes", [100, 33]), (1, 3, 1030, 4, 1, 128, "ends", None), (2, 65, 257, 3, 3, 256, "holes", None),
     (1, 150, 300, 16, 2, 64, None, None), (2, 1, 300, 40, 1, 96, "holes", None),
-    (6, 700, 90, 32, 32, 8, "holes", [700, 1, 0, 300, 699, 700]), (70, 100, 40, 16, 16, 16, "ends", None)]  # sorted by their work
+    (6, 700, 90, 32, 32, 8, "holes", [700, 1, 0, 300, 699, 700]), (70, 100, 40, 16, 16, 16, "ends", None),  # sorted by their work
+    (3, 3, 2500, 2, 1, 64, "holes", None), (2, 400, 2100, 2, 2, 16, "ends", [400, 129])]  # ends of masks found once
 
 
 def make_mask(kind, B, S, g):

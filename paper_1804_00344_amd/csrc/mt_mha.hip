@@ -1,14 +1,14 @@
 // Attention of query heads over keys and values in pages of a cache, or in rows of another length under a mask:
 //   y = sum_j softmax_j(scale q.k_j) v_j over the keys that a query sees.
 // Here: how a call is split over the chip, and the join of the parts of a key axis that is cut.
-#include "mt_mha_step.h"
+#include "mt_mha_row.h"
 
 namespace mt {
 
 namespace {
 
 struct Plan {
-  bool step, share;
+  bool step, share, few;
   bool sort;  // masked sentences by their work
   bool ends;  // the ends of masks looked for once and not by every workgroup
   int tiles, parts;
@@ -22,7 +22,10 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
   if (window && n_keys > (long long)window + S) n_keys = (long long)window + S;  // keys that a row's queries see
   // The key axis is cut until there are enough workgroups; a part has 256 keys at least.  Tiles of 128 rows want two a unit,
   // one computing scores while the other takes exponentials (300 positions over 9000, 32 heads of 128: 84 us, one 132);
-  // few rows want one, as the parts have to be joined (a token over 20000, 32 heads of 128: 27 us, two 36).
+  // tiles of 32 want one, as the parts have to be joined (a token over 20000, 32 heads of 128 in 8 groups: 26 us, two 30),
+  // but two where long sequences would get few parts (16 of 10 to 20000 of them 165 -> 116 us, all of 20000 228 -> 231); the
+  // vector units want what fits (16 tokens of up to 4000 in fp32, 4 groups of 4 heads of 128: one 52 us, two 38; in bf16 of up to
+  // 9000, 16 heads of 192: one 304, two 187, four 148).
   const long long most = n_keys / 256 < 1 ? 1 : n_keys / 256;
   auto parts = [&](long long wgs, int a_unit) {
     const long long want = a_unit * num_cu / wgs;
@@ -34,9 +37,12 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
   // less to do (heads of 64: 1000 positions of 8 heads 27 us by 128, 13 by 32; 200 over 2000 of 32 heads 32 and 25, of 128
   // heads 53 and 66; heads of 128: 300 over 9000 of 8 heads 75 and 92).
   p.step = Dh <= 128 && (rows <= kStepRows || big * parts(big, tile_unit) < num_cu || (big < num_cu && n_keys <= (Dh <= 64 ? 4096 : 2048)));
+  p.few = few_rows(rows, Dh, f32);
+  p.step |= p.few;
   const int per = p.step ? kStepRows : kTileRows;
   p.tiles = (int)((rows + per - 1) / per);
-  p.parts = parts(heads * p.tiles, p.step ? 1 : tile_unit);
+  const int unit = !p.step ? tile_unit : !p.few ? (heads * p.tiles * 4 >= num_cu ? 2 : 1) : rows == 1 ? 4 : 2;
+  p.parts = parts(heads * p.tiles, unit);
   // the waves of a workgroup share a row's keys where there are few rows, or long ones (256 tokens of 16 heads over up to 2000
   // 146 -> 131 us; 768 of 8 over up to 512 41 -> 49)
   p.share = heads * p.tiles < 8 * num_cu || n_keys >= 1024;
@@ -182,7 +188,10 @@ hipError_t launch_mha(const MhaArgs &a, hipStream_t st) {
   hipError_t e;
   if (p.step) {
     const StepPlan s{p.tiles, p.parts, 0, 0, edges};
-    e = a.bf16_io ? launch_steps_bf16(a, s, p.share, st) : launch_steps_f32(a, s, p.share, st);
+    if (p.few)
+      e = a.bf16_io ? launch_rows_bf16(a, s, p.share, st) : launch_rows_f32(a, s, p.share, st);
+    else
+      e = a.bf16_io ? launch_steps_bf16(a, s, p.share, st) : launch_steps_f32(a, s, p.share, st);
   } else {
     TilePlan t{p.tiles, p.parts, 0, false, order, edges};
     t.fold = a.table && !a.window && 2ll * a.S >= (long long)a.n_blocks << a.page_log2;

@@ -19,7 +19,7 @@ struct StepPlan {
 // Tiles of 32 rows of one key head (as in the tile kernel) and 32 keys at a time, each wave with its own part of LDS and
 // no barriers.  SHARE: the four waves of a workgroup take the tiles of keys in turn and join their sums at the end, for
 // short latency; else each wave has its own rows, for many of them.  Bound by memory where the cache is long (16 tokens over
-// 32768 positions, 8 key heads of 128 in bf16: 364 us, 5.9 TB/s; by tiles of 128 rows 412), by one tile's latency where it is not.
+// 32768 positions, 8 key heads of 128 in bf16: 367 us, 5.9 TB/s; by tiles of 128 rows 412), by one tile's latency where it is not.
 // The 32 columns of a product that one token leaves empty cost nothing then (matrix units 8% busy).
 template <typename T, int DP, bool PAGED, bool SHARE>
 __global__ void __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 256 ? 2 : 1) step_kernel(MhaArgs a, StepPlan plan) {

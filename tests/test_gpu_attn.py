@@ -432,3 +432,29 @@ def test_append_out_of_range(dtype):
     mt.mt_attn_append(a, q, k, v, out, dev(torch.tensor([17, 16], dtype=torch.int32)), table, kc, vc)
     assert mt.mt_attn_device_errors(a) == 4
     assert torch.equal(vc[2, 0, 0], v[0, 2])  # page 9 of 3: the last one
+
+
+FEW = [  # B, S, Hq, Hk, Dh, page, window, lens, n_new: one to four rows of a key head
+    (2, 1, 4, 4, 192, 64, 0, [5000, 1], None),
+    (2, 1, 8, 2, 200, 16, 0, [2900, 700], None),
+    (1, 4, 2, 2, 64, 8, 0, [1029], None),
+    (3, 2, 4, 2, 256, 16, 30, [90, 31, 600], [2, 1, 2]),
+    (3, 3, 3, 3, 24, 32, 5, [3, 2, 70], [3, 3, 0]),
+    (260, 1, 8, 8, 16, 8, 0, [1 + 7 * b % 41 for b in range(260)], None),  # a wave a row
+    (260, 1, 32, 8, 72, 8, 11, [1 + 5 * b % 37 for b in range(260)], None),
+]
+FEW_CROSS = [  # B, T, S, Hq, Hk, Dh, mask, n_q
+    (2, 1, 2100, 3, 3, 192, "holes", None), (3, 2, 700, 4, 2, 256, "ends", [2, 0, 1]), (2, 4, 90, 2, 2, 40, "holes", [4, 3]),
+    (260, 1, 23, 8, 8, 64, "ends", None), (260, 1, 37, 32, 8, 200, "holes", None)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", FEW, ids=lambda c: "-".join(str(v) for v in c[:7]))
+def test_paged_few_rows(case, dtype):
+    test_paged(case, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", FEW_CROSS, ids=lambda c: "-".join(str(v) for v in c[:7]))
+def test_cross_few_rows(case, dtype):
+    test_cross(case, dtype)

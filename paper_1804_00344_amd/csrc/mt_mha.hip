@@ -39,7 +39,7 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
   p.step = Dh <= 128 && (rows <= kStepRows || big * parts(big, tile_unit) < num_cu || (big < num_cu && n_keys <= (Dh <= 64 ? 4096 : 2048)));
   p.few = few_rows(rows, Dh, f32);
   p.step |= p.few;
-  const int per = p.step ? kStepRows : kTileRows;
+  const int per = p.few ? kRowRows : p.step ? kStepRows : kTileRows;
   p.tiles = (int)((rows + per - 1) / per);
   const int unit = !p.step ? tile_unit : !p.few ? (heads * p.tiles * 4 >= num_cu ? 2 : 1) : rows == 1 ? 4 : 2;
   p.parts = parts(heads * p.tiles, unit);

@@ -1,14 +1,18 @@
-// Attention of up to four query rows by the vector units: kernel and launch, instantiated by mt_mha_row_*.hip.
+// Attention of tiles of up to four query rows by the vector units: kernel and launch, instantiated by mt_mha_row_*.hip.
 #pragma once
 
 #include "mt_mha_step.h"
 
 namespace mt {
 
-constexpr int kRowRows = 4;
+constexpr int kRowRows = 4;  // of a tile
 
-// Where the vector units are faster than the matrix units, which have no step kernel for more than 128 features
-constexpr bool few_rows(long long rows, int Dh, bool f32) { return rows <= kRowRows && (f32 || Dh > 128 || rows == 1); }
+// Where the vector units are faster than the matrix units, which have no step kernel for more than 128 features (16 sentences
+// of up to 1000 positions, 8 heads of 256 in fp32: 8 rows a head 57 us, 16 rows 97, 32 rows 165, by tiles of 128 rows 172 to 182;
+// heads of 128: 8 rows 34, 12 rows 51, by the step kernel 41 and 37)
+constexpr bool few_rows(long long rows, int Dh, bool f32) {
+  return f32 ? rows <= (Dh > 128 ? 16 : kRowRows) : rows <= (Dh > 128 ? kRowRows : 1);
+}
 
 // v of all lanes that differ in bits O .. 32 of their number, combined
 template <int O, typename F>
@@ -51,7 +55,7 @@ __device__ __forceinline__ float word_at(const Words &w, int e) {
   return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
 }
 
-// Up to NR rows of one key head.  A wave reads NL chunks of 16 bytes a lane of keys and of values at a time, whole rows by
+// Tiles of up to NR rows of one key head.  A wave reads NL chunks of 16 bytes a lane of keys and of values at a time, whole rows by
 // CH neighbouring lanes, and multiplies them where they are: a score is summed over its CH lanes, a value's products stay in
 // the lane that has its features until the end.  The next keys are on their way while this tile's values are multiplied, and
 // the other way round.  Nothing is staged in LDS, so that three to four times the waves of the step kernel have loads on
@@ -69,14 +73,14 @@ __global__ void __launch_bounds__(256, NR == 1 ? 4 : 2) row_kernel(MhaArgs a, St
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned w = plan.first + xcd_remap(blockIdx.x, gridDim.x), job = SHARE ? w : w * 4 + wave;
   if (job >= plan.jobs) return;
-  const int part = (int)(job % (unsigned)plan.parts), bh = (int)(job / (unsigned)plan.parts);
-  const int b = bh / a.Hk, h = bh - b * a.Hk;
-  const RowSpan span = row_span<PAGED>(a, b, h == 0 && part == 0 && lane == 0);
-  const int R = span.n * a.G;
+  const int part = (int)(job % (unsigned)plan.parts), tile = (int)(job / (unsigned)plan.parts % (unsigned)plan.tiles);
+  const int bh = (int)(job / (unsigned)plan.parts / (unsigned)plan.tiles), b = bh / a.Hk, h = bh - b * a.Hk;
+  const RowSpan span = row_span<PAGED>(a, b, h == 0 && tile == 0 && part == 0 && lane == 0);
+  const int r0 = tile * NR, R = span.n * a.G - r0;  // of the rows, those from r0
   if (R <= 0) return;
   int lo, hi, lo2, hi2;  // keys that some row sees: [lo, hi2); that all see: [lo2, hi)
-  seen_keys<PAGED>(a, span, 0, lo, hi);
-  seen_keys<PAGED>(a, span, span.n - 1, lo2, hi2);
+  seen_keys<PAGED>(a, span, r0 / a.G, lo, hi);
+  seen_keys<PAGED>(a, span, (r0 + min(NR, R) - 1) / a.G, lo2, hi2);
   const int chunk = lane % CH, group = lane / CH;
   const bool feature = chunk * EPC < a.Dh;
   // ---- the rows' features in this lane
@@ -84,7 +88,7 @@ __global__ void __launch_bounds__(256, NR == 1 ? 4 : 2) row_kernel(MhaArgs a, St
   int qlo[NR], qhi[NR];
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
-    const int rr = min(r, R - 1), i = rr / a.G, hq = h * a.G + rr - i * a.G;
+    const int rr = r0 + min(r, R - 1), i = rr / a.G, hq = h * a.G + rr - i * a.G;
     seen_keys<PAGED>(a, span, i, qlo[r], qhi[r]);
     typename V::Raw v = {};
     if (feature) v = V::raw_any((const T *)a.q + ((long long)b * a.S + i) * a.ldq + (long long)hq * a.Dh + chunk * EPC);
@@ -310,11 +314,11 @@ __global__ void __launch_bounds__(256, NR == 1 ? 4 : 2) row_kernel(MhaArgs a, St
   if (lane >= CH || !feature) return;
   const long long rows = (long long)a.B * a.Hq * a.S;
   const Parts parts = parts_of(a.ws, rows, plan.parts);
-  const long long prow = part * rows + (long long)bh * a.S * a.G;
+  const long long prow = part * rows + (long long)bh * a.S * a.G + r0;
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
     if (r >= R) break;
-    const int i = r / a.G, hq = h * a.G + r - i * a.G;
+    const int i = (r0 + r) / a.G, hq = h * a.G + r0 + r - i * a.G;
     if (plan.parts > 1) {
       float *po = parts.o + (prow + r) * a.Dh + chunk * EPC;
 #pragma unroll
@@ -331,7 +335,7 @@ __global__ void __launch_bounds__(256, NR == 1 ? 4 : 2) row_kernel(MhaArgs a, St
 
 template <typename T, int DP, int NR, bool PAGED>
 hipError_t launch_rows_of(const MhaArgs &a, StepPlan plan, bool share, hipStream_t st) {
-  const long long jobs = (long long)a.B * a.Hk * plan.parts, all = share ? jobs : (jobs + 3) / 4;
+  const long long jobs = (long long)a.B * a.Hk * plan.tiles * plan.parts, all = share ? jobs : (jobs + 3) / 4;
   plan.jobs = (unsigned)jobs;
   const long long most = 1 << 22;  // workgroups of a launch
   for (long long first = 0; first < all; first += most) {
@@ -354,7 +358,7 @@ hipError_t launch_rows_as(const MhaArgs &a, const StepPlan &plan, bool share, hi
   return launch_rows_of<T, 256, NR, PAGED>(a, plan, share, st);
 }
 
-// S * G is at most kRowRows, and few_rows of it
+// rows of which few_rows holds
 template <typename T>
 hipError_t launch_rows_typed(const MhaArgs &a, const StepPlan &plan, bool share, hipStream_t st) {
   const bool one = (long long)a.S * a.G == 1;

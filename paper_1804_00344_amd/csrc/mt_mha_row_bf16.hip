@@ -1,4 +1,4 @@
-// Attention of up to four query rows, bf16.
+// Attention of tiles of up to four query rows, bf16.
 #include "mt_mha_row.h"
 
 namespace mt {

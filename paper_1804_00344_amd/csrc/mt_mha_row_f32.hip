@@ -1,4 +1,4 @@
-// Attention of up to four query rows, fp32.
+// Attention of tiles of up to four query rows, fp32.
 #include "mt_mha_row.h"
 
 namespace mt {

@@ -458,3 +458,9 @@ def test_paged_few_rows(case, dtype):
 @pytest.mark.parametrize("case", FEW_CROSS, ids=lambda c: "-".join(str(v) for v in c[:7]))
 def test_cross_few_rows(case, dtype):
     test_cross(case, dtype)
+
+
+@pytest.mark.parametrize("B,S,Hq,Hk,Dh,window", [(2, 5, 6, 3, 232, 0), (1, 16, 2, 2, 136, 0), (3, 7, 4, 2, 256, 9)])
+def test_paged_wide_heads_in_tiles_of_few_rows(B, S, Hq, Hk, Dh, window):
+    lens = [300, S, 33][:B]
+    test_paged((B, S, Hq, Hk, Dh, 16, window, lens, [S, 2, S - 1][:B]), "f32")

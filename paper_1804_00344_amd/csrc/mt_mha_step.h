@@ -184,9 +184,7 @@ hipError_t launch_steps_of(const MhaArgs &a, StepPlan plan, bool share, hipStrea
 template <typename T, bool PAGED>
 hipError_t launch_steps_as(const MhaArgs &a, const StepPlan &plan, bool share, hipStream_t st) {
   if (a.Dh <= 64) return launch_steps_of<T, 64, PAGED>(a, plan, share, st);
-  if (a.Dh <= 128) return launch_steps_of<T, 128, PAGED>(a, plan, share, st);
-  if constexpr (sizeof(T) == 2) return launch_steps_of<T, 256, PAGED>(a, plan, share, st);
-  return hipErrorInvalidValue;  // fp32 heads of more than 128 features: a tile in flight would not fit a wave's registers
+  return launch_steps_of<T, 128, PAGED>(a, plan, share, st);  // of wider heads a tile in flight would not fit a wave's registers
 }
 
 hipError_t launch_steps_bf16(const MhaArgs &a, const StepPlan &plan, bool share, hipStream_t st);

@@ -473,7 +473,8 @@ class PagedCache:
             mt.mt_pages_pack(self.attn, self.table, self.lens, self.k, self.v, table, lens, out.k, out.v, out.free, ws=ws,
                              stream=stream)
         self._wait()  # the workspace is given back
-        out.free = n_pages - out.free
+        out.free.neg_().add_(n_pages)  # the used pages, until here
+        out._wait()
         out.table, out.lens = table, lens
         return out
 

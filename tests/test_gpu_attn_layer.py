@@ -208,3 +208,19 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for row in ys:
         assert torch.equal(row[0], want[0]) and torch.equal(row[1], want[1])
+
+
+def test_a_packed_cache_counts_its_free_pages():
+    """Also where other streams than the current one pack and go on."""
+    attn = mt.mt_attn_load(mt.make_attn_config(2, 1, 64, page=8))
+    cache = PagedCache(attn, 2, 40, 6)
+    cache.advance(i32([-1] * 5), i32([3, 0, 17, 8, 9]))  # 1 + 0 + 3 + 1 + 2 pages
+    assert int(cache.free) == 33
+    first, second = torch.cuda.Stream(), torch.cuda.Stream()
+    small = cache.pack(12, stream=first)
+    assert int(small.free) == 5 and small.lens.tolist() == [3, 0, 17, 8, 9]
+    small = cache.pack(12, stream=first)
+    small.advance(i32([0, 0, 3]), i32([1, 1, 1]), stream=second)  # a copy of the first page, and a page behind the fourth's
+    torch.cuda.synchronize()
+    assert int(small.free) == 8 and small.lens.tolist() == [4, 4, 9]
+    assert cache.pack(6).lens.tolist() == [0] * 5 and mt.mt_attn_device_errors(attn) == 8

@@ -194,8 +194,7 @@ __global__ void __launch_bounds__(256) list_kernel(PagesArgs a, Space s, int row
     }
 }
 
-// All of the above by one workgroup, the counts in LDS, for tables and pools of moderate size: 5 rows of a pool of 23
-// pages 15 -> 7.6 us with the copies, 768 rows of 3900 pages 38 -> 22 (7 of them here: rows, table, counts and ranks wait for each other).
+// All of the above by one workgroup, the counts in LDS, for tables and pools of moderate size: 768 rows of 3900 pages 38 -> 22 (7 of them here: rows, table, counts and ranks wait for each other).
 constexpr int kSmallPages = 8192, kSmallRows = 2048, kSmallEntries = 1 << 15;
 
 template <bool GROW>
@@ -359,6 +358,18 @@ __device__ __forceinline__ void copy_chunks(char *dst, const char *src, int n, F
   }
 }
 
+// The page that row r goes on writing, copied to another one in slice blockIdx.y: its positions so far, a run of every head
+__device__ __forceinline__ void copy_begun(const PagesArgs &a, const Row &r, int from, int to) {
+  const long long size = page_size(a), base = (long long)(blockIdx.y >> 1) * a.n_pages * size;
+  char *const cache = (char *)(blockIdx.y & 1 ? a.v_out : a.k_out) + base;
+  const int run = (int)((r.len & ((1 << a.page_log2) - 1)) * a.head_bytes / 16), head = (int)(a.head_bytes << a.page_log2);
+  auto where = [&](int i) __attribute__((always_inline)) -> long long {
+    const int h = i / run;
+    return h * head + (i - h * run) * 16;
+  };
+  copy_chunks(cache + to * size, cache + from * size, run * a.Hk, where);
+}
+
 // Row m: its table and length, and (blockIdx.y: a layer's keys or values) the copy of its shared page.
 __global__ void __launch_bounds__(256) assign_kernel(PagesArgs a, Space s) {
   const int m = blockIdx.x;
@@ -386,17 +397,16 @@ __global__ void __launch_bounds__(256) assign_kernel(PagesArgs a, Space s) {
       if (m == 0 && a.free_out) *a.free_out = free_all - need_all;
     }
   }
-  if (!cow) return;
-  const long long size = page_size(a), base = (long long)(blockIdx.y >> 1) * a.n_pages * size;
-  const long long from = base + page_of(a, r, r.blocks - 1, false) * size, to = base + s.list[begin] * size;
-  char *const cache = (char *)(blockIdx.y & 1 ? a.v_out : a.k_out);
-  // the positions so far: a run of every head
-  const int run = (int)((r.len & ((1 << a.page_log2) - 1)) * a.head_bytes / 16), head = (int)(a.head_bytes << a.page_log2);
-  auto where = [&](int i) __attribute__((always_inline)) -> long long {
-    const int h = i / run;
-    return h * head + (i - h * run) * 16;
-  };
-  copy_chunks(cache + to, cache + from, run * a.Hk, where);
+  if (cow) copy_begun(a, r, page_of(a, r, r.blocks - 1, false), s.list[begin]);
+}
+
+// Pages list[0 .. used) of slice y, a layer's keys or values, to the front of the other cache
+__device__ __forceinline__ void move_pages(const PagesArgs &a, const int *list, int used, int y) {
+  const long long size = page_size(a), layer = y >> 1;
+  const char *in = (const char *)(y & 1 ? a.v_in : a.k_in) + layer * a.n_pages * size;
+  char *out = (char *)(y & 1 ? a.v_out : a.k_out) + layer * a.n_pages_out * size;
+  for (int i = blockIdx.x; i < used; i += gridDim.x)
+    copy_chunks(out + i * size, in + list[i] * size, (int)(size / 16), [](int c) __attribute__((always_inline)) { return c * 16ll; });
 }
 
 // Pack: the pages, each slice blockIdx.y a layer's keys or values; TABLES: in front of them a slice that renumbers the tables
@@ -418,13 +428,131 @@ __global__ void __launch_bounds__(256) move_kernel(PagesArgs a, Space s) {
     }
     return;
   }
-  if (fails) return;
-  const long long size = page_size(a);
-  const int y = blockIdx.y - TABLES, layer = y >> 1;
-  const char *in = (const char *)(y & 1 ? a.v_in : a.k_in) + (long long)layer * a.n_pages * size;
-  char *out = (char *)(y & 1 ? a.v_out : a.k_out) + (long long)layer * a.n_pages_out * size;
-  for (int i = blockIdx.x; i < used; i += gridDim.x)
-    copy_chunks(out + i * size, in + s.list[i] * size, (int)(size / 16), [](int c) __attribute__((always_inline)) { return c * 16ll; });
+  if (!fails) move_pages(a, s.list, used, blockIdx.y - TABLES);
+}
+
+// A call on small tables and pools in one launch: every workgroup makes the plan for itself, in LDS, instead of waiting for
+// one that does: 5 rows of a pool of 21 pages 6.9 -> 4.1 us (the call 10.0 -> 7.2), 120 rows of 445 pages through six layers
+// 9.3 -> 7.6; 240 rows of 866 pages through six 11.9 -> 15.4, so not where many workgroups would plan for many entries.  Packed,
+// whose plan is shorter: 106 pages through three layers 6.0 -> 3.3 us, 558 through six 21.9 -> 21.2.  Grid as assign_kernel's or
+// move_kernel<false>'s.
+constexpr int kTinyPages = 1024, kTinyRows = 256, kTinyEntries = 2048;
+
+template <bool GROW>
+__global__ void __launch_bounds__(256) tiny_kernel(PagesArgs a) {
+  __shared__ int refs[kTinyPages], list[kTinyPages], growers[GROW ? kTinyPages : 1], last[GROW ? kTinyPages : 1];
+  __shared__ int src[kTinyRows], len[kTinyRows], add[GROW ? kTinyRows : 1], end[GROW ? kTinyRows : 1];  // of the rows; end: their last page
+  __shared__ int too_long, mine[2];  // pages that the rows before this workgroup's take, and its own
+  const int t = threadIdx.x, pmask = (1 << a.page_log2) - 1, n = a.M * a.n_blocks;
+  const bool one = blockIdx.x == 0 && blockIdx.y == 0;  // reports, and writes what is there once
+  for (int p = t; p < a.n_pages; p += 256) {
+    refs[p] = 0;
+    if (GROW) growers[p] = last[p] = 0;
+  }
+  if (t == 0) too_long = 0;
+  if (t < a.M) {
+    const Row r = row_of(a, t, one);
+    src[t] = r.src;
+    len[t] = r.len;
+    if (GROW) add[t] = r.add;
+  }
+  __syncthreads();
+  auto row = [&](int m) {
+    Row r;
+    r.src = src[m];
+    r.len = len[m];
+    r.blocks = (r.len + pmask) >> a.page_log2;
+    r.add = GROW ? add[m] : 0;
+    return r;
+  };
+  for (int e = t; e < n; e += 256) {
+    const int m = e / a.n_blocks, j = e - m * a.n_blocks;
+    const Row r = row(m);
+    if (j >= r.blocks) continue;
+    const int p = page_of(a, r, j, one);
+    if (!GROW) {
+      refs[p] = 1;
+      continue;
+    }
+    atomicAdd(&refs[p], 1);
+    if (j == r.blocks - 1) {
+      end[m] = p;
+      if (r.add > 0 && (r.len & pmask)) {
+        atomicAdd(&growers[p], 1);
+        atomicMax(&last[p], m + 1);
+      }
+    }
+  }
+  __syncthreads();
+  int need_all = 0, total;
+  if (GROW) {
+    int need = 0;
+    if (t < a.M) {
+      const Row r = row(t);
+      const int after = blocks_after(a, r);
+      if (after > a.n_blocks) {
+        too_long = 1;
+      } else {
+        need = after - r.blocks;
+        if (r.add > 0 && (r.len & pmask)) {
+          const int p = end[t];
+          need += refs[p] > 1 && !(last[p] == t + 1 && growers[p] == refs[p]);
+        }
+      }
+    }
+    const int before = block_scan(need, need_all);
+    if (t == (int)blockIdx.x) mine[0] = before, mine[1] = need;
+  }
+  const int per = (a.n_pages + 255) / 256, first = t * per;  // a thread's pages are neighbours
+  int count = 0;
+  for (int i = 0; i < per; ++i)
+    if (first + i < a.n_pages) count += (refs[first + i] == 0) == GROW;
+  int at = block_scan(count, total);
+  for (int i = 0; i < per; ++i)
+    if (first + i < a.n_pages && (refs[first + i] == 0) == GROW) {
+      list[at] = first + i;
+      if (!GROW) refs[first + i] = at;
+      ++at;
+    }
+  __syncthreads();
+  const bool fails = GROW ? too_long || need_all > total : total > a.n_pages_out;
+  if (one && t == 0) {
+    if (a.free_out) *a.free_out = GROW ? (fails ? a.n_pages : total - need_all) : fails ? 0 : total;
+    if (fails) atomicOr(a.err, kErrRoom);
+  }
+  if (!GROW) {
+    if (one) {
+      for (int e = t; e < n; e += 256) {
+        const int m = e / a.n_blocks, j = e - m * a.n_blocks;
+        const Row r = row(m);
+        a.table_out[e] = !fails && j < r.blocks ? refs[page_of(a, r, j, false)] : -1;
+        if (j == 0) a.len_out[m] = fails ? 0 : r.len;
+      }
+    }
+    if (!fails) move_pages(a, list, total, blockIdx.y);
+    return;
+  }
+  const int m = blockIdx.x;
+  const Row r = row(m);
+  const int begin = mine[0], after = fails ? 0 : blocks_after(a, r), cow = fails ? 0 : mine[1] - (after - r.blocks);
+  if (blockIdx.y == 0) {
+    for (int j = t; j < a.n_blocks; j += 256) {
+      int p = -1;
+      if (!fails && j < r.blocks)
+        p = cow && j == r.blocks - 1 ? list[begin] : page_of(a, r, j, false);
+      else if (j < after)
+        p = list[begin + cow + j - r.blocks];
+      a.table_out[(long long)m * a.n_blocks + j] = p;
+    }
+    if (t == 0) a.len_out[m] = fails ? 0 : r.len + r.add;
+  }
+  if (cow) copy_begun(a, r, end[m], list[begin]);
+}
+
+// wgs: workgroups of the launch
+bool tiny(const PagesArgs &a, long long wgs, long long most) {
+  const long long n = (long long)a.M * a.n_blocks;
+  return a.n_pages <= kTinyPages && a.M <= kTinyRows && n <= kTinyEntries && wgs * n <= most;
 }
 
 }  // namespace
@@ -457,6 +585,10 @@ bool plan(const PagesArgs &a, const Space &s, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_advance(const PagesArgs &a, hipStream_t st) {
+  if (tiny(a, 2ll * a.M * a.layers, 1 << 21)) {
+    hipLaunchKernelGGL(tiny_kernel<true>, dim3(a.M, 2 * a.layers), dim3(256), 0, st, a);
+    return hipGetLastError();
+  }
   const Space s = space(a.ws, a.M, a.n_pages);
   plan<true>(a, s, st);
   hipLaunchKernelGGL(assign_kernel, dim3(a.M, 2 * a.layers), dim3(256), 0, st, a, s);
@@ -464,8 +596,12 @@ hipError_t launch_advance(const PagesArgs &a, hipStream_t st) {
 }
 
 hipError_t launch_pack(const PagesArgs &a, hipStream_t st) {
-  const Space s = space(a.ws, a.M, a.n_pages);
   const int most = a.n_pages < a.n_pages_out ? a.n_pages : a.n_pages_out, x = most < 65536 ? most : 65536;
+  if (tiny(a, 2ll * x * a.layers, 1 << 23)) {
+    hipLaunchKernelGGL(tiny_kernel<false>, dim3(x, 2 * a.layers), dim3(256), 0, st, a);
+    return hipGetLastError();
+  }
+  const Space s = space(a.ws, a.M, a.n_pages);
   if (plan<false>(a, s, st))
     hipLaunchKernelGGL(move_kernel<false>, dim3(x, 2 * a.layers), dim3(256), 0, st, a, s);
   else

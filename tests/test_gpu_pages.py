@@ -165,3 +165,46 @@ def test_pack(dtype, Hk, Dh, page, layers, M):
         assert torch.equal(to.cpu(), as_table(tables, 8, -1))
         for out, src in ((ko, p.k), (vo, p.v)):
             assert torch.equal(out[:, :len(used)].cpu(), src[:, used]) and bool((out[:, len(used):] == 7).all())
+
+
+@pytest.mark.parametrize("M,n_pages,n_blocks,layers", [
+    (256, 1024, 8, 2), (256, 1024, 8, 3), (255, 1023, 3, 6), (257, 1024, 7, 1), (200, 1025, 10, 1), (100, 1000, 21, 1),
+    (2048, 8192, 16, 1), (2049, 8192, 15, 1)])
+def test_at_the_sizes_where_the_plan_changes(M, n_pages, n_blocks, layers):
+    """Every workgroup its own plan, one workgroup's, many workgroups': room, no room, entries out of range, packed."""
+    a = layer(1, 1, 8, "bf16", page=8)
+    p = Pool(a, layers, n_pages, n_blocks, 8)
+    g = gen(M + layers)
+    most = min(8 * n_pages // (2 * M), 8 * n_blocks - 3)
+    assert p.advance([-1] * M, torch.randint(0, most + 1, (M,), generator=g).tolist())
+    row = torch.randint(-1, M, (M,), generator=g).tolist()
+    assert p.advance(row, torch.randint(0, 3, (M,), generator=g).tolist())
+    kept = list(p.rows)
+    assert not p.advance(list(range(M)), [0] * (M - 1) + [8 * n_blocks])  # past the blocks of a table
+    if n_pages < M * n_blocks:
+        assert not p.advance(list(range(M)), [8 * n_blocks - n for n, _ in kept])  # all that tables have room for
+    # pages out of range: clamped and reported
+    table = as_table([r[1] for r in kept], n_blocks, -77)
+    long = [m for m, (n, _) in enumerate(kept) if n > 8]
+    table[long[0], 0], table[long[-1], 1] = -3, n_pages + 5
+    clean = table.clone()
+    clean[long[0], 0], clean[long[-1], 1] = 0, n_pages - 1
+    ws = space(mt.mt_pages_workspace_bytes(a, M, n_pages))
+    got = []
+    for t in (table, clean):
+        to, ln = torch.empty(M, n_blocks, dtype=torch.int32, device=DEV), torch.empty(M, dtype=torch.int32, device=DEV)
+        mt.mt_pages_advance(a, i32(list(range(M - 1)) + [M]), i32([0] * M), dev(t), i32([n for n, _ in kept]), to, ln, p.dk, p.dv, ws=ws)
+        got.append((mt.mt_attn_device_errors(a), to, ln))
+    assert got[0][0] == 1 | 4 and got[1][0] == 1
+    assert torch.equal(got[0][1], got[1][1]) and torch.equal(got[0][2], got[1][2]) and got[1][2].tolist() == [n for n, _ in kept]
+    # packed
+    tables, used = ref.pack(kept, 8)
+    n_out = len(used) + 2
+    ko, vo = (torch.full((layers, n_out) + tuple(a.page_shape), 7.0, dtype=IO["bf16"], device=DEV) for _ in range(2))
+    to, ln, un = torch.empty(M, n_blocks, dtype=torch.int32, device=DEV), torch.empty(M, dtype=torch.int32, device=DEV), i32([0])
+    mt.mt_pages_pack(a, dev(as_table([r[1] for r in kept], n_blocks, -77)), i32([n for n, _ in kept]), p.dk, p.dv, to, ln, ko, vo,
+                     un, ws=ws)
+    assert mt.mt_attn_device_errors(a) == 0 and int(un) == len(used) and ln.tolist() == [n for n, _ in kept]
+    assert torch.equal(to.cpu(), as_table(tables, n_blocks, -1))
+    for out, src in ((ko, p.k), (vo, p.v)):
+        assert torch.equal(out[:, :len(used)].cpu(), src[:, used]) and bool((out[:, len(used):] == 7).all())

@@ -20,10 +20,12 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
   Plan p;
   const long long rows = (long long)S * (Hq / Hk), heads = (long long)B * Hk;
   if (window && n_keys > (long long)window + S) n_keys = (long long)window + S;  // keys that a row's queries see
-  // The key axis is cut until there are enough workgroups; a part has 256 keys at least.  Tiles of 128 rows want two a unit,
-  // one computing scores while the other takes exponentials (300 positions over 9000, 32 heads of 128: 84 us, one 132);
-  // tiles of 32 want one, as the parts have to be joined (a token over 20000, 32 heads of 128 in 8 groups: 26 us, two 30),
-  // but two where long sequences would get few parts (16 of 10 to 20000 of them 165 -> 116 us, all of 20000 228 -> 231); the
+  // The key axis is cut until there are enough workgroups; a part has 256 keys at least.  Tiles of 128 rows want what a
+  // unit's registers hold, some computing scores while others take exponentials (300 positions over 9000, 32 heads of 128: two
+  // a unit 84 us, one 132; 700 over 9000, 32 heads of 64: three 93, two 121; 2048 over 20000, 8 heads of 64: 132 and 127);
+  // tiles of 32 want one, as the parts have to be joined (a token over 20000, 32 heads of 128 in 8 groups: 26 us, two 30; 6 x
+  // 100 queries over 900, 8 heads of 64: 14 us, two 17), but two where long sequences of one tile would get few parts (16
+  // tokens over 10 to 20000 positions 165 -> 116 us, all of 20000 228 -> 231); the
   // vector units want what fits (16 tokens of up to 4000 in fp32, 4 groups of 4 heads of 128: one 52 us, two 38; in bf16 of up to
   // 9000, 16 heads of 192: one 304, two 187, four 148).
   const long long most = n_keys / 256 < 1 ? 1 : n_keys / 256;
@@ -31,7 +33,7 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
     const long long want = a_unit * num_cu / wgs;
     return (int)(want < 1 ? 1 : want < most ? want : most);
   };
-  const int tile_unit = Dh <= 128 ? 2 : 1;  // what its registers leave room for
+  const int tile_unit = Dh <= 64 ? 3 : Dh <= 128 ? 2 : 1;
   const long long big = heads * ((rows + kTileRows - 1) / kTileRows);
   // Tiles of 128 rows read the keys a quarter as often as those of 32, which fill the chip and end sooner where there is
   // less to do (heads of 64: 1000 positions of 8 heads 27 us by 128, 13 by 32; 200 over 2000 of 32 heads 32 and 25, of 128
@@ -41,7 +43,7 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
   p.step |= p.few;
   const int per = p.few ? kRowRows : p.step ? kStepRows : kTileRows;
   p.tiles = (int)((rows + per - 1) / per);
-  const int unit = !p.step ? tile_unit : !p.few ? (heads * p.tiles * 4 >= num_cu ? 2 : 1) : rows == 1 ? 4 : 2;
+  const int unit = !p.step ? tile_unit : !p.few ? (p.tiles == 1 && heads * 4 >= num_cu ? 2 : 1) : rows == 1 ? 4 : 2;
   p.parts = parts(heads * p.tiles, unit);
   // the waves of a workgroup share a row's keys where there are few rows, or long ones (256 tokens of 16 heads over up to 2000
   // 146 -> 131 us; 768 of 8 over up to 512 41 -> 49)

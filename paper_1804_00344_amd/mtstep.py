@@ -746,7 +746,7 @@ def mt_attn_device_errors(layer: Attn) -> int:
 
 
 # The operators' small calls take the host longer than the device: what is checked of a tensor is written out here, each
-# property asked for once (a call of mt_attn_paged 4.4 -> 3.3 us, its launch 3.6).
+# property asked for once (a call of mt_attn_paged 4.4 -> 3.7 us, its launch 3.3).
 
 def _lead_rows(t, name, B, S, width, layer):
     """(address, row stride) of a matrix of B*S equally spaced rows in the layer's type."""

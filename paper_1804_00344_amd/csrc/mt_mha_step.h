@@ -13,6 +13,7 @@ struct StepPlan {
   int parts;  // the key axis is cut into
   int first;  // workgroup of this launch
   unsigned jobs;  // rows' tiles of all key heads and parts: below 2^31
+  bool falling;   // whether a row's tiles differ much in their keys, over several rounds of workgroups
   const int2 *edges;  // of each sentence's mask: its first valid position, one past its last; or NULL: not yet known
 };
 
@@ -28,9 +29,13 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T
   __shared__ float2 ends[4][32];
   __shared__ int odds[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31;
-  const unsigned w = plan.first + xcd_remap(blockIdx.x, gridDim.x), job = SHARE ? w : w * 4 + wave;
+  // a key head's jobs are neighbours on one XCD; or, falling: the last tiles of all heads, which see the most keys, come first,
+  // and no XCD has all of a long sequence's
+  const bool falling = PAGED && plan.falling;
+  const unsigned w = plan.first + (falling ? blockIdx.x : xcd_remap(blockIdx.x, gridDim.x)), job = SHARE ? w : w * 4 + wave;
   if (job >= plan.jobs) return;
-  const int part = (int)(job % (unsigned)plan.parts), u = (int)(job / (unsigned)plan.parts), bh = u / plan.tiles, tile = u - bh * plan.tiles;
+  const int part = (int)(job % (unsigned)plan.parts), u = (int)(job / (unsigned)plan.parts), heads = a.B * a.Hk;
+  const int bh = falling ? (u + u / heads) % heads : u / plan.tiles, tile = falling ? plan.tiles - 1 - u / heads : u - bh * plan.tiles;
   const int b = bh / a.Hk, h = bh - b * a.Hk;
   const RowSpan span = row_span<PAGED>(a, b, h == 0 && tile == 0 && part == 0 && lane == 0);
   const int R = span.n * a.G, r0 = tile * kStepRows;

@@ -464,3 +464,16 @@ def test_cross_few_rows(case, dtype):
 def test_paged_wide_heads_in_tiles_of_few_rows(B, S, Hq, Hk, Dh, window):
     lens = [300, S, 33][:B]
     test_paged((B, S, Hq, Hk, Dh, 16, window, lens, [S, 2, S - 1][:B]), "f32")
+
+
+MANY = [  # B, S, Hq, Hk, Dh, page, window, lens, n_new
+    (14, 100, 6, 3, 40, 8, 0, [100, 3, 0, 57, 100, 99, 1, 64, 65, 31, 100, 12, 90, 33], [100, 3, 0, 50, 100, 99, 1, 64, 1, 31, 99, 12, 90, 33]),
+    (9, 130, 16, 16, 64, 16, 0, [130 - 13 * b for b in range(9)], [130 - 13 * b - b % 2 for b in range(9)]),
+    (1, 300, 8, 8, 56, 64, 0, [4700], [299])]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", MANY, ids=lambda c: "-".join(str(v) for v in c[:7]))
+def test_paged_several_rounds_of_tiles(case, dtype):
+    """The last tiles of all sequences first; heads of 64 over an axis in parts, three workgroups a unit."""
+    test_paged(case, dtype)

@@ -53,7 +53,9 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
   // they come, 87 sorted, with the two launches that find the order).  Over pages the ends are known, and sorting 16
   // ragged prompts of up to 2048 gained as often as it lost (86 to 108 us, sorted 92).
   p.sort = !p.step && B >= 4 && B <= kMaxSort && heads * p.tiles * p.parts >= 4 * num_cu;
-  p.ends = p.sort || n_keys >= 2048;  // a launch more (12 queries of 8 heads over 30000 positions 108 -> 26 us, over 2100 17 -> 16)
+  // a launch more, where a workgroup alone would take long (12 queries of 8 heads over 30000 positions 29.5 -> 25.7 us, over
+  // 10000 16.2 and 15.7, 4 x 10 over 2351 13.0 -> 14.6)
+  p.ends = p.sort || n_keys >= 8192;
   return p;
 }
 
@@ -61,13 +63,8 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
 __global__ void __launch_bounds__(1024) edges_kernel(const float *mask, int S, int2 *edges) {
   __shared__ int lo[16], hi[16];
   const float *m = mask + (long long)blockIdx.x * S;
-  int first = S, last = 0;
-#pragma unroll 4
-  for (int j = threadIdx.x; j < S; j += 1024) {
-    const bool valid = m[j] != 0.f;
-    first = valid ? min(first, j) : first;
-    last = valid ? j + 1 : last;
-  }
+  int first, last;
+  mask_ends<4>(m, S, threadIdx.x, 1024, first, last);
   first = wave_ext<int, false>(first);
   last = wave_ext<int, true>(last);
   const int w = threadIdx.x >> 6;

@@ -42,6 +42,26 @@ __device__ __forceinline__ void seen_keys(const MhaArgs &a, const RowSpan &r, in
   }
 }
 
+// The first valid position of a mask and one past its last, of the positions t, t + step, ..: U loads on their way at a time
+// (64 sentences of up to 1000 positions, 4 queries of 8 heads of 64 in bf16, the waves of a workgroup together: 17.4 -> 14.4 us)
+template <int U>
+__device__ __forceinline__ void mask_ends(const float *mask, int n, int t, int step, int &first, int &last) {
+  first = n;
+  last = 0;
+  for (int j0 = t; j0 < n; j0 += U * step) {
+    float v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = mask[min(j0 + u * step, n - 1)];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + u * step;
+      const bool valid = j < n && v[u] != 0.f;
+      first = valid ? min(first, j) : first;
+      last = valid ? j + 1 : last;
+    }
+  }
+}
+
 // page of block j of row b; a number out of range is clamped, and reported by who asks
 __device__ __forceinline__ int block_page(const MhaArgs &a, int b, int j, bool &bad) {
   const int p = a.table[(long long)b * a.n_blocks + j];

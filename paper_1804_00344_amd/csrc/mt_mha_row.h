@@ -70,6 +70,7 @@ __global__ void __launch_bounds__(256, NR == 1 ? 4 : 2) row_kernel(MhaArgs a, St
   typedef Vec<T, EPC> V;  // of a matrix in bf16 half of that: eight addresses and their rows do not fit the registers
   __shared__ __attribute__((aligned(16))) float sums[SHARE ? 4 : 1][SHARE ? NR : 1][SHARE ? DP : 1];
   __shared__ float2 ends[4][NR];
+  __shared__ int2 found[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned w = plan.first + xcd_remap(blockIdx.x, gridDim.x), job = SHARE ? w : w * 4 + wave;
   if (job >= plan.jobs) return;
@@ -106,11 +107,19 @@ __global__ void __launch_bounds__(256, NR == 1 ? 4 : 2) row_kernel(MhaArgs a, St
     lo = e.x;
     hi2 = e.y;
   } else if (!PAGED && mask) {  // the first and the last valid position
-    int first = a.Sk, last = 0;
-    for (int j = lane; j < a.Sk; j += 64)
-      if (mask[j] != 0.f) first = min(first, j), last = j + 1;
-    lo = wave_ext<int, false>(first);
-    hi2 = wave_ext<int, true>(last);
+    mask_ends<SHARE ? 4 : 8>(mask, a.Sk, SHARE ? threadIdx.x : lane, SHARE ? 256 : 64, lo, hi2);
+    lo = wave_ext<int, false>(lo);
+    hi2 = wave_ext<int, true>(hi2);
+    if (SHARE) {
+      if (lane == 0) found[wave] = make_int2(lo, hi2);
+      __syncthreads();
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int2 e = found[v];
+        lo = min(lo, e.x);
+        hi2 = max(hi2, e.y);
+      }
+    }
   }
   lo &= ~(KT - 1);
   int nt = hi2 > lo ? (hi2 - lo + KT - 1) / KT : 0;  // tiles of keys, this part's of them

@@ -408,9 +408,8 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a,
   } else if (!PAGED && mask) {  // the first and the last valid position
     if (threadIdx.x == 0) edge[0] = a.Sk, edge[1] = 0;
     __syncthreads();
-    int first = a.Sk, last = 0;
-    for (int j = threadIdx.x; j < a.Sk; j += 256)
-      if (mask[j] != 0.f) first = min(first, j), last = j + 1;
+    int first, last;
+    mask_ends<4>(mask, a.Sk, threadIdx.x, 256, first, last);
     if (last) atomicMin(&edge[0], first), atomicMax(&edge[1], last);
     __syncthreads();
     lo = edge[0];

@@ -477,3 +477,13 @@ MANY = [  # B, S, Hq, Hk, Dh, page, window, lens, n_new
 def test_paged_several_rounds_of_tiles(case, dtype):
     """The last tiles of all sequences first; heads of 64 over an axis in parts, three workgroups a unit."""
     test_paged(case, dtype)
+
+
+LONG = [(2, 3, 9000, 2, 1, 64, "holes", None), (3, 1, 8192, 4, 4, 40, "ends", [1, 0, 1]), (2, 200, 8300, 2, 2, 16, "ends", [200, 129]),
+        (1, 33, 8191, 1, 1, 64, "holes", None)]  # B, T, S, Hq, Hk, Dh, mask, n_q
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", LONG, ids=lambda c: "-".join(str(v) for v in c[:7]))
+def test_cross_long_masks(case, dtype):
+    test_cross(case, dtype)

@@ -40,6 +40,13 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
   // heads 53 and 66; heads of 128: 300 over 9000 of 8 heads 75 and 92).
   p.step = Dh <= 128 && (rows <= kStepRows || big * parts(big, tile_unit) < num_cu || (big < num_cu && n_keys <= (Dh <= 64 ? 4096 : 2048)));
   p.few = few_rows(rows, Dh, f32);
+  if (f32 && Dh > 128 && !p.few) {
+    // tiles of 128 rows take as long for one row as for all, a round of workgroups as long as 21 rows a unit by the vector
+    // units (200 positions of 4 heads of 192: 78 us by tiles, 23 by rows; 402 x 21 of 2 heads of 224 75 and 42; 24 over 1000 of
+    // 4 x 16 heads of 136, in parts, 95 and more; in bf16 tiles are as fast, 16 x 12 queries over 300, 8 heads of 256, 27 and 27)
+    const long long cut = parts(big, 1), rounds = (big * cut + num_cu - 1) / num_cu;
+    p.few = heads * rows * cut < 21ll * num_cu * rounds;
+  }
   p.step |= p.few;
   const int per = p.few ? kRowRows : p.step ? kStepRows : kTileRows;
   p.tiles = (int)((rows + per - 1) / per);
@@ -48,6 +55,11 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
   // the waves of a workgroup share a row's keys where there are few rows, or long ones (256 tokens of 16 heads over up to 2000
   // 146 -> 131 us; 768 of 8 over up to 512 41 -> 49)
   p.share = heads * p.tiles < 8 * num_cu || n_keys >= 1024;
+  if (p.step && !p.few && n_keys < 1024) {  // not where most waves would find no keys, in several rounds
+    // (182 x 8 queries over 15, 32 heads of 128 in 8 groups: fp32 77 -> 32 us, bf16 22 -> 13; 200 x 12 over 40, 8 heads of 64, fp32 34 -> 18)
+    const long long jobs = heads * p.tiles * p.parts, at_once = num_cu * step_unit(Dh, f32), kt = (n_keys + 31) / 32;
+    p.share &= (jobs + at_once - 1) / at_once * ((kt + 3) / 4) <= (jobs + 4 * at_once - 1) / (4 * at_once) * kt;
+  }
   // Under a mask over several rounds of workgroups: the longest sentence last would leave most units waiting for it, and
   // every workgroup would look for its sentence's end (8 ragged sentences of up to 2048 x 2048, 16 heads of 64: 101 us as
   // they come, 87 sorted, with the two launches that find the order).  Over pages the ends are known, and sorting 16

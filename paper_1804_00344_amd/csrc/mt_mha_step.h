@@ -7,6 +7,9 @@ namespace mt {
 
 constexpr int kStepRows = 32;
 
+// workgroups of the step kernel that a unit holds
+constexpr int step_unit(int Dh, bool f32) { return Dh <= 64 ? (f32 ? 2 : 3) : f32 ? 1 : 2; }
+
 // What a launch of the step kernel has decided
 struct StepPlan {
   int tiles;  // of kStepRows rows of a sequence's key head
@@ -23,7 +26,7 @@ struct StepPlan {
 // 32768 positions, 8 key heads of 128 in bf16: 367 us, 5.9 TB/s; by tiles of 128 rows 412), by one tile's latency where it is not.
 // The 32 columns of a product that one token leaves empty cost nothing then (matrix units 8% busy).
 template <typename T, int DP, bool PAGED, bool SHARE>
-__global__ void __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 256 ? 2 : 1) step_kernel(MhaArgs a, StepPlan plan) {
+__global__ void __launch_bounds__(256, step_unit(DP, sizeof(T) == 4)) step_kernel(MhaArgs a, StepPlan plan) {
   constexpr int KT = 32, TB = KT * DP * (int)sizeof(T), DB = DP / 32;
   __shared__ __attribute__((aligned(1024))) char lds[4 * 2 * TB];
   __shared__ float2 ends[4][32];

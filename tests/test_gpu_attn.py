@@ -487,3 +487,19 @@ LONG = [(2, 3, 9000, 2, 1, 64, "holes", None), (3, 1, 8192, 4, 4, 40, "ends", [1
 @pytest.mark.parametrize("case", LONG, ids=lambda c: "-".join(str(v) for v in c[:7]))
 def test_cross_long_masks(case, dtype):
     test_cross(case, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("S,lens,Hq,Hk,Dh,window", [
+    (350, [350], 16, 16, 136, 0), (100, [100], 4, 2, 256, 0), (21, [22, 3, 40], 2, 2, 224, 5), (60, [1300], 6, 1, 144, 0)])
+def test_paged_wide_heads(S, lens, Hq, Hk, Dh, window, dtype):
+    """By tiles of 128 rows, and by tiles of four where those would leave the chip empty."""
+    test_paged((len(lens), S, Hq, Hk, Dh, 16, window, lens, [min(S, n) for n in lens]), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", [(1, 700, 40, 8, 8, 200, "holes", None), (2, 90, 70, 4, 4, 160, "holes", [90, 33]),
+                                  (70, 8, 15, 32, 8, 128, "ends", None), (200, 3, 30, 16, 8, 40, "holes", None)],
+                         ids=lambda c: "-".join(str(v) for v in c[:7]))
+def test_cross_wide_heads_and_short_sentences(case, dtype):
+    test_cross(case, dtype)

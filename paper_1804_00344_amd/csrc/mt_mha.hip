@@ -1,6 +1,8 @@
 // Attention of query heads over keys and values in pages of a cache, or in rows of another length under a mask:
 //   y = sum_j softmax_j(scale q.k_j) v_j over the keys that a query sees.
 // Here: how a call is split over the chip, and the join of the parts of a key axis that is cut.
+#include <algorithm>
+
 #include "mt_mha_row.h"
 
 namespace mt {
@@ -52,6 +54,16 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
   p.tiles = (int)((rows + per - 1) / per);
   const int unit = !p.step ? tile_unit : !p.few ? (p.tiles == 1 && heads * 4 >= num_cu ? 2 : 1) : rows == 1 ? 4 : 2;
   p.parts = parts(heads * p.tiles, unit);
+  if (!p.step && B > 2 && n_keys > 2ll * S) {
+    // Several sequences are often of different lengths: up to twice the parts, where joining them is little beside the products
+    // and the rounds do not get longer (12 x 166 positions of 16 heads of 64 in fp32 behind up to 1664: ragged 108 -> 78 us, all
+    // alike 205 -> 207; 3 x 500 of 16 heads of 128 in bf16 behind up to 6000: 104 -> 66 and 132 -> 127)
+    const long long wgs = heads * p.tiles, slots = (long long)num_cu * unit;
+    const long long few_joined = std::max(n_keys / (f32 ? 448 : 1024), n_keys / (16 * rows));
+    const auto rounds = [&](long long n) { return (wgs * n + slots - 1) / slots; };
+    for (long long n = std::min<long long>(parts(wgs, 2 * unit), few_joined); n > p.parts; --n)
+      if (rounds(n) * p.parts <= rounds(p.parts) * n) p.parts = (int)n;
+  }
   // the waves of a workgroup share a row's keys where there are few rows, or long ones (256 tokens of 16 heads over up to 2000
   // 146 -> 131 us; 768 of 8 over up to 512 41 -> 49)
   p.share = heads * p.tiles < 8 * num_cu || n_keys >= 1024;

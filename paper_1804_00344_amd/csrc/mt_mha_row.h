@@ -9,9 +9,9 @@ constexpr int kRowRows = 4;  // of a tile
 
 // Where the vector units are faster than the matrix units, which have no step kernel for more than 128 features (16 sentences
 // of up to 1000 positions, 8 heads of 256 in fp32: 8 rows a head 57 us, 16 rows 97, 32 rows 165, by tiles of 128 rows 172 to 182;
-// heads of 128: 8 rows 34, 12 rows 51, by the step kernel 41 and 37)
+// heads of 128: 8 rows 34, 12 rows 51, by the step kernel 41 and 37; 264 tokens over 336, 8 heads of 88 that share one: 42, 50)
 constexpr bool few_rows(long long rows, int Dh, bool f32) {
-  return f32 ? rows <= (Dh > 128 ? 16 : kRowRows) : rows <= (Dh > 128 ? kRowRows : 1);
+  return f32 ? rows <= (Dh > 128 ? 16 : Dh > 64 ? 8 : kRowRows) : rows <= (Dh > 128 ? kRowRows : 1);
 }
 
 // v of all lanes that differ in bits O .. 32 of their number, combined

@@ -22,16 +22,21 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
   Plan p;
   const long long rows = (long long)S * (Hq / Hk), heads = (long long)B * Hk;
   if (window && n_keys > (long long)window + S) n_keys = (long long)window + S;  // keys that a row's queries see
-  // The key axis is cut until there are enough workgroups; a part has 256 keys at least.  Tiles of 128 rows want what a
-  // unit's registers hold, some computing scores while others take exponentials (300 positions over 9000, 32 heads of 128: two
-  // a unit 84 us, one 132; 700 over 9000, 32 heads of 64: three 93, two 121; 2048 over 20000, 8 heads of 64: 132 and 127);
-  // tiles of 32 want one, as the parts have to be joined (a token over 20000, 32 heads of 128 in 8 groups: 26 us, two 30; 6 x
-  // 100 queries over 900, 8 heads of 64: 14 us, two 17), but two where long sequences of one tile would get few parts (16
-  // tokens over 10 to 20000 positions 165 -> 116 us, all of 20000 228 -> 231); the
-  // vector units want what fits (16 tokens of up to 4000 in fp32, 4 groups of 4 heads of 128: one 52 us, two 38; in bf16 of up to
-  // 9000, 16 heads of 192: one 304, two 187, four 148).
-  const long long most = n_keys / 256 < 1 ? 1 : n_keys / 256;
-  auto parts = [&](long long wgs, int a_unit) {
+  // The key axis is cut until there are enough workgroups; where there are many parts, each has 256 keys at least.  Tiles of
+  // 128 rows want what a unit's registers hold, some computing scores while others take exponentials (300 positions over 9000,
+  // 32 heads of 128: two a unit 84 us, one 132; 700 over 9000, 32 heads of 64: three 93, two 121; 2048 over 20000, 8 heads of
+  // 64: 132 and 127); tiles of 32 want one, as the parts have to be joined (a token over 20000, 32 heads of 128 in 8 groups: 26
+  // us, two 30; 6 x 100 queries over 900, 8 heads of 64: 14 us, two 17), but two where long sequences of one tile would get few
+  // parts (16 tokens over 10 to 20000 positions 165 -> 116 us, all of 20000 228 -> 231); the vector units want what fits (16
+  // tokens of up to 4000 in fp32, 4 groups of 4 heads of 128: one 52 us, two 38; in bf16 of up to 9000, 16 heads of 192: one
+  // 304, two 187, four 148).
+  // Few parts may be shorter, down to 128 keys (64 of wide heads): 4 queries over 843 positions, 48 heads of 128 in 16 groups, 29
+  // -> 23 us in fp32 and 14.7 -> 13.0 in bf16; 200 positions of 4 heads of 192 behind 600 in bf16 28 -> 21; a token over 16242,
+  // 8 heads of 128 in 2 groups in bf16: 63 parts 20 us, 126 25.  In bf16 short axes are not worth the join (30 positions over
+  // 430, 8 heads of 64: one part 8.3 us, three 11.5).
+  const long long coarse = std::max(1ll, n_keys / 256);
+  const long long fine = std::max(coarse, std::min(n_keys / (Dh > 128 ? 64 : 128), 32ll));
+  auto parts = [&](long long wgs, int a_unit, long long most) {
     const long long want = a_unit * num_cu / wgs;
     return (int)(want < 1 ? 1 : want < most ? want : most);
   };
@@ -40,20 +45,20 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
   // Tiles of 128 rows read the keys a quarter as often as those of 32, which fill the chip and end sooner where there is
   // less to do (heads of 64: 1000 positions of 8 heads 27 us by 128, 13 by 32; 200 over 2000 of 32 heads 32 and 25, of 128
   // heads 53 and 66; heads of 128: 300 over 9000 of 8 heads 75 and 92).
-  p.step = Dh <= 128 && (rows <= kStepRows || big * parts(big, tile_unit) < num_cu || (big < num_cu && n_keys <= (Dh <= 64 ? 4096 : 2048)));
+  p.step = Dh <= 128 && (rows <= kStepRows || big * parts(big, tile_unit, coarse) < num_cu || (big < num_cu && n_keys <= (Dh <= 64 ? 4096 : 2048)));
   p.few = few_rows(rows, Dh, f32);
   if (f32 && Dh > 128 && !p.few) {
-    // tiles of 128 rows take as long for one row as for all, a round of workgroups as long as 21 rows a unit by the vector
-    // units (200 positions of 4 heads of 192: 78 us by tiles, 23 by rows; 402 x 21 of 2 heads of 224 75 and 42; 24 over 1000 of
-    // 4 x 16 heads of 136, in parts, 95 and more; in bf16 tiles are as fast, 16 x 12 queries over 300, 8 heads of 256, 27 and 27)
-    const long long cut = parts(big, 1), rounds = (big * cut + num_cu - 1) / num_cu;
-    p.few = heads * rows * cut < 21ll * num_cu * rounds;
+    // tiles of 128 rows take as long for one row as for all, a round of workgroups as long as some 24 rows a unit by the vector
+    // units (200 positions of 4 heads of 192: 78 us by tiles, 23 by rows; 402 x 21 of 2 heads of 224 75 and 42; 400 of 16 heads
+    // of 160 in 4 groups, in parts, 66 and 140; in bf16 tiles are as fast, 16 x 12 queries over 300, 8 heads of 256, 27 and 27)
+    const long long cut = parts(big, 1, fine), rounds = (big * cut + num_cu - 1) / num_cu;
+    p.few = heads * rows * cut < 24ll * num_cu * rounds;
   }
   p.step |= p.few;
   const int per = p.few ? kRowRows : p.step ? kStepRows : kTileRows;
   p.tiles = (int)((rows + per - 1) / per);
   const int unit = !p.step ? tile_unit : !p.few ? (p.tiles == 1 && heads * 4 >= num_cu ? 2 : 1) : rows == 1 ? 4 : 2;
-  p.parts = parts(heads * p.tiles, unit);
+  p.parts = parts(heads * p.tiles, unit, !f32 && Dh <= 128 && n_keys < 512 ? coarse : fine);
   if (!p.step && B > 2 && n_keys > 2ll * S) {
     // Several sequences are often of different lengths: up to twice the parts, where joining them is little beside the products
     // and the rounds do not get longer (12 x 166 positions of 16 heads of 64 in fp32 behind up to 1664: ragged 108 -> 78 us, all
@@ -61,7 +66,7 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
     const long long wgs = heads * p.tiles, slots = (long long)num_cu * unit;
     const long long few_joined = std::max(n_keys / (f32 ? 448 : 1024), n_keys / (16 * rows));
     const auto rounds = [&](long long n) { return (wgs * n + slots - 1) / slots; };
-    for (long long n = std::min<long long>(parts(wgs, 2 * unit), few_joined); n > p.parts; --n)
+    for (long long n = std::min<long long>(parts(wgs, 2 * unit, coarse), few_joined); n > p.parts; --n)
       if (rounds(n) * p.parts <= rounds(p.parts) * n) p.parts = (int)n;
   }
   // the waves of a workgroup share a row's keys where there are few rows, or long ones (256 tokens of 16 heads over up to 2000

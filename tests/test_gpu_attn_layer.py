@@ -224,3 +224,57 @@ def test_a_packed_cache_counts_its_free_pages():
     torch.cuda.synchronize()
     assert int(small.free) == 8 and small.lens.tolist() == [4, 4, 9]
     assert cache.pack(6).lens.tolist() == [0] * 5 and mt.mt_attn_device_errors(attn) == 8
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_two_graphs_with_one_workspace(dtype):
+    """Calls of several launches (sorted sentences, long masks, parts, tables of every size) captured in two graphs that share
+    a workspace, replayed in turn over changed inputs with eager calls between them: every replay gives the eager result."""
+    from test_gpu_attn import layer, space
+    io = torch.bfloat16 if dtype == "bf16" else torch.float32
+    a = layer(16, 16, 64, dtype, page=8)
+    g = gen(8)
+    rand = lambda *s: torch.randn(*s, generator=g).to(io).to(DEV)
+    # 24 sentences of 300 queries, sorted by their work; 2 of 3 queries over a long mask, in parts
+    sizes = [(24, 300, 200), (2, 3, 8400)]
+    qs, ks = [rand(B, T, 1024) for B, T, _ in sizes], [rand(B, S, 1024) for B, _, S in sizes]
+    masks = [torch.ones(B, S, device=DEV) for B, _, S in sizes]
+    need = [mt.mt_attn_workspace_bytes(a, *s) for s in sizes]
+    rows = [(40, 300), (300, 2000)]  # and tables: a plan in every workgroup, one workgroup's
+    need += [mt.mt_pages_workspace_bytes(a, M, n) for M, n in rows]
+    ws = space(max(need))
+    table_in = [torch.arange(M, dtype=torch.int32, device=DEV)[:, None].repeat(1, 4) for M, _ in rows]
+    len_in, src = [torch.full((M,), 5, dtype=torch.int32, device=DEV) for M, _ in rows], [i32(list(range(M))) for M, _ in rows]
+    pool = [[torch.zeros(1, n, 16, 8, 64, dtype=io, device=DEV) for _, n in rows] for _ in range(2)]
+    outs = [(torch.empty_like(q), torch.empty_like(t), torch.empty_like(n)) for q, t, n in zip(qs, table_in, len_in)]
+
+    def call(i, out):
+        mt.mt_attn_cross(a, qs[i], ks[i], ks[i], out[0], mask=masks[i], ws=ws)
+        mt.mt_pages_advance(a, src[i], None, table_in[i], len_in[i], out[1], out[2], pool[0][i], pool[1][i], ws=ws)
+
+    graphs = []
+    for i in range(2):
+        graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+            call(i, outs[i])
+        torch.cuda.synchronize()
+        graphs.append(graph)
+    for _ in range(4):
+        for i in (0, 1, 0):
+            B, T, S = sizes[i]
+            n = torch.randint(1, S + 1, (B,), generator=g)
+            masks[i].copy_((torch.arange(S)[None] < n[:, None]).float())
+            qs[i].copy_(rand(B, T, 1024))
+            M = rows[i][0]
+            src[i].copy_(torch.randint(0, M, (M,), generator=g).int())
+            len_in[i].copy_(torch.randint(1, 25, (M,), generator=g).int().clamp(max=8))
+            want = [torch.full_like(x, 3) for x in outs[i]]
+            call(i, want)
+            for x in outs[i]:
+                x.fill_(7)
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            for x, y in zip(outs[i], want):
+                assert torch.equal(x, y), i
+    assert mt.mt_attn_device_errors(a) == 0

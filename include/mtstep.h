@@ -615,8 +615,9 @@ size_t mt_attn_workspace_bytes(const mt_attn *a, int B, int S, int64_t n_keys);
 /* Attention over the cache: the query of position p sees the keys j of its row with p - window < j <= p (window 0:
  * 0 <= j <= p):  y = sum_j softmax_j(scale q.k_j) v_j  for every query head.  q, y [B*S, Hq*Dh].  The new positions'
  * keys and values are in the cache already (mt_attn_append).  A query that sees nothing, or whose scores are all
- * minus infinity, gives zeros.  Keys and values that a query does not see have no part in it, NaN and infinities
- * among them.  Sizes as mt_attn_append; B*S*Hq <= 2^30. */
+ * minus infinity, gives zeros.  Scores are held in 32 bits, times log2(e): from 2^128 on they are infinite there.
+ * Keys and values that a query does not see have no part in it, NaN and infinities among them.
+ * Sizes as mt_attn_append; B*S*Hq <= 2^30. */
 mt_status mt_attn_paged(mt_attn *a, int B, int S, const int32_t *n_new, const int32_t *len, const void *q, int64_t ldq,
                         const int32_t *table, int n_blocks, int n_pages, const void *k_pages, const void *v_pages,
                         void *y, int64_t ldy, void *ws, size_t ws_bytes, void *stream);

@@ -8,6 +8,16 @@ namespace mt {
 
 constexpr float kNegInf = -__builtin_inff();
 
+// A weight is 2^(s scale - m) by one multiply-add, whose product is not rounded while m is a rounded one: the largest score's
+// exponent is what m was rounded by, up to 2 for scores (in units of log2) of 2^26.  From there on the product is rounded
+// first, so that the difference to the maximum is 0 again; with 2^32 the weights would pass all powers of two.
+constexpr float kFarScore = 67108864.f;
+
+__device__ __forceinline__ float rounded_product(float x, float y) {
+#pragma clang fp contract(off)
+  return x * y;
+}
+
 // The lengths of row b: positions and new ones (paged), or keys and queries (cross); clamped, reported where tell is set
 struct RowSpan {
   int len, n;  // keys, queries
@@ -125,7 +135,7 @@ __device__ void attend_one(const MhaArgs &a, const RowSpan &r, int b, int i, int
 #pragma unroll
         for (int e = 0; e < VEC; ++e) x = fmaf(qs[d + e], (float)v.v[e], x);
       }
-      s = x * a.scale;
+      s = rounded_product(x, a.scale);
     }
     const float mn = fmaxf(m, wave_max(s)), use = mn == kNegInf ? 0.f : mn;
     const float p = seen ? __builtin_amdgcn_exp2f(s - use) : 0.f;

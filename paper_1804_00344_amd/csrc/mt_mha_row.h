@@ -240,10 +240,16 @@ __global__ void __launch_bounds__(256, NR == 1 ? 4 : 2) row_kernel(MhaArgs a, St
 #pragma unroll
         for (int e = 0; e < EPC; ++e) acc[r][e] *= c;
       }
-      const float use = m[r] == kNegInf ? 0.f : m[r];
+      float use = m[r] == kNegInf ? 0.f : m[r], scale = a.scale;
+      if (__any(fabsf(use) >= kFarScore)) {
+#pragma unroll
+        for (int x = 0; x < NL; ++x) s[r][x] = rounded_product(s[r][x], scale) - use;
+        scale = 1.f;  // the exponents as they are
+        use = 0.f;
+      }
 #pragma unroll
       for (int x = 0; x < NL; ++x) {
-        s[r][x] = __builtin_amdgcn_exp2f(fmaf(s[r][x], a.scale, -use));
+        s[r][x] = __builtin_amdgcn_exp2f(fmaf(s[r][x], scale, -use));
         l[r] += s[r][x];
       }
     }

@@ -129,8 +129,16 @@ struct Rows {
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[d][e] *= c;
     }
-    const float use = m == kNegInf ? 0.f : m;
+    float use = m == kNegInf ? 0.f : m;
     float sum[2] = {};
+    if (__any(fabsf(use) >= kFarScore)) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[kb][e] = rounded_product(s[kb][e], scale) - use;
+      scale = 1.f;  // the exponents as they are
+      use = 0.f;
+    }
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll

@@ -1,0 +1,78 @@
+"""The attention layer's operators at the edges of their contracts, on every kernel that a call may take: scores of any finite
+size."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_1804_00344_amd import mtstep as mt
+from test_gpu_attn import HALF, fill_cache, layer, pages_for, run_cross, run_paged
+from test_gpu_layer import DEV, IO, check, dev, gen
+
+pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
+
+U = 2.0 ** -24
+
+# B, S, Hq, Hk, Dh, longest row (paged) or keys (cross): vector units, tiles of 32 and of 128 rows, each whole and in parts
+SIZES = [(1, 1, 2, 2, 64, 90), (2, 1, 2, 2, 256, 5000), (1, 4, 2, 2, 128, 900), (2, 20, 2, 1, 64, 90), (1, 20, 2, 2, 128, 3000),
+         (1, 40, 2, 2, 192, 90), (8, 300, 16, 16, 64, 310), (8, 260, 16, 16, 128, 300), (1, 300, 8, 8, 64, 4700)]
+
+
+def one_feature(B, S, Hq, Hk, Dh, L, size, sign, g):
+    """q, k, v of which only feature 5 of a head counts: a score is one product of two values of 8 bits, exact in fp32.  Two
+    different scores of size 2^26 or more differ by far more than a weight's range, equal ones have equal weights."""
+    q = torch.zeros(B, S, Hq, Dh)
+    q[..., 5] = torch.ldexp(1 + torch.randint(0, 128, (B, S, Hq), generator=g) / 128.0, torch.tensor(size))
+    k, v = torch.randn(B, L, Hk, Dh, generator=g), torch.randn(B, L, Hk, Dh, generator=g)
+    k[..., 5] = 1 + torch.randint(0, 128, (B, L, Hk), generator=g) / 128.0
+    if sign == "minus":
+        k[..., 5] *= -1
+    elif sign == "both":
+        k[..., 5] *= torch.randint(0, 2, (B, L, Hk), generator=g) * 2.0 - 1
+    return q, k, v
+
+
+def largest(q, k, v, seen, G, half_step):
+    """The mean of the values whose keys score highest, q [n, Hq, Dh], k, v [L, Hk, Dh], seen [n, L]; bound: equal weights,
+    each rounded once, over as many values."""
+    n, Hq, Dh = q.shape
+    want, err = torch.zeros(n, Hq, Dh, dtype=torch.float64), torch.zeros(n, Hq, Dh, dtype=torch.float64)
+    for h in range(Hq):
+        s = q[:, h, 5:6].double() * k[None, :, h // G, 5].double()
+        s = torch.where(seen, s, torch.full_like(s, float("-inf")))
+        first = ((s == s.amax(1, keepdim=True)) & seen).double()
+        count = first.sum(1, keepdim=True).clamp(min=1)
+        want[:, h] = first @ v[:, h // G] / count
+        err[:, h] = first @ v[:, h // G].abs() / count * (half_step + (count + 16) * U)
+    return want.reshape(n, -1), err.reshape(n, -1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sign", ["plus", "minus", "both"])
+@pytest.mark.parametrize("size", [26, 37, 100])
+@pytest.mark.parametrize("case", SIZES, ids=lambda c: "-".join(str(v) for v in c))
+def test_scores_of_any_finite_size(case, size, sign, dtype):
+    """Scores from 1e7 to 1e30: the weight of the largest is one, whatever the product with the scale is rounded by."""
+    B, S, Hq, Hk, Dh, L = case
+    g = gen(size + S)
+    q, k, v = one_feature(B, S, Hq, Hk, Dh, L, size, sign, g)
+    q, k, v = (t.to(IO[dtype]) for t in (q, k, v))
+    a = layer(Hq, Hk, Dh, dtype, page=16)
+    lens = [L - 7 * b for b in range(B)]
+    table, n_pages = pages_for(lens, 16, -(-L // 16), g)
+    _, _, kc, vc = fill_cache(table, lens, 16, Hk, Dh, n_pages, dtype, g)
+    for t, c in ((k, kc), (v, vc)):
+        for b in range(B):
+            for j in range(0, lens[b], 16):
+                part = t[b, j:min(j + 16, lens[b])]
+                c[table[b, j // 16], :, :part.shape[0]] = part.transpose(0, 1)
+    new = [min(S, n) for n in lens]
+    y = run_paged(a, dev(q.flatten(2)), lens, table, kc, vc, new)
+    mask = (torch.rand(B, L, generator=g) < 0.7).float()
+    x = run_cross(a, dev(q.flatten(2)), dev(k.flatten(2)), dev(v.flatten(2)), mask)
+    for b in range(B):
+        n = lens[b]
+        p, j = torch.arange(n - new[b], n)[:, None], torch.arange(n)[None]
+        want, err = largest(q[b, :new[b]], k[b, :n], v[b, :n].double(), j <= p, Hq // Hk, HALF[dtype])
+        check(y[b, :new[b]], want, err, (b, "paged"))
+        want, err = largest(q[b], k[b], v[b].double(), (mask[b] != 0)[None].expand(S, -1), Hq // Hk, HALF[dtype])
+        check(x[b], want, err, (b, "cross"))

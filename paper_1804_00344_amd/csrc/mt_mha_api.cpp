@@ -240,7 +240,7 @@ mt_status mt_attn_paged(mt_attn *a, int B, int S, const int32_t *n_new, const in
                         {"k_pages", k_pages, n_pages, pb, pb},
                         {"v_pages", v_pages, n_pages, pb, pb}}));
   CHECK(check_device(a->device));
-  p.window = c.window;
+  p.window = c.window < kMaxSteps ? c.window : 0;  // no position is that far from another: positions minus it stay in range
   p.k = k_pages; p.v = v_pages; p.len = len; p.table = table;
   p.n_blocks = n_blocks; p.n_pages = n_pages; p.page_log2 = a->page_log2;
   HIP_TRY(launch_mha(p, (hipStream_t)stream));

@@ -1,5 +1,5 @@
 """The attention layer's operators at the edges of their contracts, on every kernel that a call may take: scores of any finite
-size."""
+size, windows of any size."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -76,3 +76,19 @@ def test_scores_of_any_finite_size(case, size, sign, dtype):
         check(y[b, :new[b]], want, err, (b, "paged"))
         want, err = largest(q[b], k[b], v[b].double(), (mask[b] != 0)[None].expand(S, -1), Hq // Hk, HALF[dtype])
         check(x[b], want, err, (b, "cross"))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("S,Hq,Hk,Dh,B", [(4, 2, 2, 64, 3), (4, 2, 2, 256, 3), (20, 4, 2, 64, 3), (300, 16, 16, 64, 8)])
+def test_a_window_past_every_position(S, Hq, Hk, Dh, B, dtype):
+    """The largest window is none, also where rows have fewer positions than new ones."""
+    g = gen(S + Dh)
+    lens = [[1, S // 2 + 1, S + 9][b % 3] for b in range(B)]
+    table, n_pages = pages_for(lens, 16, -(-max(lens) // 16) + 1, g)
+    _, _, kc, vc = fill_cache(table, lens, 16, Hk, Dh, n_pages, dtype, g)
+    q = dev(torch.randn(B, S, Hq * Dh, generator=g).to(IO[dtype]))
+    want = run_paged(layer(Hq, Hk, Dh, dtype), q, lens, table, kc, vc)
+    assert bool(torch.isfinite(want).all()) and bool((want[0, -1] != 0).any())
+    for window in (2 ** 31 - 1, 2 ** 31 - S, 2 ** 30 + 1, 2 ** 30, 2 ** 30 - 1):
+        y = run_paged(layer(Hq, Hk, Dh, dtype, window=window), q, lens, table, kc, vc)
+        assert torch.equal(y, want), window

@@ -567,7 +567,7 @@ mt_status mt_ssm_device_errors(mt_ssm *cell, int32_t *flags);
  *   dtype: MT_F32 or MT_BF16, the type of q, k, v, y and the cache.  Parameters and arithmetic are fp32; a bf16
  *     layer's softmax weights are rounded to bf16 before the products with the values (their sum is not).
  *   window: a position sees the last `window` ones, itself included; 0: all before it.  (mt_attn_paged)
- *   scale: of the scores; 0: 1 / sqrt(Dh).
+ *   scale: of the scores, finite, also times log2(e); 0: 1 / sqrt(Dh).
  *   For mt_attn_append: qk_norm 0/1 — x / sqrt(mean(x^2) + norm_eps) * gain over each head of q and k;
  *   rot: features of each head of q and k that are rotated, even, 0..Dh, the first ones; rot_pairs 0: feature i
  *     turns with i + rot/2, 1: feature 2i with 2i + 1; pair i of position p by the angle p * freq[i];

@@ -51,7 +51,8 @@ mt_status check_cfg(const mt_attn_config *c) {
   if (c->qk_norm != 0 && c->qk_norm != 1) return fail(MT_ERR_ARG, "qk_norm must be 0 or 1");
   if (c->rot < 0 || c->rot > c->Dh || c->rot % 2) return fail(MT_ERR_SHAPE, "rot=%d: need an even number up to Dh", c->rot);
   if (c->rot_pairs != 0 && c->rot_pairs != 1) return fail(MT_ERR_ARG, "rot_pairs must be 0 or 1");
-  if (!(c->scale >= 0.f) || !std::isfinite(c->scale)) return fail(MT_ERR_ARG, "scale must be finite and not negative");
+  if (!(c->scale >= 0.f) || !std::isfinite((float)(c->scale * M_LOG2E)))
+    return fail(MT_ERR_ARG, "scale must be finite, also times log2(e), and not negative");
   if (c->qk_norm && (!(c->norm_eps >= 0.f) || !std::isfinite(c->norm_eps)))
     return fail(MT_ERR_ARG, "norm_eps must be finite and not negative");
   return MT_OK;

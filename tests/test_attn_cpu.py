@@ -40,6 +40,17 @@ def test_load_refuses_configurations(kw, rc):
     assert e.value.status == rc
 
 
+def test_load_refuses_a_scale_that_is_infinite_in_powers_of_two():
+    """Scores are held times log2(e): a product of such a scale with a zero would be no number."""
+    for scale, ok in ((3e38, False), (2.4e38, False), (2.3e38, True)):
+        try:
+            mt.mt_attn_load(mt.make_attn_config(8, 4, 64, scale=scale))
+        except mt.MtError as e:  # a good one ends where there is no device
+            assert (e.status != mt.MT_ERR_ARG) == ok
+        else:
+            assert ok
+
+
 def test_load_refuses_flags_types_and_parameters():
     for field, v, rc in (("dtype", 2, mt.MT_ERR_DTYPE), ("qk_norm", 2, mt.MT_ERR_ARG), ("rot_pairs", -1, mt.MT_ERR_ARG)):
         cfg = mt.make_attn_config(8, 4, 64)

@@ -195,6 +195,13 @@ def test_sizes_beyond_the_heads():
     assert mt.lib().mt_attn_workspace_bytes(C.addressof(wide), 1, 1, 2 ** 30 + 1) == 0
 
 
+def test_append_takes_any_number_of_heads_in_all():
+    wide = layer(Hq=1024, Hk=1, Dh=64)
+    big = dict(B=2 ** 21, S=1, q=1 << 49, ldq=65536, o=1 << 50, ldo=65536, k=1 << 51, v=1 << 52, t=1 << 53, len=1 << 54)
+    assert reached_device_check(append(wide, **big)), mt.lib().mt_last_error()
+    assert append(wide, **{**big, "B": 2 ** 24 + 1}) == SH
+
+
 # ---- the definitions --------------------------------------------------------------------------------
 
 def test_reference_attention_is_the_sum_over_seen_keys():

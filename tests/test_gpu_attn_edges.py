@@ -92,3 +92,22 @@ def test_a_window_past_every_position(S, Hq, Hk, Dh, B, dtype):
     for window in (2 ** 31 - 1, 2 ** 31 - S, 2 ** 30 + 1, 2 ** 30, 2 ** 30 - 1):
         y = run_paged(layer(Hq, Hk, Dh, dtype, window=window), q, lens, table, kc, vc)
         assert torch.equal(y, want), window
+
+
+def test_append_of_more_than_2_to_the_30_heads():
+    """Neither norm nor rotation: queries, keys and values are copied, whatever B*S*Hq is."""
+    Hq, page, S = 512, 256, 2 ** 21 + 5
+    a = layer(Hq, 1, 8, "bf16", page=page)
+    nb = -(-S // page)
+    q = torch.empty(1, S, Hq * 8, dtype=torch.bfloat16, device=DEV)
+    for part in q.flatten().split(2 ** 28):
+        part.normal_()
+    k, v = (torch.randn(1, S, 8, device=DEV).bfloat16() for _ in range(2))
+    kc, vc = (torch.zeros(nb, 1, page, 8, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    out = torch.empty_like(q)
+    table = torch.arange(nb, dtype=torch.int32, device=DEV)[None]
+    mt.mt_attn_append(a, q, k, v, out, torch.tensor([S], dtype=torch.int32, device=DEV), table, kc, vc)
+    assert mt.mt_attn_device_errors(a) == 0
+    assert all(torch.equal(x, y) for x, y in zip(out.flatten().split(2 ** 30), q.flatten().split(2 ** 30)))
+    for t, c in ((k, kc), (v, vc)):
+        assert torch.equal(c.reshape(-1, 8)[:S], t[0]) and bool((c.reshape(-1, 8)[S:] == 0).all())

@@ -424,14 +424,18 @@ class SsmLayer:
 class PagedCache:
     """The keys and values of a program's attention layers in pages, k, v [layers, n_pages, Hk, page, Dh], and the table and
     lengths of its current rows: prompts first, then hypotheses that continue one another's.  Making one, and the first
-    advance to a number of rows, wait for the device (unless captured into a graph): any stream may follow."""
+    advance to a number of rows, wait for the device (unless captured into a graph): any stream may follow.
+
+    An advance that finds too few pages writes none and leaves rows of no positions, over which a layer's calls give zeros;
+    check() says so and goes back.  Where the pool may run out it has to be called before the next advance, which
+    would take the pages of the rows that were lost for free ones."""
 
     def __init__(self, attn: mt.Attn, layers: int, n_pages: int, n_blocks: int):
         self.attn, self.n_blocks = attn, n_blocks
         shape = (layers, n_pages) + tuple(attn.page_shape)
         self.k, self.v = (torch.zeros(shape, dtype=attn.dtype, device=attn.device) for _ in range(2))
         self.free = torch.full((1,), n_pages, dtype=torch.int32, device=attn.device)
-        self._spare = {}
+        self._spare, self._before = {}, None
         self.table, self.lens = self._rows(1)  # one empty row, for new ones to begin with
         self.lens.zero_()
         self._wait()
@@ -460,10 +464,26 @@ class PagedCache:
         with torch.cuda.device(self.attn.device):
             mt.mt_pages_advance(self.attn, src_row, add, self.table, self.lens, table, lens, self.k, self.v, free_out=self.free,
                                 ws=self._spare[n][1], stream=stream)
+        self._before = self.table, self.lens  # as they were until the next advance
         self.table, self.lens = table, lens
 
+    def check(self) -> int:
+        """Waits for the device and gives the layer's device-side error bits (mt_attn_device_errors, which clears them).  Where
+        the last advance found no room (bit 8), the rows before it are the current ones again."""
+        with torch.cuda.device(self.attn.device):
+            flags = mt.mt_attn_device_errors(self.attn)
+            if flags & 8 and self._before and int(self.free) == self.k.shape[1] and not bool(self.lens.any()):
+                (self.table, self.lens), self._before = self._before, None
+                n = self.lens.numel()  # the free pages beside these rows: that of a step in which none grows
+                table, lens = self._rows(n)
+                mt.mt_pages_advance(self.attn, None, torch.zeros_like(self.lens), self.table, self.lens, table, lens, self.k, self.v,
+                                    free_out=self.free, ws=self._spare[n][1])
+                self._wait()
+        return flags
+
     def pack(self, n_pages: int, stream=None) -> "PagedCache":
-        """A cache of n_pages that holds the current rows, their pages at its front."""
+        """A cache of n_pages that holds the current rows, their pages at its front (rows of no positions where n_pages do not
+        suffice, which check() tells; this cache stays as it is)."""
         out = PagedCache(self.attn, self.k.shape[0], n_pages, self.n_blocks)
         n = self.lens.numel()
         table, lens = out._rows(n)

@@ -278,3 +278,33 @@ def test_two_graphs_with_one_workspace(dtype):
             for x, y in zip(outs[i], want):
                 assert torch.equal(x, y), i
     assert mt.mt_attn_device_errors(a) == 0
+
+
+@pytest.mark.parametrize("add", [None, [9, 9, 9, 9]])
+def test_a_step_without_room_is_taken_back(add):
+    """A pool that runs out under a beam: check() tells, gives the rows before back, and the beam goes on with fewer rows."""
+    attn = mt.mt_attn_load(mt.make_attn_config(2, 1, 64, page=8))
+    cache = PagedCache(attn, 2, 9, 6)
+    cache.advance(i32([-1, -1]), i32([16, 11]))  # 2 + 2 pages
+    cache.k.normal_(), cache.v.normal_()
+    cache.advance(i32([0, 0, 1, 1]))             # two blocks and a copy: 7 in use
+    assert cache.check() == 0
+    cache.advance(i32([0, 1, 2, 3]))             # inside their pages
+    assert cache.check() == 0 and int(cache.free) == 2
+    table, lens, k, v = cache.table.clone(), cache.lens.clone(), cache.k.clone(), cache.v.clone()
+    many = [m % 4 for m in range(12)] if add is None else [0, 1, 2, 3]
+    for _ in range(2):
+        cache.advance(i32(many), None if add is None else i32(add))  # more than two copies, or blocks
+        assert cache.check() == 8
+        assert torch.equal(cache.table, table) and torch.equal(cache.lens, lens) and int(cache.free) == 2
+        assert torch.equal(cache.k, k) and torch.equal(cache.v, v)
+        assert cache.check() == 0 and torch.equal(cache.lens, lens)  # once
+    hist = [cached(cache, layer, m) for layer in range(2) for m in (0, 2)]
+    cache.advance(i32([0, 2]), i32([5, 9]))      # the two others' pages are free again
+    assert cache.check() == 0 and cache.lens.tolist() == [23, 22] and int(cache.free) == 9 - 3 - 3
+    for (layer, m), (hk, hv) in zip([(l, m) for l in range(2) for m in (0, 1)], hist):
+        n, (gk, gv) = len(hk), cached(cache, layer, m)
+        assert torch.equal(gk[:n], hk) and torch.equal(gv[:n], hv)
+    # rows that are given back are no loss: nothing to go back to, whatever another cache of the layer has reported
+    cache.advance(i32([-1, -1]), i32([0, 0]))
+    assert cache.check() == 0 and cache.lens.tolist() == [0, 0] and int(cache.free) == 9

@@ -424,7 +424,8 @@ class SsmLayer:
 class PagedCache:
     """The keys and values of a program's attention layers in pages, k, v [layers, n_pages, Hk, page, Dh], and the table and
     lengths of its current rows: prompts first, then hypotheses that continue one another's.  Making one, and the first
-    advance to a number of rows, wait for the device (unless captured into a graph): any stream may follow.
+    advance to a number of rows from one power of two to the next, wait for the device (unless captured into a graph): any
+    stream may follow.
 
     An advance that finds too few pages writes none and leaves rows of no positions, over which a layer's calls give zeros;
     check() says so and goes back.  Where the pool may run out it has to be called before the next advance, which
@@ -436,7 +437,7 @@ class PagedCache:
         self.k, self.v = (torch.zeros(shape, dtype=attn.dtype, device=attn.device) for _ in range(2))
         self.free = torch.full((1,), n_pages, dtype=torch.int32, device=attn.device)
         self._spare, self._before = {}, None
-        self.table, self.lens = self._rows(1)  # one empty row, for new ones to begin with
+        self.table, self.lens, _ = self._rows(1)  # one empty row, for new ones to begin with
         self.lens.zero_()
         self._wait()
 
@@ -446,24 +447,26 @@ class PagedCache:
                 torch.cuda.synchronize(self.attn.device)
 
     def _rows(self, n):
-        """A table and lengths of n rows that are not the current ones."""
-        i32 = dict(dtype=torch.int32, device=self.attn.device)
-        if n not in self._spare:
-            pair = [(torch.empty(n, self.n_blocks, **i32), torch.empty(n, **i32)) for _ in range(2)]
-            self._spare[n] = pair, torch.empty(mt.mt_pages_workspace_bytes(self.attn, n, self.k.shape[1]), dtype=torch.uint8,
-                                               device=self.attn.device)
+        """A table and lengths of n rows that are not the current ones, and a workspace: of two each for up to a power of two."""
+        i32, most = dict(dtype=torch.int32, device=self.attn.device), 1 << (n - 1).bit_length()
+        if most not in self._spare:
+            ws = mt.mt_pages_workspace_bytes(self.attn, most, self.k.shape[1])
+            self._spare[most] = [(torch.empty(most, self.n_blocks, **i32), torch.empty(most, **i32)) for _ in range(2)] + [
+                torch.empty(ws, dtype=torch.uint8, device=self.attn.device)]
             self._wait()
-        pair = self._spare[n][0]
-        return pair[1] if getattr(self, "table", None) is pair[0][0] else pair[0]
+        one, other, ws = self._spare[most]
+        current = getattr(self, "table", None)
+        table, lens = other if current is not None and current.data_ptr() == one[0].data_ptr() else one
+        return table[:n], lens[:n], ws
 
     def advance(self, src_row, add=None, stream=None):
         """Rows that continue src_row [M] int32 (below 0: new ones) of the current ones, with room for add [M] (None: 1 each)
         more positions."""
         n = src_row.numel()
-        table, lens = self._rows(n)
+        table, lens, ws = self._rows(n)
         with torch.cuda.device(self.attn.device):
             mt.mt_pages_advance(self.attn, src_row, add, self.table, self.lens, table, lens, self.k, self.v, free_out=self.free,
-                                ws=self._spare[n][1], stream=stream)
+                                ws=ws, stream=stream)
         self._before = self.table, self.lens  # as they were until the next advance
         self.table, self.lens = table, lens
 
@@ -475,9 +478,9 @@ class PagedCache:
             if flags & 8 and self._before and int(self.free) == self.k.shape[1] and not bool(self.lens.any()):
                 (self.table, self.lens), self._before = self._before, None
                 n = self.lens.numel()  # the free pages beside these rows: that of a step in which none grows
-                table, lens = self._rows(n)
+                table, lens, ws = self._rows(n)
                 mt.mt_pages_advance(self.attn, None, torch.zeros_like(self.lens), self.table, self.lens, table, lens, self.k, self.v,
-                                    free_out=self.free, ws=self._spare[n][1])
+                                    free_out=self.free, ws=ws)
                 self._wait()
         return flags
 
@@ -486,7 +489,7 @@ class PagedCache:
         suffice, which check() tells; this cache stays as it is)."""
         out = PagedCache(self.attn, self.k.shape[0], n_pages, self.n_blocks)
         n = self.lens.numel()
-        table, lens = out._rows(n)
+        table, lens, _ = out._rows(n)
         ws = torch.empty(mt.mt_pages_workspace_bytes(self.attn, n, self.k.shape[1]), dtype=torch.uint8, device=self.attn.device)
         self._wait()
         with torch.cuda.device(self.attn.device):

@@ -308,3 +308,25 @@ def test_a_step_without_room_is_taken_back(add):
     # rows that are given back are no loss: nothing to go back to, whatever another cache of the layer has reported
     cache.advance(i32([-1, -1]), i32([0, 0]))
     assert cache.check() == 0 and cache.lens.tolist() == [0, 0] and int(cache.free) == 9
+
+
+def test_a_shrinking_beam_stays_in_its_buffers():
+    """From 16 hypotheses to 9, and back: no new buffers, no wait for the device, every row what it continues."""
+    attn = mt.mt_attn_load(mt.make_attn_config(1, 1, 8, page=8))
+    cache = PagedCache(attn, 1, 60, 4)
+    cache.advance(i32([-1] * 16), i32([1 + m % 3 for m in range(16)]))
+    lens = [1 + m % 3 for m in range(16)]
+    g = gen(9)
+    cache._wait = lambda: pytest.fail("waits for the device")
+    for n in [15, 14, 13, 12, 11, 10, 9, 12, 16]:
+        src = torch.randint(0, len(lens), (n,), generator=g).tolist()
+        before, pages = cache.table.tolist(), cache.table.data_ptr()
+        cache.advance(i32(src))
+        lens = [lens[r] + 1 for r in src]
+        assert cache.lens.tolist() == lens and cache.table.shape == (n, 4) and cache.table.data_ptr() != pages
+        table = cache.table.tolist()
+        written = [t[(ln - 1) // 8] for t, ln in zip(table, lens)]
+        assert len(set(written)) == n  # a page of its own to go on writing
+        for t, r, ln in zip(table, src, lens):
+            assert t[:(ln - 1) // 8] == before[r][:(ln - 1) // 8]
+    assert mt.mt_attn_device_errors(attn) == 0

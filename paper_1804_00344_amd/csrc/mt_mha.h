@@ -28,6 +28,14 @@ struct MhaArgs {
   int32_t *err;
   int num_cu;
 };
+// How a call is split over the chip
+struct MhaPlan {
+  int tiles, parts;        // of a key head's rows; of the key axis
+  bool step, few, share;   // tiles of 32 rows, not of 128; of those, of four by the vector units; waves share a tile's keys
+  bool sort;               // masked sentences by their work
+  bool ends;               // the ends of masks looked for once and not by every workgroup
+};
+MhaPlan mha_plan(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window, bool f32, int num_cu);
 size_t mha_workspace_bytes(int Hq, int Hk, int Dh, bool f32, int B, int S, long long n_keys, int window, int num_cu);
 hipError_t launch_mha(const MhaArgs &a, hipStream_t st);
 
@@ -46,6 +54,12 @@ struct AppendArgs {
   int32_t *err;
   int num_cu;
 };
+// positions of a workgroup, and whether results are stored past the L2s
+struct AppendForm {
+  int tokens;
+  bool stream;
+};
+AppendForm append_form(int B, int S, int Hq, int Hk, int Dh, int esize, bool aligned, int num_cu);
 hipError_t launch_append(const AppendArgs &a, hipStream_t st);
 
 // ---- page tables (mt_pages.hip) ----

@@ -8,18 +8,11 @@
 namespace mt {
 
 namespace {
-
-struct Plan {
-  bool step, share, few;
-  bool sort;  // masked sentences by their work
-  bool ends;  // the ends of masks looked for once and not by every workgroup
-  int tiles, parts;
-};
-
 constexpr int kMaxSort = 1024;
+}  // namespace
 
-Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window, bool f32, int num_cu) {
-  Plan p;
+MhaPlan mha_plan(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window, bool f32, int num_cu) {
+  MhaPlan p;
   const long long rows = (long long)S * (Hq / Hk), heads = (long long)B * Hk;
   if (window && n_keys > (long long)window + S) n_keys = (long long)window + S;  // keys that a row's queries see
   // The key axis is cut until there are enough workgroups; where there are many parts, each has 256 keys at least.  Tiles of
@@ -87,6 +80,8 @@ Plan plan_of(int Hq, int Hk, int Dh, int B, int S, long long n_keys, int window,
   p.ends = p.sort || n_keys >= 8192;
   return p;
 }
+
+namespace {
 
 // The first valid position of each sentence and one past its last: a workgroup each
 __global__ void __launch_bounds__(1024) edges_kernel(const float *mask, int S, int2 *edges) {
@@ -190,7 +185,7 @@ void launch_join(const MhaArgs &a, int n_parts, hipStream_t st) {
 size_t mha_workspace_bytes(int Hq, int Hk, int Dh, bool f32, int B, int S, long long n_keys, int window, int num_cu) {
   size_t most = 256;  // of both attentions: only that over pages has the window
   for (int w : {window, 0}) {
-    const Plan p = plan_of(Hq, Hk, Dh, B, S, n_keys, w, f32, num_cu);
+    const MhaPlan p = mha_plan(Hq, Hk, Dh, B, S, n_keys, w, f32, num_cu);
     size_t n = p.parts > 1 ? (parts_bytes((long long)B * Hq * S, p.parts, Dh) + 255) / 256 * 256 : 256;
     if (p.ends) n += (size_t)kMaxSort * 4 + ((size_t)B * 8 + 255) / 256 * 256;  // behind the parts: places and edges
     if (n > most) most = n;
@@ -199,7 +194,7 @@ size_t mha_workspace_bytes(int Hq, int Hk, int Dh, bool f32, int B, int S, long 
 }
 
 hipError_t launch_mha(const MhaArgs &a, hipStream_t st) {
-  const Plan p = plan_of(a.Hq, a.Hk, a.Dh, a.B, a.S, a.table ? (long long)a.n_blocks << a.page_log2 : a.Sk, a.window,
+  const MhaPlan p = mha_plan(a.Hq, a.Hk, a.Dh, a.B, a.S, a.table ? (long long)a.n_blocks << a.page_log2 : a.Sk, a.window,
                         !a.bf16_io, a.num_cu);
   int *order = nullptr;
   int2 *edges = nullptr;

@@ -242,38 +242,53 @@ void launch_as(const AppendArgs &a, hipStream_t st) {
                        a, per_row, base);
 }
 
-// Several positions of a workgroup share its start and keep loads on their way: only where there are enough of them, and
-// as many as fill its lanes (87 x 1507 of 2 heads of 64: 4 positions 152 us, 16 97).  Aligned results larger than the
-// L2s together are stored past them (8 x 4096 x 48 heads of 128, two heads a lane: 192 -> 166 us).
 template <typename T, int LP>
 hipError_t by_rows(const AppendArgs &a, hipStream_t st) {
-  const long long rows = (long long)a.B * a.S;
-  const bool many = rows >= 16ll * a.num_cu && a.S >= 4;
   const bool aligned = (uintptr_t)a.qo % 16 == 0 && a.ldqo % (16 / (int)sizeof(T)) == 0;
-  if (many && aligned && (double)rows * (a.Hq + 2 * a.Hk) * a.Dh * sizeof(T) > 32e6 && (a.Hq + a.Hk) * LP > 128)
+  const AppendForm f = append_form(a.B, a.S, a.Hq, a.Hk, a.Dh, sizeof(T), aligned, a.num_cu);
+  if (f.stream)
     launch_as<T, LP, 4, true>(a, st);
-  else if (many && (a.Hq + a.Hk) * LP <= 128 && rows >= 64ll * a.num_cu && a.S >= 16)
+  else if (f.tokens == 16)
     launch_as<T, LP, 16, false>(a, st);
-  else if (many)
+  else if (f.tokens == 4)
     launch_as<T, LP, 4, false>(a, st);
   else
     launch_as<T, LP, 1, false>(a, st);
   return hipGetLastError();
 }
 
+// lanes of a head
+int head_lanes(int Dh, int esize) {
+  int n = 1;
+  while (n * 16 < Dh * esize) n *= 2;
+  return n;
+}
+
 template <typename T>
 hipError_t by_lanes(const AppendArgs &a, hipStream_t st) {
-  const int lanes = (a.Dh * (int)sizeof(T) + 15) / 16;
-  if (lanes <= 1) return by_rows<T, 1>(a, st);
-  if (lanes <= 2) return by_rows<T, 2>(a, st);
-  if (lanes <= 4) return by_rows<T, 4>(a, st);
-  if (lanes <= 8) return by_rows<T, 8>(a, st);
-  if (lanes <= 16) return by_rows<T, 16>(a, st);
-  if (lanes <= 32) return by_rows<T, 32>(a, st);
+  switch (head_lanes(a.Dh, sizeof(T))) {
+    case 1: return by_rows<T, 1>(a, st);
+    case 2: return by_rows<T, 2>(a, st);
+    case 4: return by_rows<T, 4>(a, st);
+    case 8: return by_rows<T, 8>(a, st);
+    case 16: return by_rows<T, 16>(a, st);
+    case 32: return by_rows<T, 32>(a, st);
+  }
   return by_rows<T, 64>(a, st);
 }
 
 }  // namespace
+
+// Several positions of a workgroup share its start and keep loads on their way: only where there are enough of them, and
+// as many as fill its lanes (87 x 1507 of 2 heads of 64: 4 positions 152 us, 16 97).  Aligned results larger than the
+// L2s together are stored past them (8 x 4096 x 48 heads of 128, two heads a lane: 192 -> 166 us).
+AppendForm append_form(int B, int S, int Hq, int Hk, int Dh, int esize, bool aligned, int num_cu) {
+  const long long rows = (long long)B * S;
+  const int lanes = (Hq + Hk) * head_lanes(Dh, esize);
+  if (rows < 16ll * num_cu || S < 4) return {1, false};
+  if (aligned && (double)rows * (Hq + 2 * Hk) * Dh * esize > 32e6 && lanes > 128) return {4, true};
+  return {lanes <= 128 && rows >= 64ll * num_cu && S >= 16 ? 16 : 4, false};
+}
 
 hipError_t launch_append(const AppendArgs &a, hipStream_t st) {
   return a.bf16_io ? by_lanes<bf16>(a, st) : by_lanes<float>(a, st);

@@ -32,3 +32,28 @@ def encoder_form(B, H, bf16):
 
 def vocab_chunks(E, V, M, bf16=1, num_cu=256):
     return _fn("_ZN2mt12vocab_chunksEiiiii", C.c_int, 5)(bf16, M, V, E, num_cu)
+
+
+class MhaPlan(C.Structure):
+    _fields_ = [("tiles", C.c_int), ("parts", C.c_int)] + [(n, C.c_bool) for n in ("step", "few", "share", "sort", "ends")]
+
+
+def attn_plan(B, S, Hq, Hk, Dh, n_keys, dtype, window=0, num_cu=256):
+    """(form, parts of the key axis, whether waves share a tile's keys, masked sentences sorted) of mt_attn_paged or mt_attn_cross;
+    the form: "rows" (tiles of four by the vector units), "steps" (tiles of 32 rows) or "tiles" (of 128)."""
+    f = mt.lib()._ZN2mt8mha_planEiiiiixibi
+    f.restype, f.argtypes = MhaPlan, [C.c_int] * 5 + [C.c_longlong, C.c_int, C.c_bool, C.c_int]
+    p = f(Hq, Hk, Dh, B, S, n_keys, window, dtype == "f32", num_cu)
+    return "rows" if p.few else "steps" if p.step else "tiles", p.parts, p.share, p.sort
+
+
+class AppendForm(C.Structure):
+    _fields_ = [("tokens", C.c_int), ("stream", C.c_bool)]
+
+
+def append_form(B, S, Hq, Hk, Dh, dtype, aligned=True, num_cu=256):
+    """(positions of a workgroup, whether results are stored past the L2s) of mt_attn_append."""
+    f = mt.lib()._ZN2mt11append_formEiiiiiibi
+    f.restype, f.argtypes = AppendForm, [C.c_int] * 6 + [C.c_bool, C.c_int]
+    r = f(B, S, Hq, Hk, Dh, 4 if dtype == "f32" else 2, aligned, num_cu)
+    return r.tokens, r.stream

@@ -330,3 +330,43 @@ def test_a_shrinking_beam_stays_in_its_buffers():
         for t, r, ln in zip(table, src, lens):
             assert t[:(ln - 1) // 8] == before[r][:(ln - 1) // 8]
     assert mt.mt_attn_device_errors(attn) == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_tables_follow_a_beam_search(dtype):
+    """Prompts, then steps whose hypotheses mt_beam_topk chooses: its row_out is mt_pages_advance's src_row as it stands."""
+    from paper_1804_00344_amd import synth
+    from paper_1804_00344_amd.runner import Decoder
+    B, S, K, V, n_blocks = 3, 13, 4, 500, 4
+    w, l = make(3, dtype)
+    cache = PagedCache(l.attn, 1, 50, n_blocks)
+    l.set_batch(B, S, K, n_blocks * PAGE)
+    g = gen(10)
+    new = [13, 1, 7]
+    cache.advance(i32([-1] * B), i32(new))
+    l.prompt(torch.randn(B, S, E, generator=g).to(l.io_dtype).to(DEV), cache, 0, i32(new))
+    hist = [cached(cache, 0, m) for m in range(B)]
+    p = synth.with_sizes(synth.PRESETS["tiny_f32"], V=V, B=B, K=K)
+    dec = Decoder.from_preset(p, synth.make_weights(p))
+    M = B * K
+    ws = torch.empty(mt.mt_workspace_bytes(dec.model, B, K, 8), dtype=torch.uint8, device=DEV)
+    emb, wo = (torch.randn(V, E, generator=g).to(DEV) for _ in range(2))
+    score = torch.tensor([0.0] + [-1e30] * (K - 1), device=DEV).repeat(B)  # one live hypothesis each
+    tok, bp = torch.ones(M, dtype=torch.int32, device=DEV), torch.empty(M, dtype=torch.int32, device=DEV)
+    row = i32([m // K for m in range(M)])  # the first step continues the prompts
+    forked = False
+    for t in range(8):
+        cache.advance(row)
+        parents = row.tolist()
+        forked = forked or (t > 0 and len(set(parents)) < M)
+        out = l.step(emb[tok.long()].to(l.io_dtype), cache, 0)
+        v_new = l.sb["qkv"][:, 0, QD + KD:]
+        kv = [cached(cache, 0, m) for m in range(M)]
+        for m, r in enumerate(parents):  # its parent's positions, and its own
+            (k, v), (ok, ov) = kv[m], hist[r]
+            assert len(k) == len(ok) + 1 and torch.equal(k[:-1], ok) and torch.equal(v[:-1], ov), (t, m)
+            assert torch.equal(v[-1], v_new[m].cpu())
+        hist = kv
+        logp = torch.log_softmax(out.float() @ wo.T, 1)
+        mt.mt_beam_topk(dec.model, B, K, score, logp, score, tok, bp, row, ws)
+    assert forked and cache.check() == 0

@@ -601,7 +601,8 @@ mt_status mt_attn_free(mt_attn *a);
 
 /* Norms, rotation and store: q_out = R(norm(q)) for every new position, and R(norm(k)), v into the pages that the
  * tables give them.  q, q_out [B*S, Hq*Dh] (q_out may be q with the same stride), k, v [B*S, Hk*Dh].  No position of a
- * page may be written by two rows.  Angles are formed in 64 bits: exact to a rounding at any position.
+ * page may be written by two rows.  Angles are formed in 64 bits: that of pair i at position p is off by at most
+ * |p freq[i]| 2^-51 + 2^-23 radians.
  * B, S >= 1, B*S <= 2^24; 1 <= n_blocks, n_blocks*page <= 2^30; B*n_blocks <= 2^30; 1 <= n_pages <= 2^24. */
 mt_status mt_attn_append(mt_attn *a, int B, int S, const int32_t *n_new, const int32_t *len, const void *q, int64_t ldq,
                          const void *k, int64_t ldk, const void *v, int64_t ldv, void *q_out, int64_t ldqo,

@@ -103,8 +103,9 @@ mt_status mt_attn_load(const mt_attn_config *cfg, const mt_attn_weights *w, mt_a
     double turns[128];
     float g[512];
   } host;
-  for (int i = 0; i < half; ++i)
-    host.turns[i] = (w->freq ? (double)w->freq[i] : std::pow((double)cfg->rot_base, -2.0 * i / cfg->rot)) / (2 * M_PI);
+  constexpr long double kTurn = 6.283185307179586476925286766559L;
+  for (int i = 0; i < half; ++i)  // rounded once
+    host.turns[i] = (double)((w->freq ? (long double)w->freq[i] : std::pow((long double)cfg->rot_base, -2.0L * i / cfg->rot)) / kTurn);
   for (int i = half; i < 128; ++i) host.turns[i] = 0;
   for (int i = 0; i < 256; ++i) {
     host.g[i] = cfg->qk_norm && w->gq && i < Dh ? w->gq[i] : 1.f;

@@ -44,9 +44,10 @@ __device__ __forceinline__ void put_rows(T *p, const float (&x)[VEC]) {
 
 // A head takes LP lanes (a power of two) of VEC features each, one 16-byte access per lane, and a lane U heads at a
 // time, step by step together: one, as more waves bring more loads on their way than more heads of a lane do (8 x 4096 x
-// 48 heads of 128 in bf16: one 157 us, 5.1 TB/s, two 166, four 210).  A workgroup takes TOK positions of a row, whose angles its threads form first (in 64
-// bits, as turns: the product keeps 2^-22 of a turn at position 2^30) and all heads share.  Partners of a rotation come
-// from the lane half a head away where the lanes are a whole head, else through LDS.
+// 48 heads of 128 in bf16: one 157 us, 5.1 TB/s, two 166, four 210).  A workgroup takes TOK positions of a row, whose
+// angles its threads form first and all heads share: in 64 bits, as turns, so that the factor and the product are off by 2^-53 of
+// themselves each and what is left of the last turn by 2^-26 of one (1.6 roundings of 32 bits, in radians).  Partners of a rotation
+// come from the lane half a head away where the lanes are a whole head, else through LDS.
 template <typename T, int LP, int TOK, bool STREAM>
 __global__ void __launch_bounds__(256) append_kernel(AppendArgs a, int per_row, int base) {
   constexpr int VEC = 16 / sizeof(T), U = 1, HEADS = 256 / LP;

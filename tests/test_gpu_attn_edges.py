@@ -1,5 +1,7 @@
 """The attention layer's operators at the edges of their contracts, on every kernel that a call may take: scores of any finite
 size, windows of any size."""
+from decimal import Decimal, getcontext
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -111,3 +113,33 @@ def test_append_of_more_than_2_to_the_30_heads():
     assert all(torch.equal(x, y) for x, y in zip(out.flatten().split(2 ** 30), q.flatten().split(2 ** 30)))
     for t, c in ((k, kc), (v, vc)):
         assert torch.equal(c.reshape(-1, 8)[:S], t[0]) and bool((c.reshape(-1, 8)[S:] == 0).all())
+
+
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("base", [500.0, 10000.0, 1e30])
+def test_angles_at_any_position(base, given):
+    """Against angles of 50 digits: a frequency in turns and its product with the position are rounded to 64 bits, 2^-53 of it
+    each; what is left of the last turn to 32 bits, 1.6 u (which the bound of a rotation has)."""
+    getcontext().prec = 60
+    turn = 2 * Decimal("3.14159265358979323846264338327950288419716939937510582097494")
+    base = float(torch.tensor(base, dtype=torch.float32))
+    Dh, page, positions = 64, 256, [5, 1000003, 2 ** 24 + 1, 2 ** 30 - 5]
+    exact = [Decimal(base) ** (Decimal(-2 * i) / Dh) for i in range(Dh // 2)]
+    given_freq = torch.tensor([float(f) for f in exact]).float() * 3 if given else None
+    if given:
+        exact = [Decimal(float(f)) for f in given_freq]
+    a = layer(1, 1, Dh, "f32", dict(freq=given_freq) if given else None, page=page, rot=Dh, rot_base=base)
+    g = gen(5)
+    q, k, v = (torch.randn(4, 1, Dh, generator=g) for _ in range(3))
+    table = torch.arange(4, dtype=torch.int32, device=DEV)[:, None].repeat(1, 2 ** 30 // page)
+    kc, vc = (torch.zeros(4, 1, page, Dh, device=DEV) for _ in range(2))
+    out = torch.empty(4, 1, Dh, device=DEV)
+    mt.mt_attn_append(a, dev(q), dev(k), dev(v), out, torch.tensor([p + 1 for p in positions], dtype=torch.int32, device=DEV), table, kc, vc)
+    assert mt.mt_attn_device_errors(a) == 0
+    far = torch.tensor([[float(p * f) for f in exact] for p in positions], dtype=torch.float64).repeat(1, 2)
+    rest = torch.tensor([[float(p * f % turn) for f in exact] for p in positions], dtype=torch.float64)  # of the last turn
+    c, s = torch.cos(rest), torch.sin(rest)
+    for got, x in ((out[:, 0], q), (torch.stack([kc[b, 0, p % page] for b, p in enumerate(positions)]), k)):
+        lo, hi = x[:, 0].double().split(Dh // 2, 1)
+        mag = (lo.abs() + hi.abs()).repeat(1, 2)
+        check(got, torch.cat([lo * c - hi * s, hi * c + lo * s], 1), mag * (8 * U + far * 2.0 ** -51), "rotated")

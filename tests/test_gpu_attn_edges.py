@@ -134,7 +134,8 @@ def test_angles_at_any_position(base, given):
     table = torch.arange(4, dtype=torch.int32, device=DEV)[:, None].repeat(1, 2 ** 30 // page)
     kc, vc = (torch.zeros(4, 1, page, Dh, device=DEV) for _ in range(2))
     out = torch.empty(4, 1, Dh, device=DEV)
-    mt.mt_attn_append(a, dev(q), dev(k), dev(v), out, torch.tensor([p + 1 for p in positions], dtype=torch.int32, device=DEV), table, kc, vc)
+    lens = torch.tensor([p + 1 for p in positions], dtype=torch.int32, device=DEV)
+    mt.mt_attn_append(a, dev(q), dev(k), dev(v), out, lens, table, kc, vc)
     assert mt.mt_attn_device_errors(a) == 0
     far = torch.tensor([[float(p * f) for f in exact] for p in positions], dtype=torch.float64).repeat(1, 2)
     rest = torch.tensor([[float(p * f % turn) for f in exact] for p in positions], dtype=torch.float64)  # of the last turn

@@ -44,8 +44,9 @@ __device__ __forceinline__ void put_rows(T *p, const float (&x)[VEC]) {
 
 // A head takes LP lanes (a power of two) of VEC features each, one 16-byte access per lane, and a lane U heads at a
 // time, step by step together: one, as more waves bring more loads on their way than more heads of a lane do (8 x 4096 x
-// 48 heads of 128 in bf16: one 157 us, 5.1 TB/s, two 166, four 210).  A workgroup takes TOK positions of a row, whose
-// angles its threads form first and all heads share: in 64 bits, as turns, so that the factor and the product are off by 2^-53 of
+// 48 heads of 128 in bf16: one 157 us, 5.1 TB/s, two 166, four 210).  The loops over them stay for the order that the compiler
+// makes of them: written out for one, calls of few positions took 1 to 4% longer (151 tokens of 80 heads of 128 5.5 -> 5.9 us).
+// A workgroup takes TOK positions of a row, whose angles its threads form first and all heads share: in 64 bits, as turns, so that the factor and the product are off by 2^-53 of
 // themselves each and what is left of the last turn by 2^-26 of one (1.6 roundings of 32 bits, in radians).  Partners of a rotation
 // come from the lane half a head away where the lanes are a whole head, else through LDS.
 template <typename T, int LP, int TOK, bool STREAM>
@@ -282,7 +283,7 @@ hipError_t by_lanes(const AppendArgs &a, hipStream_t st) {
 
 // Several positions of a workgroup share its start and keep loads on their way: only where there are enough of them, and
 // as many as fill its lanes (87 x 1507 of 2 heads of 64: 4 positions 152 us, 16 97).  Aligned results larger than the
-// L2s together are stored past them (8 x 4096 x 48 heads of 128, two heads a lane: 192 -> 166 us).
+// L2s together are stored past them (8 x 4096 x 48 heads of 128 in bf16: 164 -> 159 us).
 AppendForm append_form(int B, int S, int Hq, int Hk, int Dh, int esize, bool aligned, int num_cu) {
   const long long rows = (long long)B * S;
   const int lanes = (Hq + Hk) * head_lanes(Dh, esize);

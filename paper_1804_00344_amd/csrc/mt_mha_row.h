@@ -225,31 +225,26 @@ __global__ void __launch_bounds__(256, NR == 1 ? 4 : 2) row_kernel(MhaArgs a, St
           }
         }
     }
-    // ---- weights: the maximum moves where a score passes it by 2^8, as in the step kernel
+    // ---- weights: the maximum moves where a score passes it by 2^8, as in the step kernel.  It is one of the scores before the
+    // scale, so that differences to it are exact near it, whatever the scores' size
     auto larger = [](float x, float y) { return fmaxf(x, y); };
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
       float mx = s[r][0];
 #pragma unroll
       for (int x = 1; x < NL; ++x) mx = fmaxf(mx, s[r][x]);
-      mx = across<CH>(mx, larger) * a.scale;
-      if (__any(mx > m[r] + 8.f)) {
-        const float mn = fmaxf(m[r], mx), c = m[r] == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m[r] - mn);
+      mx = across<CH>(mx, larger);
+      if (__any((mx - m[r]) * a.scale > 8.f)) {
+        const float mn = fmaxf(m[r], mx), c = m[r] == kNegInf ? 0.f : __builtin_amdgcn_exp2f((m[r] - mn) * a.scale);
         m[r] = mn;
         l[r] *= c;
 #pragma unroll
         for (int e = 0; e < EPC; ++e) acc[r][e] *= c;
       }
-      float use = m[r] == kNegInf ? 0.f : m[r], scale = a.scale;
-      if (__any(fabsf(use) >= kFarScore)) {
-#pragma unroll
-        for (int x = 0; x < NL; ++x) s[r][x] = rounded_product(s[r][x], scale) - use;
-        scale = 1.f;  // the exponents as they are
-        use = 0.f;
-      }
+      const float use = m[r] == kNegInf ? 0.f : m[r];
 #pragma unroll
       for (int x = 0; x < NL; ++x) {
-        s[r][x] = __builtin_amdgcn_exp2f(fmaf(s[r][x], scale, -use));
+        s[r][x] = __builtin_amdgcn_exp2f((s[r][x] - use) * a.scale);
         l[r] += s[r][x];
       }
     }
@@ -304,7 +299,7 @@ __global__ void __launch_bounds__(256, NR == 1 ? 4 : 2) row_kernel(MhaArgs a, St
 #pragma unroll
       for (int v = 0; v < 4; ++v) mm = fmaxf(mm, ends[v][r].x);
       const float use = mm == kNegInf ? 0.f : mm;
-      auto factor = [&](float x) { return x == kNegInf ? 1.f : __builtin_amdgcn_exp2f(x - use); };  // sums without a maximum: zeros, or NaN
+      auto factor = [&](float x) { return x == kNegInf ? 1.f : __builtin_amdgcn_exp2f((x - use) * a.scale); };  // sums without a maximum: zeros, or NaN
 #pragma unroll
       for (int v = 0; v < 4; ++v) ll = fmaf(ends[v][r].y, factor(ends[v][r].x), ll);
       const float c = factor(m[r]);
@@ -335,10 +330,13 @@ __global__ void __launch_bounds__(256, NR == 1 ? 4 : 2) row_kernel(MhaArgs a, St
     if (r >= R) break;
     const int i = (r0 + r) / a.G, hq = h * a.G + r0 + r - i * a.G;
     if (plan.parts > 1) {
+      // the sums relative to the maximum times the scale, rounded: less what that is off by, where it is not all that there is
+      const float ms = m[r] * a.scale, c = fabsf(ms) < kFarScore ? __builtin_amdgcn_exp2f(fmaf(m[r], a.scale, -ms)) : 1.f;
       float *po = parts.o + (prow + r) * a.Dh + chunk * EPC;
 #pragma unroll
-      for (int e = 0; e < EPC; e += 4) *(float4 *)(po + e) = make_float4(acc[r][e], acc[r][e + 1], acc[r][e + 2], acc[r][e + 3]);
-      if (lane == 0) parts.ml[prow + r] = make_float2(m[r], l[r]);
+      for (int e = 0; e < EPC; e += 4)
+        *(float4 *)(po + e) = make_float4(acc[r][e] * c, acc[r][e + 1] * c, acc[r][e + 2] * c, acc[r][e + 3] * c);
+      if (lane == 0) parts.ml[prow + r] = make_float2(ms, l[r] * c);
     } else {
       const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
 #pragma unroll

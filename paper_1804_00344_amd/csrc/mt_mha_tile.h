@@ -84,6 +84,7 @@ struct Rows {
   typename M::Q q[STEPS];
   f32x16 o[DB];  // features 32 d + 8 (r / 4) + 4 (lane / 32) + r % 4
   float m, l;    // maximum that the sums are relative to; this half's sum of weights
+  float bound;   // the score from which the maximum moves
 
   __device__ __forceinline__ void start(const T *src, bool live, int Dh) {
     constexpr int VEC = 16 / ES;
@@ -97,7 +98,7 @@ struct Rows {
     }
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] = (f32x16)(0.f);
-    m = kNegInf;
+    m = bound = kNegInf;
     l = 0.f;
   }
 
@@ -120,25 +121,27 @@ struct Rows {
 #pragma unroll
       for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
     mx = both_halves_max(mx) * scale;
-    if (__any(mx > m + 8.f)) {
+    float use = m == kNegInf ? 0.f : m;
+    if (__builtin_expect(__any(mx > bound), 0)) {
       const float mn = fmaxf(m, mx), c = m == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m - mn);
       m = mn;
+      bound = max_bound(m);
+      use = m == kNegInf ? 0.f : m;
       l *= c;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[d][e] *= c;
+      if (__builtin_expect(__any(fabsf(use) >= kFarScore), 0)) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[kb][e] = rounded_product(s[kb][e], scale) - use;
+        scale = 1.f;  // the exponents as they are
+        use = 0.f;
+      }
     }
-    float use = m == kNegInf ? 0.f : m;
     float sum[2] = {};
-    if (__any(fabsf(use) >= kFarScore)) {
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[kb][e] = rounded_product(s[kb][e], scale) - use;
-      scale = 1.f;  // the exponents as they are
-      use = 0.f;
-    }
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll

@@ -1,4 +1,4 @@
-// Device helpers shared by the attention kernels: where a key's features are, what a query sees, and one query by one wave.
+// Device helpers shared by the attention kernels: what a query sees, the ends of masks, where a call's parts go.
 #pragma once
 
 #include "mt_layer_dev.h"
@@ -77,21 +77,6 @@ __device__ __forceinline__ void mask_ends(const float *mask, int n, int t, int s
   }
 }
 
-// page of block j of row b; a number out of range is clamped, and reported by who asks
-__device__ __forceinline__ int block_page(const MhaArgs &a, int b, int j, bool &bad) {
-  const int p = a.table[(long long)b * a.n_blocks + j];
-  bad |= (unsigned)p >= (unsigned)a.n_pages;
-  return min(max(p, 0), a.n_pages - 1);
-}
-
-// element offset of key j of row b and key head h from the cache's (or the rows') beginning
-template <bool PAGED>
-__device__ __forceinline__ long long key_at(const MhaArgs &a, int b, int h, int j, long long ld, bool &bad) {
-  if (PAGED)
-    return ((((long long)block_page(a, b, j >> a.page_log2, bad) * a.Hk + h) << a.page_log2) + (j & ((1 << a.page_log2) - 1))) * a.Dh;
-  return ((long long)b * a.Sk + j) * ld + h * a.Dh;
-}
-
 // Where a call's parts of a result go that the key axis is cut for: part s of row (b*Hk + h)*S*G + i*G + g holds the
 // sums of its keys, the maximum that they are relative to and their weights' sum (both halves of a pair)
 struct Parts {
@@ -106,70 +91,6 @@ __host__ __device__ inline Parts parts_of(void *ws, long long rows, int parts) {
 }
 inline size_t parts_bytes(long long rows, int parts, int Dh) {
   return (size_t)(((rows * parts * 2 + 63) & ~63ll) + rows * parts * Dh) * 4;
-}
-
-// One query head of one query by one wave over its keys in [k0, k1): 64 keys at a time, a key per lane for the scores
-// (running maximum and sum in 32 bits), a feature per lane for the values.  qs: 256 floats of LDS of the wave.  A key
-// that is not seen is not read.  Gives the result, or where po is set the sums and their pair.
-template <typename T, bool PAGED>
-__device__ void attend_one(const MhaArgs &a, const RowSpan &r, int b, int i, int hq, int k0, int k1, float *qs,
-                           float *po, float2 *pml) {
-  constexpr int VEC = 16 / sizeof(T);
-  typedef Vec<T, VEC> V;
-  const int lane = threadIdx.x & 63, h = hq / a.G;
-  const long long row = (long long)b * a.S + i;
-  const T *q = (const T *)a.q + row * a.ldq + (long long)hq * a.Dh;
-  for (int d = lane; d < a.Dh; d += 64) qs[d] = (float)q[d];
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  int lo, hi;
-  seen_keys<PAGED>(a, r, i, lo, hi);
-  lo = max(lo, k0);
-  hi = min(hi, k1);
-  float m = kNegInf, l = 0.f, acc[4] = {};
-  bool bad = false;  // reported by the caller's own reads
-  for (int t = lo; t < hi; t += 64) {
-    const int j = t + lane;
-    const bool seen = j < hi && (PAGED || !a.mask || a.mask[(long long)b * a.Sk + j] != 0.f);
-    float s = kNegInf;
-    if (seen) {
-      const T *k = (const T *)a.k + key_at<PAGED>(a, b, h, j, a.ldk, bad);
-      float x = 0.f;
-      for (int d = 0; d < a.Dh; d += VEC) {
-        const typename V::Raw v = V::raw_any(k + d);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) x = fmaf(qs[d + e], (float)v.v[e], x);
-      }
-      s = rounded_product(x, a.scale);
-    }
-    const float mn = fmaxf(m, wave_max(s)), use = mn == kNegInf ? 0.f : mn;
-    const float p = seen ? __builtin_amdgcn_exp2f(s - use) : 0.f;
-    const float c = m == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m - use);
-    m = mn;
-    l = l * c + wave_sum(p);
-#pragma unroll
-    for (int f = 0; f < 4; ++f) acc[f] *= c;
-    for (unsigned long long left = __ballot(seen); left; left &= left - 1) {
-      const int kk = __builtin_ctzll(left);
-      const float w = lane_f(p, kk);
-      const T *v = (const T *)a.v + key_at<PAGED>(a, b, h, t + kk, a.ldv, bad);
-#pragma unroll
-      for (int f = 0; f < 4; ++f)
-        if (lane + 64 * f < a.Dh) acc[f] = fmaf(w, (float)v[lane + 64 * f], acc[f]);
-    }
-  }
-  T *y = (T *)a.y + row * a.ldy + (long long)hq * a.Dh;
-#pragma unroll
-  for (int f = 0; f < 4; ++f) {
-    const int d = lane + 64 * f;
-    if (d >= a.Dh) continue;
-    if (po)
-      po[d] = acc[f];
-    else
-      Store<T>::put(y + d, l == 0.f ? 0.f : acc[f] / l);
-  }
-  if (po && lane == 0) *pml = make_float2(m, l);
-  __builtin_amdgcn_wave_barrier();
 }
 
 }  // namespace mt

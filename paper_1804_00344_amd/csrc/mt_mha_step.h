@@ -31,7 +31,6 @@ __global__ void __launch_bounds__(256, step_unit(DP, sizeof(T) == 4)) step_kerne
   __shared__ __attribute__((aligned(1024))) char lds[4 * 2 * TB];
   __shared__ float2 ends[4][32];
   __shared__ int2 found[4];
-  __shared__ int odds[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31;
   // a key head's jobs are neighbours on one XCD; or, falling: the last tiles of all heads, which see the most keys, come first,
   // and no XCD has all of a long sequence's
@@ -112,6 +111,18 @@ __global__ void __launch_bounds__(256, step_unit(DP, sizeof(T) == 4)) step_kerne
     __builtin_amdgcn_wave_barrier();
   }
   if (PAGED && (SHARE ? wave : 0) < nt && mv.bad) atomicOr(a.err, kErrPage);
+  if (PAGED && __any(odd)) {  // values that are no numbers where some rows see them and others not: those that do
+    for (t = SHARE ? wave : 0; t < nt; t += every) {
+      const int k0 = lo + t * KT;
+      if (k0 + KT <= hi && k0 >= lo2) continue;
+      mv.put_again(k0, buf);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      me.odd_values(buf + TB, 0, k0 + 4 * (lane >> 5) - qlo, max(qhi - qlo, 0));
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
   me.l = both_halves_sum(me.l);
   // ---- results
   const long long rows = (long long)a.B * a.Hq * a.S;
@@ -127,10 +138,7 @@ __global__ void __launch_bounds__(256, step_unit(DP, sizeof(T) == 4)) step_kerne
       else
         me.put(y, a.Dh);
     }
-    odd = __any(odd);
   } else {
-    const int any_odd = __any(odd);
-    if (lane == 0) odds[wave] = any_odd;
     if (lane < 32) ends[wave][lane] = make_float2(me.m, me.l);
     __syncthreads();
     float m = kNegInf, l = 0.f;
@@ -170,15 +178,6 @@ __global__ void __launch_bounds__(256, step_unit(DP, sizeof(T) == 4)) step_kerne
       }
     }
     if (cut && live && wave == 0 && lane < 32) parts.ml[prow + r] = make_float2(m, l);
-    odd = odds[0] | odds[1] | odds[2] | odds[3];
-  }
-  if (!PAGED || !odd) return;
-  // values that are no numbers where some rows see them and others not: row by row instead
-  if (SHARE) __syncthreads();
-  for (int x = SHARE ? wave : 0; x < kStepRows && r0 + x < R; x += SHARE ? 4 : 1) {
-    const int ii = (r0 + x) / a.G, hh = h * a.G + (r0 + x) - ii * a.G;
-    attend_one<T, PAGED>(a, span, b, ii, hh, lo, lo + nt * KT, (float *)buf, cut ? parts.o + (prow + r0 + x) * a.Dh : nullptr,
-                         cut ? parts.ml + prow + r0 + x : nullptr);
   }
 }
 

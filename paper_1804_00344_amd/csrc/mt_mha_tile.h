@@ -25,6 +25,16 @@ struct Tile<bf16> {
   __device__ static __forceinline__ int swap_v(int row) {
     return ROWB >= 256 ? (row & 3) << 2 : (row & 2) << 1;
   }
+  // Of two elements (one in fp32) those that are no numbers: infinities go to plus as 2^127 or to minus as -2^127, NaN to both, whose
+  // products with 2^127 are infinities again and with zero nothing.  Gives the elements that are numbers.
+  __device__ static __forceinline__ unsigned split(unsigned v, unsigned &plus, unsigned &minus) {
+    auto all = [](unsigned bits) { return (bits & 0x00010001u) * 0xffffu; };
+    const unsigned over = all(((v & 0x7f807f80u) + 0x00800080u) >> 15), nan = all(((v & 0x007f007fu) + 0x007f007fu) >> 7) & over;
+    const unsigned below = all(v >> 15);
+    plus = over & (nan | ~below) & 0x7f007f00u;
+    minus = over & (nan | below) & 0xff00ff00u;
+    return v & ~over;
+  }
   __device__ static __forceinline__ void qk(f32x16 &s, const char *k, const Q &q) {
     s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8 *)k, q, s, 0, 0, 0);
   }
@@ -39,6 +49,12 @@ struct Tile<float> {
   template <int ROWB>
   __device__ static __forceinline__ int swap_v(int row) {
     return (row & 4) << 1;
+  }
+  __device__ static __forceinline__ unsigned split(unsigned v, unsigned &plus, unsigned &minus) {
+    const bool over = (v & 0x7f800000u) == 0x7f800000u, nan = over && (v & 0x007fffffu), below = v >> 31;
+    plus = over && (nan || !below) ? 0x7f000000u : 0u;
+    minus = over && (nan || below) ? 0xff000000u : 0u;
+    return over ? 0u : v;
   }
   __device__ static __forceinline__ void qk(f32x16 &s, const char *k, const Q &q) {
     const f32x4 kk = *(const f32x4 *)k;
@@ -96,10 +112,13 @@ struct Rows {
       if (live && d < Dh) v = Vec<T, VEC>::raw_any(src + d);
       __builtin_memcpy(&q[s], &v, 16);
     }
-#pragma unroll
-    for (int d = 0; d < DB; ++d) o[d] = (f32x16)(0.f);
+    clear();
     m = bound = kNegInf;
     l = 0.f;
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] = (f32x16)(0.f);
   }
 
   // scores of 32 keys, rows row0 .. of the tile in LDS
@@ -194,6 +213,71 @@ struct Rows {
               0, 0);
       }
     }
+  }
+
+  // What values that are no numbers make of the sums of the queries that see them, where the tile's products had zeros for them:
+  // infinities and NaN, added to o.  32 keys, rows row0 .. of the tile in LDS as it was in memory; a query sees this lane's key i of
+  // them where first + i < n.  Products of one sign overflow by themselves; together with the others', or added to an infinity by
+  // the product, they would not.
+  __device__ __forceinline__ void odd_values(const char *vals, int row0, unsigned first, unsigned n) {
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+    auto seen = [&](int e) { return first + 8 * (e / 4) + e % 4 < n ? 0x1p127f : 0.f; };
+    if constexpr (ES == 2) {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef s16x4 __attribute__((address_space(3))) * Lp;
+      const int l16 = lane & 15;
+#pragma unroll 1
+      for (int hf = 0; hf < 2; ++hf) {
+        bf16x8 p;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = (bf16)seen(hf * 8 + e);
+        const int row = row0 + hf * 16 + 4 * half + l16 / 4;
+        const char *from = vals + row * ROWB + (l16 & 1) * 8;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const int c = (4 * d + 2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1)) ^ M::template swap_v<ROWB>(row);
+          union {
+            s16x4 q[2];
+            unsigned w[4];
+            bf16x8 v;
+          } f, minus;
+          f.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lp)(from + (c << 4)));
+          f.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lp)(from + 8 * ROWB + (c << 4)));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) M::split(f.w[i], f.w[i], minus.w[i]);
+          o[d] += __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, p, (f32x16)(0.f), 0, 0, 0);
+          o[d] += __builtin_amdgcn_mfma_f32_32x32x16_bf16(minus.v, p, (f32x16)(0.f), 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll 1
+      for (int e = 0; e < 16; ++e) {
+        const int row = row0 + 8 * (e / 4) + 4 * half + e % 4;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          unsigned plus, minus;
+          M::split(*(const unsigned *)(vals + row * ROWB + (((d * 32 + (lane & 31)) * 4) ^ (M::template swap_v<ROWB>(row) << 4))), plus, minus);
+          o[d] += __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(plus), seen(e), (f32x16)(0.f), 0, 0, 0);
+          o[d] += __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(minus), seen(e), (f32x16)(0.f), 0, 0, 0);
+        }
+      }
+    }
+  }
+
+  // adds o to what put or put_part has stored
+  template <typename R>
+  __device__ __forceinline__ void add(R *y, int Dh) const {
+    const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int f = d * 32 + 2 * e + 4 * half;
+        if (f >= Dh) continue;
+        const auto was = Vec<R, 4>::raw_any(y + f);
+        const float v[4] = {(float)was.v[0] + o[d][e], (float)was.v[1] + o[d][e + 1], (float)was.v[2] + o[d][e + 2], (float)was.v[3] + o[d][e + 3]};
+        Vec<R, 4>::put_any(y + f, v);
+      }
   }
 
   // sums and their pair of a part (l: of both halves)
@@ -335,8 +419,8 @@ struct Mover {
     __builtin_memcpy(&vr[x], &vv, 16);
   }
   // The tile that was fetched, into LDS.  Values that no row may see are zeros (their weights are).  mixed: some rows see
-  // keys of the tile that others do not; says whether one of its values is no number then, as its weights' zeros would
-  // not hide that.
+  // keys of the tile that others do not; values that are no numbers, which zeros of weights would not hide, are zeros then, and
+  // said to have been there.
   __device__ __forceinline__ bool put(int k0, char *buf, bool mixed) {
     unsigned over = 0;
     const bool all = PAGED ? k0 + KT - 1 <= last : seen == (KT == 64 ? ~0ull : (1ull << KT) - 1);
@@ -359,7 +443,27 @@ struct Mover {
       *(int4 *)(buf + r * ROWB + ((chunk ^ swap_k<ROWB>(r)) << 4)) = kr[x];
       *(int4 *)(buf + TB + r * ROWB + ((chunk ^ M::template swap_v<ROWB>(r)) << 4)) = vr[x];
     }
-    return nonfinite<T>(over);
+    const bool odd = nonfinite<T>(over);
+    if (PAGED && __builtin_expect(odd, 0)) {
+#pragma unroll 1
+      for (int r = row; r < KT; r += RSTEP) {
+        int4 *const at = (int4 *)(buf + TB + r * ROWB + ((chunk ^ M::template swap_v<ROWB>(r)) << 4)), v = *at;
+        unsigned a, b;
+        *at = make_int4(M::split(v.x, a, b), M::split(v.y, a, b), M::split(v.z, a, b), M::split(v.w, a, b));
+      }
+    }
+    return odd;
+  }
+  // The values of a tile once more, as they are in memory (few registers: what it follows needs them)
+  __device__ __forceinline__ void put_again(int k0, char *buf) const {
+#pragma unroll 1
+    for (int x = 0; x < KT; x += RSTEP) {
+      const int r = row + x, j = k0 + wave_row + x, page = min(max(table[min(j, last) >> plog], 0), top);
+      const unsigned long long at = (unsigned long long)(unsigned)page * page_bytes + (unsigned)(j & ((1 << plog) - 1)) * rowb;
+      int4 w = *(const int4 *)(v + at + lane_at);
+      if (!feature || k0 + r > last) w = make_int4(0, 0, 0, 0);
+      *(int4 *)(buf + TB + r * ROWB + ((chunk ^ M::template swap_v<ROWB>(r)) << 4)) = w;
+    }
   }
 };
 
@@ -489,22 +593,35 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a,
   const long long rows = (long long)a.B * a.Hq * a.S;
   const Parts parts = parts_of(a.ws, rows, plan.parts);
   const long long prow = part * rows + ((long long)b * a.Hk + h) * a.S * a.G;
+  float *const po = parts.o + (prow + r) * a.Dh;
+  T *const y = (T *)a.y + ((long long)b * a.S + qi) * a.ldy + (long long)hq * a.Dh;
   if (live) {
     if (plan.parts > 1)
-      me.put_part(parts.o + (prow + r) * a.Dh, parts.ml + prow + r, a.Dh);
+      me.put_part(po, parts.ml + prow + r, a.Dh);
     else
-      me.put((T *)a.y + ((long long)b * a.S + qi) * a.ldy + (long long)hq * a.Dh, a.Dh);
+      me.put(y, a.Dh);
   }
   if (!PAGED) return;
-  // values that are no numbers where some rows see them and others not: row by row instead
+  // Values that are no numbers where some rows see them and others not: for the rows that do, into sums of their own, as the
+  // kernel's would have to stay in registers for it (4 x 300 positions of 16 heads of 192 behind 2000 172 -> 192 us).  One NaN in 2 x
+  // 2048 positions over 8192, 32 heads of 128: 521 -> 557 us.
   __syncthreads();
   if (!dirty) return;
-  for (int x = wave; x < kTileRows && r0 + x < R; x += 4) {
-    const int ii = (r0 + x) / a.G, hh = h * a.G + (r0 + x) - ii * a.G;
-    const bool cut = plan.parts > 1;
-    attend_one<T, PAGED>(a, span, b, ii, hh, lo, lo + nt * KT, (float *)lds + wave * 256,
-                         cut ? parts.o + (prow + r0 + x) * a.Dh : nullptr, cut ? parts.ml + prow + r0 + x : nullptr);
+  me.clear();
+  for (int t = 0; t < nt; ++t) {
+    const int k0 = lo + t * KT;
+    if (!mixed(k0)) continue;
+    mv.put_again(k0, lds);
+    __syncthreads();
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) me.odd_values(lds + TB, kb * 32, k0 + kb * 32 + 4 * (lane >> 5) - qlo, max(qhi - qlo, 0));
+    __syncthreads();
   }
+  if (!live) return;
+  if (plan.parts > 1)
+    me.add(po, a.Dh);
+  else
+    me.add(y, a.Dh);
 }
 
 template <typename T, bool PAGED>

@@ -97,6 +97,44 @@ def test_unseen_nonfinite_values_in_tiles(case, dtype):
     assert bool(((y - want).abs() <= tol)[~dirty].all())
 
 
+# and of the other forms: B, S, Hq, Hk, Dh, L, window
+UNSEEN_FEW = [(2, 1, 8, 1, 64, 90, 40), (1, 20, 2, 2, 128, 3000, 0), (3, 9, 6, 2, 40, 120, 30), (2, 4, 2, 2, 256, 300, 0), (300, 5, 8, 8, 64, 60, 0),
+              (2, 60, 4, 4, 192, 200, 70)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", UNSEEN + UNSEEN_PARTS + UNSEEN_FEW, ids=name)
+def test_values_that_are_no_numbers_reach_their_features_alone(case, dtype):
+    """Infinities and NaN among the values, in features of their own: the formula's results for who sees them (infinities of
+    their sign, NaN for NaN and for both signs together) and for every other feature and row."""
+    B, S, Hq, Hk, Dh, L, window = case
+    g = gen(S + L + 1)
+    a = layer(Hq, Hk, Dh, dtype, page=16, window=window)
+    table, n_pages = pages_for([L] * B, 16, -(-L // 16), g)
+    ks, vs, kc, vc = fill_cache(table, [L] * B, 16, Hk, Dh, n_pages, dtype, g)
+    inf, far = float("inf"), max(L - S - (window or 99) + S // 2, 0)
+    bad = [(L - S // 2 - 1, 3, NAN), (L - 1, 4, inf), (L - S // 2 - 1, 5, -inf), (L - S // 3 - 1, 6, inf), (L - 1, 6, -inf), (far, 7, inf),
+           (far, 2, NAN), (min(far + 1, L - 1), Dh - 1, -inf)]
+    bad = [(j, f, x) for (j, f), x in {(j, f): x for j, f, x in bad}.items()]  # of a position's two the last
+    for j, f, x in bad:
+        vc[table[0, j // 16], 0, j % 16, f] = x
+        vs[0][j, f] = 0
+    q = torch.randn(B, S, Hq * Dh, generator=g).to(IO[dtype])
+    y = run_paged(a, dev(q), [L] * B, table, kc, vc)
+    seen, G = ref.causal(L - S, S, L, window), Hq // Hk
+    want, err = ref.heads(q[0].double(), ks[0].double(), vs[0].double(), seen, Hq, Hk, 1 / math.sqrt(Dh), HALF[dtype])
+    for j, f, x in bad:
+        for h in range(G):
+            want[:, h * Dh + f] += torch.where(seen[:, j], torch.tensor(x, dtype=torch.float64), 0.0)
+    got, half = y[0].cpu().double(), 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    numbers = torch.isfinite(want)
+    assert bool((~numbers).any()) and torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+    assert torch.equal(got[torch.isinf(want)], want[torch.isinf(want)])
+    tol = err + half * (want.abs() + err) + 1e-37
+    assert bool(((got - want).abs() <= tol)[numbers].all())
+    assert bool(torch.isfinite(y[1:]).all())
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("Dh", [64, 128, 192])
 @pytest.mark.parametrize("shift", [1, 3])

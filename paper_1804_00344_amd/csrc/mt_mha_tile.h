@@ -100,7 +100,7 @@ struct Rows {
   typename M::Q q[STEPS];
   f32x16 o[DB];  // features 32 d + 8 (r / 4) + 4 (lane / 32) + r % 4
   float m, l;    // maximum that the sums are relative to; this half's sum of weights
-  float bound;   // the score from which the maximum moves
+  float bound;   // the score from which the maximum moves (wide heads have no register for it)
 
   __device__ __forceinline__ void start(const T *src, bool live, int Dh) {
     constexpr int VEC = 16 / ES;
@@ -141,7 +141,7 @@ struct Rows {
       for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
     mx = both_halves_max(mx) * scale;
     float use = m == kNegInf ? 0.f : m;
-    if (__builtin_expect(__any(mx > bound), 0)) {
+    if (__builtin_expect(__any(mx > (DP > 128 ? max_bound(m) : bound)), 0)) {
       const float mn = fmaxf(m, mx), c = m == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m - mn);
       m = mn;
       bound = max_bound(m);
@@ -487,7 +487,7 @@ struct TilePlan {
 template <typename T, int DP, bool PAGED>
 __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a, TilePlan plan) {
   typedef Tile<T> M;
-  // heads of more than 128 features leave no registers for more keys at a time
+  // heads of more than 128 features leave no registers for more keys at a time; in fp32 some 70 are spilled all the same
   constexpr int KT = DP > 128 ? 32 : M::KT, TB = KT * DP * (int)sizeof(T), KB = KT / 32;
   __shared__ __attribute__((aligned(1024))) char lds[4 * TB];
   __shared__ int dirty, edge[2];

@@ -552,7 +552,8 @@ mt_status mt_ssm_device_errors(mt_ssm *cell, int32_t *flags);
  *     table serves all layers.
  *   - A page table is [rows, n_blocks] int32: position p of row r is position p % page of page table[r, p / page].
  *     Rows may hold pages in common.  len [rows] int32 is the number of positions of a row; entries behind its last
- *     block are not read.  Positions of the cache that no row's len covers may hold anything.
+ *     block are not read, all before it have to be pages, also where a window leaves them behind.  Positions of the cache that
+ *     no row's len covers may hold anything.
  *   - n_new [B] int32 (NULL: all S): how many of a row's S new positions there are; they are its last ones, the i-th
  *     is position len - n_new + i (where that is below 0, nothing is stored or seen: zeros).  Rows b*S + i of the
  *     row matrices with i >= n_new[b] are neither read nor written.

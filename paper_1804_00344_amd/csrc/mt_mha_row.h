@@ -330,8 +330,10 @@ __global__ void __launch_bounds__(256, NR == 1 ? 4 : 2) row_kernel(MhaArgs a, St
     if (r >= R) break;
     const int i = (r0 + r) / a.G, hq = h * a.G + r0 + r - i * a.G;
     if (plan.parts > 1) {
-      // the sums relative to the maximum times the scale, rounded: less what that is off by, where it is not all that there is
-      const float ms = m[r] * a.scale, c = fabsf(ms) < kFarScore ? __builtin_amdgcn_exp2f(fmaf(m[r], a.scale, -ms)) : 1.f;
+      // the sums relative to the maximum times the scale, rounded: less what that is off by, where it is not all that there is;
+      // none where it is minus infinity
+      const float ms = m[r] * a.scale, left = ms == kNegInf && m[r] != kNegInf ? 0.f : 1.f;
+      const float c = fabsf(ms) < kFarScore ? __builtin_amdgcn_exp2f(fmaf(m[r], a.scale, -ms)) : left;
       float *po = parts.o + (prow + r) * a.Dh + chunk * EPC;
 #pragma unroll
       for (int e = 0; e < EPC; e += 4)

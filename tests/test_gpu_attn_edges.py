@@ -144,3 +144,29 @@ def test_angles_at_any_position(base, given):
         lo, hi = x[:, 0].double().split(Dh // 2, 1)
         mag = (lo.abs() + hi.abs()).repeat(1, 2)
         check(got, torch.cat([lo * c - hi * s, hi * c + lo * s], 1), mag * (8 * U + far * 2.0 ** -51), "rotated")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("S,Hq,Dh", [(1, 2, 64), (1, 2, 256), (4, 2, 128), (20, 2, 64)])
+def test_scores_that_are_minus_infinity_in_powers_of_two(S, Hq, Dh, dtype):
+    """Finite scores below -2^128 / log2(e), as many parts of the key axis hold alone: their keys weigh nothing beside others."""
+    L, page = 9000, 64
+    g = gen(S)
+    a = layer(Hq, Hq, Dh, dtype, page=page, scale=1.0)
+    table, n_pages = pages_for([L], page, -(-L // page), g)
+    ks, vs, kc, vc = fill_cache(table, [L], page, Hq, Dh, n_pages, dtype, g, fill=0.0)
+    kc.zero_()
+    q = torch.zeros(1, S, Hq * Dh)
+    q.view(1, S, Hq, Dh)[..., 5] = 2.0 ** 64
+    far = torch.arange(L) < L - S - 2500
+    far[-S - 7::5] = False
+    for j in range(L):
+        if far[j]:
+            kc[table[0, j // page], :, j % page, 5] = -2.0 ** 62 * 3.75
+    y = run_paged(a, dev(q.to(IO[dtype])), [L], table, kc, vc)[0]
+    v = vs[0].double()
+    for i in range(S):
+        seen = (~far) & (torch.arange(L) <= L - S + i)
+        n = int(seen.sum())
+        want = v[seen].mean(0, keepdim=True)
+        check(y[i:i + 1], want, v[seen].abs().mean(0, keepdim=True) * (HALF[dtype] + 4 * (n + 16) * U), i)

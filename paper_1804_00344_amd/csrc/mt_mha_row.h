@@ -342,7 +342,7 @@ __global__ void __launch_bounds__(256, NR == 1 ? 4 : 2) row_kernel(MhaArgs a, St
     } else {
       const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
 #pragma unroll
-      for (int e = 0; e < EPC; ++e) acc[r][e] *= inv;
+      for (int e = 0; e < EPC; ++e) acc[r][e] = times_or_zero(acc[r][e], inv);
       V::put_any((T *)a.y + ((long long)b * a.S + i) * a.ldy + (long long)hq * a.Dh + chunk * EPC, acc[r]);
     }
   }

@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(256, step_unit(DP, sizeof(T) == 4)) step_kerne
         *(float4 *)(po + f) = make_float4(v[0], v[1], v[2], v[3]);
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] *= inv;
+        for (int e = 0; e < 4; ++e) v[e] = times_or_zero(v[e], inv);
         Vec<T, 4>::put_any(y + f, v);
       }
     }

@@ -300,7 +300,9 @@ struct Rows {
 #pragma unroll
       for (int e = 0; e < 16; e += 4) {
         const int f = d * 32 + 2 * e + 4 * half;
-        const float v[4] = {o[d][e] * inv, o[d][e + 1] * inv, o[d][e + 2] * inv, o[d][e + 3] * inv};
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = times_or_zero(o[d][e + i], inv);
         if (f < Dh) Vec<T, 4>::put_any(y + f, v);
       }
   }
@@ -595,6 +597,7 @@ __global__ void __launch_bounds__(256, DP <= 128 ? 2 : 1) tile_kernel(MhaArgs a,
   const long long prow = part * rows + ((long long)b * a.Hk + h) * a.S * a.G;
   float *const po = parts.o + (prow + r) * a.Dh;
   T *const y = (T *)a.y + ((long long)b * a.S + qi) * a.ldy + (long long)hq * a.Dh;
+  if (plan.parts == 1 && me.l == 0.f) qhi = qlo;  // a row without any weight: zeros, whatever it sees
   if (live) {
     if (plan.parts > 1)
       me.put_part(po, parts.ml + prow + r, a.Dh);

@@ -170,3 +170,25 @@ def test_scores_that_are_minus_infinity_in_powers_of_two(S, Hq, Dh, dtype):
         n = int(seen.sum())
         want = v[seen].mean(0, keepdim=True)
         check(y[i:i + 1], want, v[seen].abs().mean(0, keepdim=True) * (HALF[dtype] + 4 * (n + 16) * U), i)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", SIZES, ids=lambda c: "-".join(str(v) for v in c))
+def test_scores_of_minus_infinity_give_zeros_whatever_the_values(case, dtype):
+    B, S, Hq, Hk, Dh, L = case
+    g = gen(S + L)
+    a = layer(Hq, Hk, Dh, dtype, page=16)
+    lens = [L - 7 * b for b in range(B)]
+    table, n_pages = pages_for(lens, 16, -(-L // 16), g)
+    _, _, kc, vc = fill_cache(table, lens, 16, Hk, Dh, n_pages, dtype, g, fill=0.0)
+    vc[table[0, ::2].long(), :, 3, ::5] = float("nan")
+    vc[table[0, ::2].long(), :, 7, 1::7] = float("inf")
+    vc[table[0, -(-L // 16) - 1], :, :, 1] = float("-inf")
+    kc.zero_()
+    kc[..., 0] = float("-inf")
+    q = dev(torch.ones(B, S, Hq * Dh).to(IO[dtype]))
+    assert bool((run_paged(a, q, lens, table, kc, vc, [min(S, n) for n in lens])[0] == 0).all())
+    k, v = torch.zeros(B, L, Hk * Dh), torch.randn(B, L, Hk * Dh, generator=g)
+    k[..., ::Dh] = float("-inf")
+    v[0, ::3, 5], v[0, L // 2:, 2] = float("nan"), float("inf")
+    assert bool((run_cross(a, q, dev(k.to(IO[dtype])), dev(v.to(IO[dtype])))[0] == 0).all())

@@ -151,11 +151,13 @@ struct Rows {
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[d][e] *= c;
-      if (__builtin_expect(__any(fabsf(use) >= kFarScore), 0)) {
+      const bool far = fabsf(use) >= kFarScore;
+      if (__builtin_expect(__any(far), 0)) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) s[kb][e] = rounded_product(s[kb][e], scale) - use;
+          for (int e = 0; e < 16; ++e)
+            s[kb][e] = far ? rounded_product(s[kb][e], scale) - use : fmaf(s[kb][e], scale, -use);
         scale = 1.f;  // the exponents as they are
         use = 0.f;
       }

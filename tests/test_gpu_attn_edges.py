@@ -81,6 +81,15 @@ def test_scores_of_any_finite_size(case, size, sign, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sign", ["plus", "minus", "both"])
+@pytest.mark.parametrize("size", [24, 27, 28, 29, 32])
+@pytest.mark.parametrize("case", [SIZES[i] for i in (2, 3, 6, 7)] + [(2, 102, 48, 16, 128, 107)], ids=lambda c: "-".join(str(v) for v in c))
+def test_scores_of_neighbouring_rows_on_both_sides_of_a_size(case, size, sign, dtype):
+    """Equal scores of a row have equal weights, wherever those of the rows beside it lie."""
+    test_scores_of_any_finite_size(case, size, sign, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("S,Hq,Hk,Dh,B", [(4, 2, 2, 64, 3), (4, 2, 2, 256, 3), (20, 4, 2, 64, 3), (300, 16, 16, 64, 8)])
 def test_a_window_past_every_position(S, Hq, Hk, Dh, B, dtype):
     """The largest window is none, also where rows have fewer positions than new ones."""
